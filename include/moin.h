@@ -77,7 +77,11 @@ typedef enum {
     MOIN_K_MX_LINEAR = 12,    /* quantised base: y = xq Wq^T + u B_e^T           */
     MOIN_K_PROBE_MFMA = 13,   /* measurement aid: bf16 matrix-core loop            */
     MOIN_K_PROBE_READ = 14,   /* measurement aid: streaming read                   */
-    MOIN_K_COUNT = 15
+    MOIN_K_KV_PLAN = 15,      /* block tables, slot maps, pages given back         */
+    MOIN_K_KV_APPEND = 16,    /* tokens into the paged cache, and back             */
+    MOIN_K_KV_ATTEND = 17,    /* attention over the paged cache                    */
+    MOIN_K_MX4_LINEAR = 18,   /* MXFP4 base: y = x Wq^T from the codes, or Wq to bf16 */
+    MOIN_K_COUNT = 19
 } moin_kernel_id;
 
 /* ---- context ----------------------------------------------------------- */
@@ -525,6 +529,123 @@ int moin_merge_adapters(moin_ctx *ctx, const void *A_stack, const void *B_stack,
                         int32_t r, int32_t d_in, int32_t d_out, const int32_t *ids,
                         const float *weights, int32_t n, int32_t r_out, void *A_out, void *B_out,
                         void *stream);
+
+/* ==== serving in four bits =========================================================
+ * A server's device memory goes to its adapters (Section 2; 9.18 MB an expert and layer at
+ * rank 128 on all projections), so what is not an adapter is held in MXFP4 here: the base
+ * weight ("Future Works", an aggressively quantised base) and the cache of keys and values.
+ * Blocks of 32 values share a power of two 2^(E-127) (byte E) and hold E2M1 elements:
+ * 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives, the even one of a pair in the low nibble.
+ * E is that of the smallest power of two, 2^-125 to 2^125, in whose units the block's largest
+ * magnitude rounds to 6 or less (above 2.98e38 it becomes 6 units, 2.55e38); elements are rounded to nearest, ties to even; a
+ * block of zeros has E = 127; a block with a NaN or an infinity has E = 255 and
+ * stands for 32 NaNs.  Every other value is exact in bf16. */
+
+/* ---- 4-bit base weight --------------------------------------------------------
+ * A weight [rows, cols] is held in records of 16 rows x 512 columns, 4352 bytes each,
+ * [ceil(rows/16)][ceil(cols/512)], padded with zeros: column 128 j + 32 g + c of row m
+ * at byte [j][g][m][c/2], then the scale bytes at [g][m][j].
+ *   moin_mx4_bytes       bytes of a weight's records (0: sizes that are not supported)
+ *   moin_mx4_quantize    src [rows, cols] bf16 -> packed
+ *   moin_mx4_dequantize  packed -> dst [rows, cols] bf16, the values that the codes stand for
+ * cols a multiple of 8, pointers 16-byte aligned; else MOIN_EINVAL.
+ *   moin_mx4_linear      y [T, d_out] = x [T, d_in] dq(W4)^T, any T.
+ *   moin_lora_linear_mx4_planned
+ *                        moin_lora_linear_planned on such a base: y = x dq(W4)^T +
+ *                        scale * act(x A_e^T) B_e^T.
+ * x, stacks, y, sizes, workspace and errors as in moin_lora_linear_planned.  Up to 256 tokens
+ * (gathered ones, where there are adapters) are multiplied with the codes; beyond, the
+ * call turns the weight into bf16 in the context's workspace (2 d_in d_out bytes more) and
+ * the results are, bit for bit, those of a bf16 weight with these values. */
+int64_t moin_mx4_bytes(int64_t rows, int64_t cols);
+int moin_mx4_quantize(moin_ctx *ctx, const void *src, int64_t rows, int64_t cols, void *packed, void *stream);
+int moin_mx4_dequantize(moin_ctx *ctx, const void *packed, int64_t rows, int64_t cols, void *dst, void *stream);
+int moin_mx4_linear(moin_ctx *ctx, const void *x, int64_t T, const void *W4, int32_t d_in, int32_t d_out, void *y,
+                    moin_dtype y_dt, void *stream);
+int moin_lora_linear_mx4_planned(moin_ctx *ctx, const moin_plan *plan, const void *x, const void *W4, const void *A_stack,
+                                 const void *B_stack, int32_t d_in, int32_t d_out, int32_t r, float scale, void *y,
+                                 moin_dtype y_dt, void *stream);
+
+/* ---- paged cache of keys and values ---------------------------------------------
+ * The caller owns the pages: data [n_pages][moin_kv_page_bytes], one such array per layer.
+ * page_tokens 64, 128 or 256; head_dim (D) 64, 128 or 256; data 16-byte aligned;
+ * n_pages * page_tokens < 2^31.  A page holds [n_kv][page_tokens / 64] records of 64 tokens,
+ * 68 D bytes each; token 16 i + m of a record (i < 4, m < 16) has its keys at
+ * [i][D/32][m][16 bytes], its values (from byte 32 D on) at [i][D/8][m][4 bytes], its scale bytes
+ * at [D/32][m][i] (keys' from byte 64 D on, values' from 66 D on).  What a page holds
+ * beyond a request's tokens is never used: it may be anything. */
+typedef struct {
+    void *data;
+    int32_t n_pages, page_tokens, n_kv, head_dim;
+} moin_kv_pages;
+int64_t moin_kv_page_bytes(int32_t page_tokens, int32_t n_kv, int32_t head_dim);
+
+/* A step's plan: block tables, slot maps and offsets from the requests' lengths, and how the
+ * attention of the step is dealt over the chip -- once per step, for all layers.
+ *   kv_lens [S]   int32  tokens that request s has in the cache
+ *   new_lens [S]  int32  tokens that the step adds to it; their sum is T; none above max_new
+ *   block_table [S, max_pages] int32  in / out: pages of each request, in order; entries from
+ *                        ceil(kv_lens / page_tokens) on are written as pages are dealt
+ *   free_pages [free_cap] int32, n_free [1] int32  a stack of free pages, dealt from the top in the
+ *                        requests' order: the j-th is free_pages[n_free - 1 - j]
+ *   n_free_out [1], kv_lens_out [S]  int32 out: after the step.  May be n_free and kv_lens
+ *                        themselves
+ *   seq_offsets [S+1] int32 out: the requests' tokens in the batch (as moin_plan_build takes)
+ *   slots [T]     int32 out: page * page_tokens + place in the page of every new token
+ *   n_heads, n_kv        query heads (a multiple of n_kv) and kv heads of the attention
+ * A request that needs more pages than are left, as the requests before it take theirs, or than
+ * its row holds gets none: its length stays, its slots are -1, its attention rows are zeros, and the
+ * sticky data fault is raised.  So it is for lengths that are negative or above max_new, and for
+ * tokens beyond T (T above the sum: slots of -1 there, rows of y left as they are; rows of a request
+ * with more than max_new tokens may be left so too).
+ * The plan serves one stream at a time.  Grows like moin_plan ("HIP graphs" above): a build for the
+ * largest S, T and max_new prepares captured ones only of the same sizes or fewer requests and tokens.
+ * Errors: MOIN_EINVAL (null, negative or unsupported sizes, T * n_heads / n_kv or
+ * S * max_pages at 2^31 and more), MOIN_ENOMEM, MOIN_ECAPTURE. */
+typedef struct moin_kv_plan moin_kv_plan;
+int moin_kv_plan_create(moin_ctx *ctx, moin_kv_plan **out);
+void moin_kv_plan_destroy(moin_kv_plan *plan);
+int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens, const int32_t *new_lens, int32_t S,
+                       int64_t T, int32_t max_new, int32_t n_heads, int32_t n_kv, int32_t page_tokens, int32_t n_pages,
+                       int32_t *block_table, int32_t max_pages, const int32_t *free_pages, int32_t free_cap,
+                       const int32_t *n_free, int32_t *n_free_out, int32_t *kv_lens_out, int32_t *seq_offsets,
+                       int32_t *slots, void *stream);
+
+/* Requests with finished[s] != 0 (int32) give their pages back: pushed on the stack in the
+ * requests' order, their table entries become -1 and their lengths 0, n_free counts them.
+ * Pages that do not exist or do not fit the stack raise the sticky data fault. */
+int moin_kv_release(moin_ctx *ctx, const int32_t *finished, int32_t S, int32_t *kv_lens, int32_t page_tokens,
+                    int32_t n_pages, int32_t *block_table, int32_t max_pages, int32_t *free_pages, int32_t free_cap,
+                    int32_t *n_free, void *stream);
+
+/* moin_kv_append: k, v [T, n_kv, head_dim] bf16, rows of tokens k_stride / v_stride elements apart
+ * (multiples of 8, so that they may be columns of one projection's output), are quantised into the
+ * slots; slot -1 is skipped, no slot may be named twice.
+ * moin_kv_gather: the values that slots [T] hold -> k, v [T, n_kv, head_dim] bf16 (exact); zeros for
+ * slot -1.
+ * Other slots outside the cache raise the sticky data fault and count as -1. */
+int moin_kv_append(moin_ctx *ctx, const moin_kv_pages *pages, const void *k, const void *v, int64_t k_stride,
+                   int64_t v_stride, int64_t T, const int32_t *slots, void *stream);
+int moin_kv_gather(moin_ctx *ctx, const moin_kv_pages *pages, const int32_t *slots, int64_t T, void *k, void *v,
+                   void *stream);
+
+/* Attention of the step's tokens over the cache (their own keys appended before).  Token i of a
+ * request with n new tokens and L keys (kv_lens_out) is at position p = L - n + i and sees the keys
+ * j <= p, with window > 0 only those with j > p - window; query head h reads kv head
+ * h / (n_heads / n_kv):
+ *     y = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  s_j = scale * q . k_j,  m = max_j s_j
+ *   q [T, n_heads, head_dim] bf16, rows of tokens q_stride elements apart (a multiple of 8)
+ *   y [T, n_heads, head_dim] out, bf16 or fp32;  lse [T, n_heads] fp32 out or NULL: m + log(sum)
+ * A row that sees no key is zeros, its lse -inf.  scale > 0 and finite.  A block of NaNs makes the
+ * rows that see it NaN, and no others.  Scores and sums are fp32; the weights enter the second
+ * product as bf16, for fp32 results as the sum of two bf16.  A call repeated gives the same bits.
+ * `plan` is of moin_kv_plan_build with the same n_heads and n_kv and the block_table it filled;
+ * pages that the cache does not have raise the sticky data fault and count as unseen.
+ * Workspace: partial results of keys that are walked in parts.  Errors: MOIN_EINVAL (null, a plan that
+ * is not built, head counts that differ, sizes, alignment), MOIN_ENOMEM, MOIN_ECAPTURE. */
+int moin_kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pages *pages, const void *q, int64_t q_stride,
+                      int32_t n_heads, const int32_t *block_table, int32_t max_pages, float scale, int32_t window, void *y,
+                      moin_dtype y_dt, float *lse, void *stream);
 
 /* ==== measurement aids (not part of the method's path) =========================== */
 

@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "kernels.h"
+#include "kv.h"
 
 namespace moin {
 hipError_t prepare_linear_kernels();
@@ -42,6 +43,16 @@ struct moin_plan {
     // set once a call that uses the plan was recorded into a HIP graph: the graph holds
     // buf's address, so a later regrowth keeps the old block (until moin_plan_destroy)
     mutable int pinned;
+    std::vector<void *> retired;
+};
+
+struct moin_kv_plan {
+    KvPlanView v;
+    void *buf;
+    size_t bytes;
+    int device;
+    int built;
+    mutable int pinned;   // as moin_plan's
     std::vector<void *> retired;
 };
 
@@ -358,7 +369,8 @@ size_t linear_ws_most(const PlanView &pv, int n, int d_in, const int32_t *d_out,
 }
 
 // The plan's buffer, at least `bytes` large; same rules under stream capture as ensure_ws.
-int plan_grow(moin_plan *plan, size_t bytes, hipStream_t st)
+template <class Plan>
+int plan_grow(Plan *plan, size_t bytes, hipStream_t st)
 {
     const bool cap = capturing(st);
     if (bytes > plan->bytes) {
@@ -469,7 +481,7 @@ int validate_linear(const void *x, const void *W, const void *A_stack, const voi
 
 int linear_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, const void *W,
                         const void *A_stack, const void *B_stack, int32_t d_in, int32_t d_out,
-                        int32_t r, float scale, void *y, moin_dtype y_dt, hipStream_t stream)
+                        int32_t r, float scale, void *y, moin_dtype y_dt, hipStream_t stream, bool mx4 = false)
 {
     if (!plan->built) return MOIN_EINVAL;
     const PlanView &pv = plan->pv;
@@ -486,14 +498,28 @@ int linear_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, con
     a.u_hi = a.u_lo = nullptr;
 
     const bool gathered = gathered_pays(pv, d_in, a.r);
+    // W in MXFP4: a few gathered tokens are multiplied with the codes; for more the weight is turned into bf16 (exactly, so that
+    // the results are those of a bf16 weight with these values), at the workspace's start, ahead of everything else there
+    const bool direct = mx4 && gathered && mx4_direct_pays(pv.T, d_in, d_out);
+    const size_t w_bytes = mx4 && !direct ? align_up((size_t)d_out * (size_t)d_in * 2, 256) : 0;
+    const auto reserve = [&](size_t bytes) -> int {
+        const size_t keep = a.r > 0 ? linear_ws_most(pv, 1, d_in, &d_out, r) : 0;
+        const int rc = ensure_ws(ctx, w_bytes + bytes, stream, false, w_bytes + keep);
+        if (rc != MOIN_OK || !w_bytes) return rc;
+        const hipError_t e = timed(ctx, MOIN_K_MX4_LINEAR, stream, [&] { return launch_mx4_dequantize(W, d_out, d_in, ctx->ws, stream); });
+        a.W = ctx->ws;
+        return e == hipSuccess ? MOIN_OK : MOIN_EHIP;
+    };
     a.ldu = gathered ? a.r : prefill_ldu(a);
     const size_t u_bytes = align_up((size_t)pv.T * (size_t)a.ldu * 2, 256);
     if (!gathered) {
-        if (a.r > 0) {
-            const int rc = ensure_ws(ctx, 2 * u_bytes, stream, false, linear_ws_most(pv, 1, d_in, &d_out, r));
+        if (a.r > 0 || w_bytes) {
+            const int rc = reserve(a.r > 0 ? 2 * u_bytes : 0);
             if (rc != MOIN_OK) return rc;
-            a.u_hi = ctx->ws;
-            a.u_lo = static_cast<char *>(ctx->ws) + u_bytes;
+        }
+        if (a.r > 0) {
+            a.u_hi = static_cast<char *>(ctx->ws) + w_bytes;
+            a.u_lo = static_cast<char *>(a.u_hi) + u_bytes;
             if (timed(ctx, MOIN_K_SHRINK, stream, [&] { return launch_prefill_shrink(pv, a, stream); }) !=
                 hipSuccess)
                 return MOIN_EHIP;
@@ -509,17 +535,23 @@ int linear_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, con
     // the contraction into parts.  Us of a call at rank 32, decode tiles / plain ones: 1300 tokens 1000 -> 2048 35 / 31, 8192 139 /
     // 90, 5000 1000 -> 5632 195 / 144, 40 000 1000 -> 136 103 / 96; in parts 1300 5640 -> 256 (22 tiles) 52 / 76, 4000
     // 2056 -> 256 (64) 41 / 43, 2000 5640 -> 1000 (128) 71 / 76, but 1300 5640 -> 2048 (176) 113 / 79.
-    LinearArgs ab = a;
-    ab.r = 0;
-    const bool parts = a.r > 0 && decode_base_splits(pv.T, d_in, d_out) > 1 &&
+    const bool parts = !direct && a.r > 0 && decode_base_splits(pv.T, d_in, d_out) > 1 &&
                        pv.T <= large_parts_tokens(d_in, d_out);
-    const bool big = pv.max_plain > 0 && !parts;
+    const bool big = pv.max_plain > 0 && !parts && !direct;
     PlanView pp = pv;
     pp.tile_row0 = pv.plain_row0; pp.tile_rows = pv.plain_rows; pp.tile_expert = pv.plain_expert;
     pp.tile_rank = pv.plain_rank; pp.n_tiles = pv.plain_n; pp.max_tiles = pv.max_plain;
     if (a.r == 0) {
         // no adapters anywhere in the call: the base GEMM writes y itself
-        if (big) {
+        if (w_bytes) {
+            const int rc = reserve(0);
+            if (rc != MOIN_OK) return rc;
+        }
+        if (direct) {
+            if (timed(ctx, MOIN_K_MX4_LINEAR, stream, [&] { return launch_mx4_linear(x, W, y, a.y_f32, pv.T, d_in, d_out, stream); }) != hipSuccess)
+                return MOIN_EHIP;
+        } else if (big) {
+            LinearArgs ab = a;
             if (timed(ctx, MOIN_K_LINEAR, stream, [&] { return launch_prefill_linear(pp, ab, stream); }) != hipSuccess)
                 return MOIN_EHIP;
         } else if (timed(ctx, MOIN_K_DECODE_BASE, stream, [&] { return launch_decode_base_only(pv, a, stream); }) !=
@@ -528,17 +560,25 @@ int linear_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, con
         return MOIN_OK;
     }
     DecodeArgs d;
-    d.lin = a;
-    d.k_splits = big ? 1 : decode_base_splits(pv.T, d_in, d_out);
+    d.k_splits = big || direct ? 1 : decode_base_splits(pv.T, d_in, d_out);
     const size_t yb_bytes = align_up((size_t)d.k_splits * (size_t)pv.T * (size_t)d_out * 4, 256);
-    const int rc = ensure_ws(ctx, 2 * u_bytes + yb_bytes, stream, false, linear_ws_most(pv, 1, d_in, &d_out, r));
+    const int rc = reserve(2 * u_bytes + yb_bytes);
     if (rc != MOIN_OK) return rc;
-    char *w = static_cast<char *>(ctx->ws);
+    d.lin = a;
+    LinearArgs ab = a;
+    ab.r = 0;
+    char *w = static_cast<char *>(ctx->ws) + w_bytes;
     d.ug_hi = w;
     d.ug_lo = w + u_bytes;
     d.ybase = reinterpret_cast<float *>(w + 2 * u_bytes);
-    d.ybase_by_pos = big ? 0 : 1;   // the small-batch base product gathers its rows in the plan's order
-    if (big) {
+    d.ybase_by_pos = big || direct ? 0 : 1;   // the small-batch base product gathers its rows in the plan's order
+    if (direct) {
+        if (timed(ctx, MOIN_K_MX4_LINEAR, stream, [&] { return launch_mx4_linear(x, W, d.ybase, 1, pv.T, d_in, d_out, stream); }) !=
+            hipSuccess)
+            return MOIN_EHIP;
+        if (timed(ctx, MOIN_K_DECODE_SHRINK, stream, [&] { return launch_decode_shrink(pv, d, stream); }) != hipSuccess)
+            return MOIN_EHIP;
+    } else if (big) {
         ab.y = d.ybase;
         ab.y_f32 = 1;
         if (timed(ctx, MOIN_K_LINEAR, stream, [&] { return launch_prefill_linear(pp, ab, stream); }) != hipSuccess)
@@ -1523,6 +1563,288 @@ int moin_set_adapter_activation(moin_ctx *ctx, int32_t activation)
     if (!ctx || activation < MOIN_ACT_NONE || activation > MOIN_ACT_GELU) return MOIN_EINVAL;
     ctx->act = activation;
     return MOIN_OK;
+}
+
+int64_t moin_mx4_bytes(int64_t rows, int64_t cols)
+{
+    return rows < 0 || cols <= 0 || rows > (1 << 24) || cols > (1 << 22) ? 0 : mx4_bytes(rows, cols);
+}
+
+static int validate_mx4(moin_ctx *ctx, const void *values, const void *packed, int64_t rows, int64_t cols)
+{
+    if (!ctx || rows < 0 || cols <= 0 || cols % 8 || rows > (1 << 24) || cols > (1 << 22)) return MOIN_EINVAL;
+    if (rows > 0 && (!values || !packed || misaligned(values, 16) || misaligned(packed, 16))) return MOIN_EINVAL;
+    return MOIN_OK;
+}
+
+int moin_mx4_quantize(moin_ctx *ctx, const void *src, int64_t rows, int64_t cols, void *packed, void *stream)
+{
+    const int vrc = validate_mx4(ctx, src, packed, rows, cols);
+    if (vrc != MOIN_OK || rows == 0) return vrc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return timed(ctx, MOIN_K_MX_QUANT, st, [&] { return launch_mx4_quantize(src, rows, cols, packed, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+}
+
+int moin_mx4_dequantize(moin_ctx *ctx, const void *packed, int64_t rows, int64_t cols, void *dst, void *stream)
+{
+    const int vrc = validate_mx4(ctx, dst, packed, rows, cols);
+    if (vrc != MOIN_OK || rows == 0) return vrc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return timed(ctx, MOIN_K_MX_QUANT, st, [&] { return launch_mx4_dequantize(packed, rows, cols, dst, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+}
+
+int moin_mx4_linear(moin_ctx *ctx, const void *x, int64_t T, const void *W4, int32_t d_in, int32_t d_out, void *y, moin_dtype y_dt,
+                    void *stream)
+{
+    if (!ctx || T < 0 || T > 0x7fffffffLL - TILE_M) return MOIN_EINVAL;
+    if (T == 0) return MOIN_OK;
+    const int vrc = validate_linear(x, W4, nullptr, nullptr, 0, d_in, d_out, 0, 1.f, y, y_dt);
+    if (vrc != MOIN_OK) return vrc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (mx4_direct_pays(T, d_in, d_out))
+        return timed(ctx, MOIN_K_MX4_LINEAR, st, [&] { return launch_mx4_linear(x, W4, y, y_dt == MOIN_F32, T, d_in, d_out, st); }) == hipSuccess
+                   ? MOIN_OK
+                   : MOIN_EHIP;
+    const int rc = ensure_ws(ctx, align_up((size_t)d_out * (size_t)d_in * 2, 256), st);
+    if (rc != MOIN_OK) return rc;
+    if (timed(ctx, MOIN_K_MX4_LINEAR, st, [&] { return launch_mx4_dequantize(W4, d_out, d_in, ctx->ws, st); }) != hipSuccess) return MOIN_EHIP;
+    LinearArgs a{};
+    a.x = x;
+    a.W = ctx->ws;
+    a.y = y;
+    a.y_f32 = y_dt == MOIN_F32;
+    a.d_in = d_in;
+    a.d_out = d_out;
+    PlanView pv{};
+    pv.T = T;
+    return timed(ctx, MOIN_K_DECODE_BASE, st, [&] { return launch_decode_base_only(pv, a, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+}
+
+int moin_lora_linear_mx4_planned(moin_ctx *ctx, const moin_plan *plan, const void *x, const void *W4, const void *A_stack, const void *B_stack,
+                                 int32_t d_in, int32_t d_out, int32_t r, float scale, void *y, moin_dtype y_dt, void *stream)
+{
+    if (!ctx || !plan || plan->device != ctx->device) return MOIN_EINVAL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    return linear_planned_impl(ctx, plan, x, W4, A_stack, B_stack, d_in, d_out, r, scale, y, y_dt, static_cast<hipStream_t>(stream), true);
+}
+
+// ---- the paged cache ----------------------------------------------------------
+
+static int log2_exact(int v)
+{
+    for (int s = 0; s < 31; ++s)
+        if (v == 1 << s) return s;
+    return -1;
+}
+
+static bool page_tokens_ok(int32_t p) { return p == 64 || p == 128 || p == 256; }
+
+int64_t moin_kv_page_bytes(int32_t page_tokens, int32_t n_kv, int32_t head_dim)
+{
+    if (!page_tokens_ok(page_tokens) || n_kv < 1 || n_kv > (1 << 16) || !kv_head_dim_ok(head_dim)) return 0;
+    return (int64_t)n_kv * (page_tokens / KV_BLOCK) * kv_record_bytes(head_dim);
+}
+
+static int kv_view(const moin_kv_pages *p, KvPages *v)
+{
+    if (!p || !p->data || misaligned(p->data, 16) || p->n_pages < 1 || moin_kv_page_bytes(p->page_tokens, p->n_kv, p->head_dim) == 0)
+        return MOIN_EINVAL;
+    if ((int64_t)p->n_pages * p->page_tokens > 0x7fffffffLL) return MOIN_EINVAL;
+    v->data = static_cast<char *>(p->data);
+    v->n_pages = p->n_pages;
+    v->n_kv = p->n_kv;
+    v->D = p->head_dim;
+    v->log_blocks = log2_exact(p->page_tokens / KV_BLOCK);
+    return MOIN_OK;
+}
+
+int moin_kv_plan_create(moin_ctx *ctx, moin_kv_plan **out)
+{
+    if (!ctx || !out) return MOIN_EINVAL;
+    *out = nullptr;
+    moin_kv_plan *p = new (std::nothrow) moin_kv_plan();
+    if (!p) return MOIN_ENOMEM;
+    p->buf = nullptr;
+    p->bytes = 0;
+    p->device = ctx->device;
+    p->built = 0;
+    p->pinned = 0;
+    *out = p;
+    return MOIN_OK;
+}
+
+void moin_kv_plan_destroy(moin_kv_plan *plan)
+{
+    if (!plan) return;
+    DeviceGuard guard(plan->device);
+    if (plan->buf) (void)hipFree(plan->buf);
+    for (void *p : plan->retired) (void)hipFree(p);
+    delete plan;
+}
+
+int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens, const int32_t *new_lens, int32_t S, int64_t T,
+                       int32_t max_new, int32_t n_heads, int32_t n_kv, int32_t page_tokens, int32_t n_pages, int32_t *block_table,
+                       int32_t max_pages, const int32_t *free_pages, int32_t free_cap, const int32_t *n_free, int32_t *n_free_out,
+                       int32_t *kv_lens_out, int32_t *seq_offsets, int32_t *slots, void *stream)
+{
+    if (!ctx || !plan || plan->device != ctx->device) return MOIN_EINVAL;
+    plan->built = 0;
+    if (S < 0 || T < 0 || max_new < 0 || free_cap < 0 || n_kv < 1 || n_kv > (1 << 16) || n_heads < n_kv || n_heads % n_kv) return MOIN_EINVAL;
+    if (!page_tokens_ok(page_tokens) || n_pages < 1 || (int64_t)n_pages * page_tokens > 0x7fffffffLL) return MOIN_EINVAL;
+    const int group = n_heads / n_kv;
+    if (group > 0xffff || T * group > 0x7fffffffLL - KV_TILE_ROWS) return MOIN_EINVAL;
+    KvPlanView &v = plan->v;
+    v = KvPlanView{};
+    v.S = S;
+    v.T = T;
+    v.n_kv = n_kv;
+    v.group = group;
+    v.max_pages = max_pages;
+    v.page_tokens = page_tokens;
+    if (S == 0) {
+        if (T != 0) return MOIN_EINVAL;
+        plan->built = 1;
+        return MOIN_OK;
+    }
+    if (max_pages < 1 || (int64_t)S * max_pages > 0x7fffffffLL || (int64_t)max_pages * page_tokens > 0x7fffffffLL) return MOIN_EINVAL;
+    if (!kv_lens || !new_lens || !block_table || (!free_pages && free_cap > 0) || !n_free || !n_free_out || !kv_lens_out || !seq_offsets ||
+        (!slots && T > 0))
+        return MOIN_EINVAL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    v.max_new = (int)std::min<int64_t>(max_new, T);
+    v.has_tile = (int64_t)v.max_new * group > KV_FEW_ROWS;
+    v.has_few = group <= KV_FEW_ROWS && (S > 1 || !v.has_tile);
+    // parts of at least 1 / goal of a list's records each: no more than the goal beside the tiles themselves, and
+    // tiles of several parts have at most twice that many
+    const int few_goal = std::max(1, KV_FEW_TARGET / n_kv), tile_goal = std::max(1, KV_TILE_TARGET / n_kv);
+    const int64_t few = v.has_few ? (int64_t)S + few_goal : 0;
+    const int64_t tiles = v.has_tile ? T * group / KV_TILE_ROWS + S + tile_goal : 0;
+    if ((few + tiles) * n_kv > 0x7fffffffLL) return MOIN_EINVAL;
+    v.max_few = (int)few;
+    v.max_tile = (int)tiles;
+    v.max_pslots = (v.has_few ? 2 * few_goal : 0) + (v.has_tile ? 2 * tile_goal : 0);
+    size_t off = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = off;
+        off = align_up(off + bytes, 256);
+        return at;
+    };
+    const size_t o_head = take(16), o_req = take((size_t)S * 16), o_rt = take((size_t)S * 8), o_few = take((size_t)few * sizeof(KvTile)),
+                 o_tile = take((size_t)tiles * sizeof(KvTile)), o_tick = take((size_t)v.max_pslots * n_kv * 4);
+    const int rc = plan_grow(plan, off, st);
+    if (rc != MOIN_OK) return rc;
+    char *b = static_cast<char *>(plan->buf);
+    v.head = reinterpret_cast<int *>(b + o_head);
+    v.req = reinterpret_cast<int4 *>(b + o_req);
+    v.req_tiles = reinterpret_cast<int2 *>(b + o_rt);
+    v.few = reinterpret_cast<KvTile *>(b + o_few);
+    v.tile = reinterpret_cast<KvTile *>(b + o_tile);
+    v.tickets = reinterpret_cast<int *>(b + o_tick);
+    const KvPlanArgs a{kv_lens, new_lens, block_table, max_pages, free_pages, n_free, free_cap, n_pages, page_tokens,
+                       n_free_out, kv_lens_out, seq_offsets, slots, ctx->err_word};
+    if (timed(ctx, MOIN_K_KV_PLAN, st, [&] { return launch_kv_plan(v, a, st); }) != hipSuccess) return MOIN_EHIP;
+    plan->built = 1;
+    return MOIN_OK;
+}
+
+int moin_kv_release(moin_ctx *ctx, const int32_t *finished, int32_t S, int32_t *kv_lens, int32_t page_tokens, int32_t n_pages,
+                    int32_t *block_table, int32_t max_pages, int32_t *free_pages, int32_t free_cap, int32_t *n_free, void *stream)
+{
+    if (!ctx || S < 0 || free_cap < 0 || !page_tokens_ok(page_tokens) || n_pages < 1) return MOIN_EINVAL;
+    if (S == 0) return MOIN_OK;
+    if (max_pages < 1 || (int64_t)S * max_pages > 0x7fffffffLL) return MOIN_EINVAL;
+    if (!finished || !kv_lens || !block_table || (!free_pages && free_cap > 0) || !n_free) return MOIN_EINVAL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return timed(ctx, MOIN_K_KV_PLAN, st, [&] {
+               return launch_kv_release(finished, S, kv_lens, block_table, max_pages, page_tokens, free_pages, n_free, free_cap, n_pages,
+                                        ctx->err_word, st);
+           }) == hipSuccess
+               ? MOIN_OK
+               : MOIN_EHIP;
+}
+
+static int validate_kv_rows(const moin_kv_pages *pages, KvPages *p, const void *k, const void *v, int64_t T, const int32_t *slots)
+{
+    const int rc = kv_view(pages, p);
+    if (rc != MOIN_OK) return rc;
+    if (T < 0 || T > 0x7fffffffLL || T * p->n_kv > ((int64_t)1 << 31) || T * p->n_kv * p->D > ((int64_t)1 << 39)) return MOIN_EINVAL;
+    if (T > 0 && (!k || !v || !slots || misaligned(k, 16) || misaligned(v, 16))) return MOIN_EINVAL;
+    return MOIN_OK;
+}
+
+int moin_kv_append(moin_ctx *ctx, const moin_kv_pages *pages, const void *k, const void *v, int64_t k_stride, int64_t v_stride, int64_t T,
+                   const int32_t *slots, void *stream)
+{
+    KvPages p;
+    if (!ctx) return MOIN_EINVAL;
+    const int rc = validate_kv_rows(pages, &p, k, v, T, slots);
+    if (rc != MOIN_OK || T == 0) return rc;
+    const int64_t row = (int64_t)p.n_kv * p.D;
+    if (k_stride % 8 || v_stride % 8 || k_stride < row || v_stride < row || k_stride > ((int64_t)1 << 31) || v_stride > ((int64_t)1 << 31)) return MOIN_EINVAL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return timed(ctx, MOIN_K_KV_APPEND, st, [&] { return launch_kv_append(p, k, v, k_stride, v_stride, T, slots, ctx->err_word, st); }) == hipSuccess
+               ? MOIN_OK
+               : MOIN_EHIP;
+}
+
+int moin_kv_gather(moin_ctx *ctx, const moin_kv_pages *pages, const int32_t *slots, int64_t T, void *k, void *v, void *stream)
+{
+    KvPages p;
+    if (!ctx) return MOIN_EINVAL;
+    const int rc = validate_kv_rows(pages, &p, k, v, T, slots);
+    if (rc != MOIN_OK || T == 0) return rc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return timed(ctx, MOIN_K_KV_APPEND, st, [&] { return launch_kv_gather(p, k, v, T, slots, ctx->err_word, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+}
+
+int moin_kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pages *pages, const void *q, int64_t q_stride, int32_t n_heads,
+                      const int32_t *block_table, int32_t max_pages, float scale, int32_t window, void *y, moin_dtype y_dt, float *lse,
+                      void *stream)
+{
+    if (!ctx || !plan || plan->device != ctx->device || !plan->built) return MOIN_EINVAL;
+    AttendArgs a;
+    const int prc = kv_view(pages, &a.pages);
+    if (prc != MOIN_OK) return prc;
+    const KvPlanView &v = plan->v;
+    if (a.pages.n_kv != v.n_kv || n_heads != v.n_kv * v.group || window < 0 || !(scale > 0.f) || scale > 3.0e38f) return MOIN_EINVAL;
+    if (y_dt != MOIN_BF16 && y_dt != MOIN_F32) return MOIN_EINVAL;
+    if (v.S == 0 || v.T == 0) return MOIN_OK;
+    if (max_pages != v.max_pages || pages->page_tokens != v.page_tokens) return MOIN_EINVAL;
+    if (!q || !y || !block_table || misaligned(q, 16) || misaligned(y, 16) || misaligned(lse, 4)) return MOIN_EINVAL;
+    if (q_stride % 8 || q_stride < (int64_t)n_heads * a.pages.D || q_stride > ((int64_t)1 << 31)) return MOIN_EINVAL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int rc = ensure_ws(ctx, (size_t)attend_partial_floats(v, a.pages.D) * 4, st);
+    if (rc != MOIN_OK) return rc;
+    if (capturing(st)) plan->pinned = 1;
+    a.q = q;
+    a.q_stride = q_stride;
+    a.block_table = block_table;
+    a.max_pages = max_pages;
+    a.window = window;
+    a.scale = scale;
+    a.y = y;
+    a.y_f32 = y_dt == MOIN_F32;
+    a.lse = lse;
+    a.partial = static_cast<float *>(ctx->ws);
+    a.err_word = ctx->err_word;
+    return timed(ctx, MOIN_K_KV_ATTEND, st, [&] { return launch_attend(v, a, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
 }
 
 int64_t moin_probe_out_len(moin_ctx *ctx)

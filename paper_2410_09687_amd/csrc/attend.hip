@@ -1,0 +1,561 @@
+// Attention of a step's tokens over the paged MXFP4 cache.  For a token at position p of its request, query head h of the
+// group that shares a kv head, and the keys j <= p (and > p - window):
+//     s_j = scale q . k_j,   y = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   m = max_j s_j,   lse = m + log sum,
+// in one pass over the keys with the running maximum and sum; a row that sees no key gives zeros and lse = -inf.
+//
+// Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T: the codes are the A operand and a row of queries is a
+// COLUMN of the accumulators.  A lane then holds 16 scores of one query row per record of 64 tokens, the softmax's
+// statistics are its own but for two exchanges between the four lanes that share the row, the scores turn into the second product's B operand
+// where they are (the contraction order over the keys is free: the keys of a lane's accumulators are taken as its slots), and the
+// rescaling of O^T is a product with the lane's own factor.  Nothing goes through LDS before the end.
+//   K: lane (m, g) (m = lane % 16, g = lane / 16) takes row m of a tile of 16 keys, channels [D/4 g, D/4 g + D/4);
+//   V: word m of each key (8 channels), for the 4 keys 4 g .. 4 g + 3 of a tile: one 16-byte load, whose eight channels are rows m
+//      of eight accumulators.  (D = 64: words m % 8, the nibbles of half m / 8.)
+// Codes become bf16 exactly, two a conversion, the block's scale in the same instruction; V's pairs of channels are then regrouped into pairs
+// of keys, one v_perm a pair.  Scores, statistics and sums are fp32; the weights exp(s - m) are rounded to bf16 for the second product, for
+// fp32 results as the sum of two bf16.
+//
+// Bound by memory where a request adds one token (68 D bytes a record and kv head against 4 D flops a row and key); by the vector
+// unit's softmax in prompts.
+#include "kv.h"
+#include "mxfp4.h"
+
+namespace moin {
+
+namespace {
+
+constexpr float NEG_INF = -__builtin_huge_valf();
+
+// What a wave holds of a record: codes and scale words.
+template <int D>
+struct Record {
+    static constexpr int KD = D / 32;            // words of K codes per tile and lane (8 channels each)
+    static constexpr int SB = D == 256 ? 2 : 1;  // blocks of 32 channels per lane
+    uint32_t k[4][KD];
+    uint32_t ks[SB];
+    uint4 v[4][SB];
+    uint4 vs[SB];
+};
+
+template <int D>
+__device__ __forceinline__ void load_record(Record<D> &r, const char *rec, int lane)
+{
+    const int m = lane & 15, g = lane >> 4;
+    if constexpr (D == 64) {
+        const char *kp = rec + (g >> 1) * 256 + m * 16 + (g & 1) * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint2 x = *reinterpret_cast<const uint2 *>(kp + i * 512);
+            r.k[i][0] = x.x;
+            r.k[i][1] = x.y;
+        }
+        r.ks[0] = *reinterpret_cast<const uint32_t *>(rec + 64 * D + (g >> 1) * 64 + m * 4);
+        const char *vp = rec + 32 * D + (m & 7) * 64 + g * 16;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[i][0] = *reinterpret_cast<const uint4 *>(vp + i * 512);
+        r.vs[0] = *reinterpret_cast<const uint4 *>(rec + 66 * D + ((m & 7) >> 2) * 64 + g * 16);
+    } else {
+#pragma unroll
+        for (int b = 0; b < Record<D>::SB; ++b) {
+            const char *kp = rec + (b * 4 + g) * 256 + m * 16;
+            const char *vp = rec + 32 * D + (b * 16 + m) * 64 + g * 16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(kp + i * 8 * D);
+                r.k[i][4 * b] = x.x;
+                r.k[i][4 * b + 1] = x.y;
+                r.k[i][4 * b + 2] = x.z;
+                r.k[i][4 * b + 3] = x.w;
+                r.v[i][b] = *reinterpret_cast<const uint4 *>(vp + i * 8 * D);
+            }
+            r.ks[b] = *reinterpret_cast<const uint32_t *>(rec + 64 * D + (b * 4 + g) * 64 + m * 4);
+            r.vs[b] = *reinterpret_cast<const uint4 *>(rec + 66 * D + (b * 4 + (m >> 2)) * 64 + g * 16);
+        }
+    }
+}
+
+// Channel of a query that element e of K operand j holds for lanes of group g; the same for the rows of O^T: channel of
+// accumulator j, row m.
+template <int D>
+__device__ __forceinline__ int k_channel(int j, int g)
+{
+    return D == 64 ? g * 16 + j * 8 : (j >> 2) * 128 + g * 32 + (j & 3) * 8;
+}
+template <int D>
+__device__ __forceinline__ int o_channel(int m)   // of accumulator 0; the others follow (D = 256: 8 further on by 128)
+{
+    return D == 64 ? (m & 7) * 8 + (m >> 3) * 4 : m * 8;
+}
+
+__device__ __forceinline__ uint32_t lows(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
+__device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+__device__ __forceinline__ bf16x8_t operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __builtin_bit_cast(bf16x8_t, make_uint4(a, b, c, d));
+}
+__device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// Maximum and sum over the four lanes of a column.
+__device__ __forceinline__ float max4(float v)
+{
+    auto a = __builtin_amdgcn_permlane32_swap(f32_bits(v), f32_bits(v), false, false);
+    v = fmaxf(bits_f32(a[0]), bits_f32(a[1]));
+    a = __builtin_amdgcn_permlane16_swap(f32_bits(v), f32_bits(v), false, false);
+    return fmaxf(bits_f32(a[0]), bits_f32(a[1]));
+}
+__device__ __forceinline__ float sum4(float v)
+{
+    auto a = __builtin_amdgcn_permlane32_swap(f32_bits(v), f32_bits(v), false, false);
+    v = bits_f32(a[0]) + bits_f32(a[1]);
+    a = __builtin_amdgcn_permlane16_swap(f32_bits(v), f32_bits(v), false, false);
+    return bits_f32(a[0]) + bits_f32(a[1]);
+}
+
+// A wave's columns (16 NT rows of queries) over the records that it walks.
+template <int D, int NT, bool Y32>
+struct Columns {
+    static constexpr int KD = Record<D>::KD, SB = Record<D>::SB, NJ = D / 16;
+    bf16x8_t q[NT][KD];
+    f32x4_t o[NT][NJ];
+    float m[NT], l[NT];    // maximum so far, in units of log2 e / scale; this lane's share of the sum
+
+    // One record.  MASKED: row nt of this lane sees keys [lo[nt], hi[nt]) alone, the request has keys up to `end`; tok: the record's first token.
+    template <bool MASKED>
+    __device__ __forceinline__ void step(Record<D> &r, int n_cols, float c, int tok, const int *lo, const int *hi, int end, int lane)
+    {
+        const int g = lane >> 4;
+        f32x4_t s[NT][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf16x8_t a[KD];
+#pragma unroll
+            for (int j = 0; j < KD; ++j)
+                a[j] = __builtin_bit_cast(bf16x8_t, mx4_decode(r.k[i][j], mx4_scale(r.ks[j / 4], i)));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (nt > 0 && nt >= n_cols) continue;
+                s[nt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < KD; ++j) s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[j], q[nt][j], s[nt][i], 0, 0, 0);
+            }
+        }
+        uint32_t p_hi[NT][4][2], p_lo[NT][4][2];   // [tile][keys 0 1, 2 3]
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt > 0 && nt >= n_cols) continue;
+            if constexpr (MASKED) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = tok + i * 16 + g * 4 + e;
+                        s[nt][i][e] = key >= lo[nt] && key < hi[nt] ? s[nt][i][e] : NEG_INF;
+                    }
+            }
+            float top = m[nt];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, fmaxf(s[nt][i][0], s[nt][i][1])), fmaxf(s[nt][i][2], s[nt][i][3]));
+            top = max4(top);
+            // (nothing seen so far: any finite number will do as the maximum)
+            const float base = top == NEG_INF ? 0.f : top * c;
+            const float shrink = __builtin_amdgcn_exp2f(fmaf(m[nt], c, -base));   // exp2(-inf) = 0 for the first keys
+            m[nt] = top;
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float w[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = __builtin_amdgcn_exp2f(fmaf(s[nt][i][e], c, -base));
+                    sum += w[e];
+                }
+                p_hi[nt][i][0] = pack_bf16x2(w[0], w[1]);
+                p_hi[nt][i][1] = pack_bf16x2(w[2], w[3]);
+                if constexpr (Y32) {
+                    p_lo[nt][i][0] = pack_bf16x2(w[0] - bits_f32(p_hi[nt][i][0] << 16), w[1] - bits_f32(p_hi[nt][i][0] & 0xFFFF0000u));
+                    p_lo[nt][i][1] = pack_bf16x2(w[2] - bits_f32(p_hi[nt][i][1] << 16), w[3] - bits_f32(p_hi[nt][i][1] & 0xFFFF0000u));
+                }
+            }
+            l[nt] = fmaf(l[nt], shrink, sum);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[nt][j] *= shrink;
+        }
+        if constexpr (MASKED) mask_values(r, n_cols, tok, lo, hi, end, lane);
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            bf16x8_t ph[NT], pl[NT];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (nt > 0 && nt >= n_cols) continue;
+                ph[nt] = operand(p_hi[nt][2 * a][0], p_hi[nt][2 * a][1], p_hi[nt][2 * a + 1][0], p_hi[nt][2 * a + 1][1]);
+                if constexpr (Y32)
+                    pl[nt] = operand(p_lo[nt][2 * a][0], p_lo[nt][2 * a][1], p_lo[nt][2 * a + 1][0], p_lo[nt][2 * a + 1][1]);
+            }
+#pragma unroll
+            for (int b = 0; b < SB; ++b) {
+                constexpr int NP = D == 64 ? 2 : 4;   // pairs of channels of a word
+                uint32_t x[8][NP];                    // [key][pair]
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int i = 2 * a + e / 4;
+                    uint32_t codes = word(r.v[i][b], e & 3);
+                    const float scale = mx4_scale(word(r.vs[b], e & 3), i);
+                    if constexpr (D == 64) codes >>= (lane & 8) * 2;
+                    x[e][0] = mx4_pair<0>(codes, scale);
+                    x[e][1] = mx4_pair<1>(codes, scale);
+                    if constexpr (D != 64) {
+                        x[e][2] = mx4_pair<2>(codes, scale);
+                        x[e][3] = mx4_pair<3>(codes, scale);
+                    }
+                }
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const bf16x8_t even = operand(lows(x[0][p], x[1][p]), lows(x[2][p], x[3][p]), lows(x[4][p], x[5][p]), lows(x[6][p], x[7][p]));
+                    const bf16x8_t odd = operand(highs(x[0][p], x[1][p]), highs(x[2][p], x[3][p]), highs(x[4][p], x[5][p]), highs(x[6][p], x[7][p]));
+                    const int j = b * 8 + 2 * p;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (nt > 0 && nt >= n_cols) continue;
+                        o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, ph[nt], o[nt][j], 0, 0, 0);
+                        o[nt][j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, ph[nt], o[nt][j + 1], 0, 0, 0);
+                        if constexpr (Y32) {
+                            o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pl[nt], o[nt][j], 0, 0, 0);
+                            o[nt][j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pl[nt], o[nt][j + 1], 0, 0, 0);
+                        }
+                    }
+                }
+            }
+        }
+    }
+
+    // The values of a record that not every row sees: what lies beyond the request's keys may hold anything and a block may
+    // stand for NaN, and 0 times that is not 0 in the product.  Their scales become 2^-127; a row that does see a block of NaNs gets
+    // its channels' NaN here, from a product of what is seen with what is NaN.
+    __device__ __forceinline__ void mask_values(Record<D> &r, int n_cols, int tok, const int *lo, const int *hi, int end, int lane)
+    {
+        const int g = lane >> 4;
+#pragma unroll
+        for (int b = 0; b < SB; ++b) {
+            uint32_t nan[4], any = 0;   // [key e]: byte i is 255 where the block stands for NaN and the request has the key
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t w = word(r.vs[b], e), bad = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t byte = 255u << (8 * i);
+                    const bool has = tok + i * 16 + g * 4 + e < end;
+                    if (has && (w & byte) == byte) bad |= byte;
+                    if (!has || (w & byte) == byte) w &= ~byte;
+                }
+                nan[e] = bad;
+                any |= bad;
+                if (e == 0) r.vs[b].x = w;
+                else if (e == 1) r.vs[b].y = w;
+                else if (e == 2) r.vs[b].z = w;
+                else r.vs[b].w = w;
+            }
+            if (__ballot(any != 0) == 0) continue;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                if (nt > 0 && nt >= n_cols) continue;
+                f32x4_t count{0.f, 0.f, 0.f, 0.f};   // row m: of the channels whose scales lane (m, .) holds
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+                    uint32_t is[4], sees[4];
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const int i = 2 * a + h / 2, e = (h & 1) * 2, key = tok + i * 16 + g * 4 + e;
+                        is[h] = (nan[e] >> (8 * i) & 1 ? 0x3F80u : 0u) | (nan[e + 1] >> (8 * i) & 1 ? 0x3F800000u : 0u);
+                        sees[h] = (key >= lo[nt] && key < hi[nt] ? 0x3F80u : 0u) | (key + 1 >= lo[nt] && key + 1 < hi[nt] ? 0x3F800000u : 0u);
+                    }
+                    count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand(is[0], is[1], is[2], is[3]),
+                                                                    operand(sees[0], sees[1], sees[2], sees[3]), count, 0, 0, 0);
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (count[e] > 0.f)
+#pragma unroll
+                        for (int j = b * 8; j < (SB == 1 ? NJ : b * 8 + 8); ++j) o[nt][j][e] = bits_f32(0x7FC00000u);
+            }
+        }
+    }
+};
+
+struct AttendK {
+    KvPlanView v;
+    AttendArgs a;
+    int list;              // 0: the tiles of few rows, 1: the others
+    int bound;             // records of the launch's list at most
+};
+
+// Output row of the request's tokens: group rows of a token are query heads of the kv head.
+__device__ __forceinline__ int64_t y_row(const KvTile &t, int row, int group, int n_kv, int h)
+{
+    const int i = row / group;
+    return ((int64_t)t.tok0 + i) * (n_kv * group) + h * group + (row - i * group);
+}
+
+__device__ __forceinline__ void put_agent(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float get_agent(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+template <int N>
+__device__ __forceinline__ void store_y(const AttendArgs &a, int64_t row, int D, int ch, const float (&x)[N])
+{
+    if (a.y_f32) {
+        float *y = static_cast<float *>(a.y) + row * D + ch;
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<float4 *>(y + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    } else {
+        char *y = static_cast<char *>(a.y) + (row * D + ch) * 2;
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            *reinterpret_cast<uint2 *>(y + i * 2) = make_uint2(pack_bf16x2(x[i], x[i + 1]), pack_bf16x2(x[i + 2], x[i + 3]));
+    }
+}
+
+constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
+
+// SPLIT: the four waves share the tile's 16 NT rows and take its records in turn.  Otherwise each has 16 NT rows of its own.
+template <int D, int NT, bool Y32, bool SPLIT>
+__global__ __launch_bounds__(256) void attend_kernel(AttendK p)
+{
+    constexpr int ROWS = SPLIT ? 16 * NT : 64 * NT, CH = D / 16;   // CH: channels of a row per thread in the joins
+    constexpr int LDO = D + 4;
+    __shared__ float lds_o[SPLIT ? 4 : 1][16][LDO];
+    __shared__ float lds_ml[4][16][2];
+    __shared__ int lds_last;
+    const KvPlanView &v = p.v;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int rec_id = blockIdx.x / v.n_kv, h = blockIdx.x - rec_id * v.n_kv;
+    if (rec_id >= v.head[p.list]) return;
+    const KvTile t = (p.list ? v.tile : v.few)[rec_id];
+    const int group = v.group, rows = t.n_tok * group, pos0 = t.kv_len - t.n_tok;
+    const int row_end = min(rows, t.row0 + ROWS);
+    // positions of the tile's first and last token
+    const int first = pos0 + t.row0 / group, last = pos0 + (row_end - 1) / group;
+    const int window = min(p.a.window > 0 ? p.a.window : 0x7fffffff, t.kv_len + 1);   // (no further: no position minus it overflows)
+    const int lo_all = max(0, first - window + 1), hi_all = max(0, last + 1);
+    const int b_lo = lo_all >> 6, n_blocks = hi_all > lo_all ? ((hi_all + 63) >> 6) - b_lo : 0;
+    const int b0 = b_lo + (int)((int64_t)n_blocks * t.part / t.n_parts), b1 = b_lo + (int)((int64_t)n_blocks * (t.part + 1) / t.n_parts);
+
+    Columns<D, NT, Y32> w;
+    const int wrow0 = SPLIT ? t.row0 : t.row0 + wave * 16 * NT;
+    const int n_cols = max(0, min(NT, (row_end - wrow0 + 15) >> 4));
+    int lo[NT], hi[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int row = wrow0 + nt * 16 + n;
+        const bool real = row < row_end;
+        const int i = real ? row / group : 0, pos = pos0 + i;
+        lo[nt] = real ? max(0, pos - window + 1) : 0;
+        hi[nt] = real ? max(0, pos + 1) : 0;
+        w.m[nt] = NEG_INF;
+        w.l[nt] = 0.f;
+#pragma unroll
+        for (int j = 0; j < Columns<D, NT, Y32>::NJ; ++j) w.o[nt][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        const char *q = static_cast<const char *>(p.a.q) +
+                        ((t.tok0 + i) * p.a.q_stride + (int64_t)(h * group + (real ? row - i * group : 0)) * D) * 2;
+#pragma unroll
+        for (int j = 0; j < Columns<D, NT, Y32>::KD; ++j) {
+            const uint4 x = *reinterpret_cast<const uint4 *>(q + k_channel<D>(j, g) * 2);
+            w.q[nt][j] = __builtin_bit_cast(bf16x8_t, real ? x : make_uint4(0, 0, 0, 0));
+        }
+    }
+    const float c = p.a.scale * LOG2E;
+    const int *table = p.a.block_table + (int64_t)t.req * p.a.max_pages;
+    const int lb = p.a.pages.log_blocks;
+    const int64_t page_bytes = p.a.pages.page_bytes();
+    const char *heads = p.a.pages.data + (((int64_t)h * kv_record_bytes(D)) << lb);
+    constexpr int STEP = SPLIT ? 4 : 1;
+    auto page_of = [&](int b) { return uniform(table[min(b, b1 - 1) >> lb]); };
+    auto record_of = [&](int b, int page) {
+        return heads + (int64_t)page * page_bytes + (b & ((1 << lb) - 1)) * kv_record_bytes(D);
+    };
+    const int first_b = b0 + (SPLIT ? wave : 0);
+    if (first_b < b1 && n_cols > 0) {
+        Record<D> cur, nxt;
+        int page = page_of(first_b), page_next = page_of(first_b + STEP);
+        bool ok = page >= 0 && page < p.a.pages.n_pages;
+        load_record<D>(cur, record_of(first_b, ok ? page : 0), lane);
+        bool bad = !ok;
+        for (int b = first_b; b < b1; b += STEP) {
+            const bool ok_next = page_next >= 0 && page_next < p.a.pages.n_pages;
+            load_record<D>(nxt, record_of(min(b + STEP, b1 - 1), ok_next ? page_next : 0), lane);
+            page_next = page_of(b + 2 * STEP);
+            const int tok = b * 64;
+            if (ok) {
+                if (tok >= last - window + 1 && tok + 63 <= first) w.template step<false>(cur, n_cols, c, tok, lo, hi, t.kv_len, lane);
+                else w.template step<true>(cur, n_cols, c, tok, lo, hi, t.kv_len, lane);
+            }
+            cur = nxt;
+            ok = ok_next;
+            bad |= b + STEP < b1 && !ok;
+        }
+        if (bad && lane == 0) atomicOr(p.a.err_word, ERR_BAD_PAGE);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) w.l[nt] = sum4(w.l[nt]);
+
+    const int ps = t.pslot + t.part;
+    float *part_o = p.a.partial + ((int64_t)ps * v.n_kv + h) * KV_TILE_ROWS * (D + 2);
+    const bool whole = t.n_parts == 1;
+    if constexpr (SPLIT) {
+        const int row = tid >> 4, ch = (tid & 15) * CH;
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt * 16 >= row_end - t.row0) break;
+            if (nt) __syncthreads();
+#pragma unroll
+            for (int k = 0; k < NT; ++k)
+                if (k == nt) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int j = 0; j < D / 16; ++j)
+                            lds_o[wave][n][o_channel<D>(g * 4 + e) + (D == 256 ? (j >> 3) * 128 + (j & 7) : j)] = w.o[k][j][e];
+                    if (g == 0) {
+                        lds_ml[wave][n][0] = w.m[k];
+                        lds_ml[wave][n][1] = w.l[k];
+                    }
+                }
+            __syncthreads();
+            float m = NEG_INF, l = 0.f, x[CH];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) m = fmaxf(m, lds_ml[u][row][0]);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[i] = 0.f;
+            const float base = m == NEG_INF ? 0.f : m * c;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float f = __builtin_amdgcn_exp2f(fmaf(lds_ml[u][row][0], c, -base));
+                l = fmaf(lds_ml[u][row][1], f, l);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) x[i] = fmaf(lds_o[u][row][ch + i], f, x[i]);
+            }
+            const int r = t.row0 + nt * 16 + row;
+            if (r >= row_end) continue;
+            if (whole) {
+                const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) x[i] *= inv;
+                const int64_t at = y_row(t, r, group, v.n_kv, h);
+                store_y(p.a, at, D, ch, x);
+                if (p.a.lse && ch == 0) p.a.lse[at] = l > 0.f || l != l ? (m * c + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
+            } else {
+                float *o = part_o + (nt * 16 + row) * (D + 2);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) put_agent(o + 2 + ch + i, x[i]);
+                if (ch == 0) {
+                    put_agent(o, m);
+                    put_agent(o + 1, l);
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int local = wave * 16 * NT + nt * 16 + n, r = t.row0 + local;
+            if (r >= row_end) continue;
+            const float l = w.l[nt], inv = whole ? (l > 0.f || l != l ? 1.f / l : 0.f) : 1.f;
+            const int64_t at = y_row(t, r, group, v.n_kv, h);
+            float *o = part_o + local * (D + 2);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                for (int b = 0; b < (D == 256 ? 2 : 1); ++b) {
+                    constexpr int N = D == 64 ? 4 : 8;
+                    float x[N];
+#pragma unroll
+                    for (int j = 0; j < N; ++j) x[j] = w.o[nt][b * 8 + j][e] * inv;
+                    const int ch = o_channel<D>(g * 4 + e) + b * 128;
+                    if (whole) store_y(p.a, at, D, ch, x);
+                    else
+#pragma unroll
+                        for (int j = 0; j < N; ++j) put_agent(o + 2 + ch + j, x[j]);
+                }
+            }
+            if (g == 0) {
+                if (!whole) {
+                    put_agent(o, w.m[nt]);
+                    put_agent(o + 1, l);
+                } else if (p.a.lse) {
+                    p.a.lse[at] = l > 0.f || l != l ? (w.m[nt] * c + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
+                }
+            }
+        }
+    }
+    if (whole) return;
+    // The tile's workgroup that reports last joins the parts, in their order.  What the parts leave are device-scope stores: a
+    // workgroup waits for its own before it reports, and nobody's L2 has to be written back.
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int *ticket = v.tickets + (int64_t)t.pslot * v.n_kv + h;
+    if (tid == 0) {
+        lds_last = atomicAdd(ticket, 1) == t.n_parts - 1;
+        if (lds_last) *ticket = 0;   // clean for the next call
+    }
+    __syncthreads();
+    if (!lds_last) return;
+    const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
+    const float *first_part = p.a.partial + ((int64_t)t.pslot * v.n_kv + h) * KV_TILE_ROWS * (D + 2);
+    for (int r0 = 0; r0 < row_end - t.row0; r0 += 16) {
+        const int local = r0 + (tid >> 4), ch = (tid & 15) * CH;
+        if (t.row0 + local >= row_end) continue;
+        const float *o = first_part + local * (D + 2);
+        float m = NEG_INF, l = 0.f, x[CH];
+        for (int u = 0; u < t.n_parts; ++u) m = fmaxf(m, get_agent(o + u * part_step));
+#pragma unroll
+        for (int i = 0; i < CH; ++i) x[i] = 0.f;
+        const float base = m == NEG_INF ? 0.f : m * c;
+        for (int u = 0; u < t.n_parts; ++u) {
+            const float f = __builtin_amdgcn_exp2f(fmaf(get_agent(o + u * part_step), c, -base));
+            l = fmaf(get_agent(o + u * part_step + 1), f, l);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[i] = fmaf(get_agent(o + u * part_step + 2 + ch + i), f, x[i]);
+        }
+        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll
+        for (int i = 0; i < CH; ++i) x[i] *= inv;
+        const int64_t at = y_row(t, t.row0 + local, group, v.n_kv, h);
+        store_y(p.a, at, D, ch, x);
+        if (p.a.lse && ch == 0) p.a.lse[at] = l > 0.f || l != l ? (m * c + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
+    }
+}
+
+template <int D, bool Y32>
+hipError_t launch_d(const KvPlanView &v, const AttendArgs &a, hipStream_t stream)
+{
+    AttendK p{v, a, 0, 0};
+    if (v.has_few) {
+        p.bound = v.max_few;
+        const dim3 grid((unsigned)v.max_few * v.n_kv);
+        if (std::min(v.max_new * (int64_t)v.group, (int64_t)KV_FEW_ROWS) <= 16)
+            hipLaunchKernelGGL((attend_kernel<D, 1, Y32, true>), grid, dim3(256), 0, stream, p);
+        else
+            hipLaunchKernelGGL((attend_kernel<D, 2, Y32, true>), grid, dim3(256), 0, stream, p);
+    }
+    if (v.has_tile) {
+        p.list = 1;
+        p.bound = v.max_tile;
+        hipLaunchKernelGGL((attend_kernel<D, 2, Y32, false>), dim3((unsigned)v.max_tile * v.n_kv), dim3(256), 0, stream, p);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t attend_partial_floats(const KvPlanView &v, int D)
+{
+    return (int64_t)v.max_pslots * v.n_kv * KV_TILE_ROWS * (D + 2);
+}
+
+hipError_t launch_attend(const KvPlanView &v, const AttendArgs &a, hipStream_t stream)
+{
+    switch (a.pages.D) {
+    case 64: return a.y_f32 ? launch_d<64, true>(v, a, stream) : launch_d<64, false>(v, a, stream);
+    case 128: return a.y_f32 ? launch_d<128, true>(v, a, stream) : launch_d<128, false>(v, a, stream);
+    case 256: return a.y_f32 ? launch_d<256, true>(v, a, stream) : launch_d<256, false>(v, a, stream);
+    default: return hipErrorInvalidValue;
+    }
+}
+
+}  // namespace moin

@@ -560,6 +560,201 @@ PyObject *merge_adapters(PyObject *const *a)
     Py_RETURN_NONE;
 }
 
+// ---- serving in four bits ----------------------------------------------------------
+
+struct Strided {
+    void *p;
+    int64_t stride;
+};
+// [T, heads, D] bf16 whose heads lie side by side; the rows of tokens may be strided.
+Strided token_rows(const at::Tensor &t, const char *name)
+{
+    if (!t.is_cuda()) {
+        PyErr_Format(PyExc_ValueError, "%s must live on the GPU", name);
+        throw Raised{};
+    }
+    if (t.scalar_type() != at::kBFloat16) {
+        PyErr_Format(PyExc_TypeError, "%s: bfloat16 expected", name);
+        throw Raised{};
+    }
+    if ((t.size(2) > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != t.size(2))) {
+        PyErr_Format(PyExc_ValueError, "%s: the heads of a token must be contiguous", name);
+        throw Raised{};
+    }
+    return Strided{t.size(0) ? t.data_ptr() : nullptr, t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2)};
+}
+moin_kv_pages kv_pages(PyObject *data, PyObject *n_pages, PyObject *page_tokens, PyObject *n_kv, PyObject *head_dim)
+{
+    return moin_kv_pages{dev_ptr(tensor(data, "pages"), "pages", at::kByte), integer32(n_pages), integer32(page_tokens), integer32(n_kv),
+                         integer32(head_dim)};
+}
+int32_t *int_ptr(const at::Tensor &t, const char *name) { return static_cast<int32_t *>(dev_ptr(t, name, at::kInt)); }
+
+// kv_plan_build(ctx, plan, kv_lens, new_lens, T, max_new, n_heads, n_kv, page_tokens, n_pages, block_table, free_pages, n_free, out, stream)
+//   -> (seq_offsets, kv_lens, slots, n_free)
+PyObject *kv_plan_build(PyObject *const *a)
+{
+    const at::Tensor &kv = tensor(a[2], "kv_lens"), &nw = tensor(a[3], "new_lens"), &table = tensor(a[10], "block_table"),
+                     &free_ = tensor(a[11], "free_pages"), &nf = tensor(a[12], "n_free");
+    const int64_t S = kv.numel(), T = integer(a[4]);
+    if (nw.numel() != S || table.dim() != 2 || table.size(0) != S) fail(PyExc_ValueError, "kv_lens [S], new_lens [S] and block_table [S,max_pages] expected");
+    if (nf.numel() != 1) fail(PyExc_ValueError, "n_free [1] expected");
+    if (T < 0) fail(PyExc_ValueError, "T must not be negative");
+    Out r[4];
+    const int64_t sizes[4] = {S + 1, S, T, 1};
+    if (a[13] == Py_None) {
+        for (int i = 0; i < 4; ++i) r[i].t = empty({sizes[i]}, at::kInt, kv);
+    } else {
+        PyObject *seq = PySequence_Fast(a[13], "out: (seq_offsets, kv_lens, slots, n_free) expected");
+        if (!seq) throw Raised{};
+        const bool four = PySequence_Fast_GET_SIZE(seq) == 4;
+        if (four)
+            for (int i = 0; i < 4; ++i) r[i].is(PySequence_Fast_GET_ITEM(seq, i));
+        Py_DECREF(seq);
+        if (!four) fail(PyExc_ValueError, "out: (seq_offsets, kv_lens, slots, n_free) expected");
+        for (int i = 0; i < 4; ++i) {
+            r[i].t = tensor(r[i].own, "out");
+            if (r[i].t.scalar_type() != at::kInt || r[i].t.numel() != sizes[i]) fail(PyExc_ValueError, "out: int32 tensors of S+1, S, T and 1 elements expected");
+        }
+    }
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    moin_kv_plan *plan = static_cast<moin_kv_plan *>(handle(a[1]));
+    const int32_t *pk = S ? int_ptr(kv, "kv_lens") : nullptr, *pn = S ? int_ptr(nw, "new_lens") : nullptr;
+    int32_t *pt = S ? int_ptr(table, "block_table") : nullptr;
+    const int32_t *pf = free_.numel() ? int_ptr(free_, "free_pages") : nullptr, *pc = int_ptr(nf, "n_free");
+    int32_t *po = int_ptr(r[0].t, "out"), *pl = S ? int_ptr(r[1].t, "out") : nullptr, *ps = T ? int_ptr(r[2].t, "out") : nullptr,
+            *pr = int_ptr(r[3].t, "out");
+    const int32_t max_new = integer32(a[5]), heads = integer32(a[6]), n_kv = integer32(a[7]), page = integer32(a[8]), pages = integer32(a[9]);
+    const int32_t S32 = size32(S), mp = size32(table.size(1)), cap = size32(free_.numel());
+    void *st = handle(a[14]);
+    call("moin_kv_plan_build", [&] {
+        return moin_kv_plan_build(ctx, plan, pk, pn, S32, T, max_new, heads, n_kv, page, pages, pt, mp, pf, cap, pc, pr, pl, po, ps, st);
+    });
+    return tuple(r, 4);
+}
+
+// kv_append(ctx, data, n_pages, page_tokens, n_kv, head_dim, k, v, slots, stream)
+PyObject *kv_append(PyObject *const *a)
+{
+    const at::Tensor &k = tensor(a[6], "k"), &v = tensor(a[7], "v"), &slots = tensor(a[8], "slots");
+    const moin_kv_pages p = kv_pages(a[1], a[2], a[3], a[4], a[5]);
+    const int64_t T = slots.numel();
+    for (const at::Tensor *t : {&k, &v})
+        if (t->dim() != 3 || t->size(0) != T || t->size(1) != p.n_kv || t->size(2) != p.head_dim)
+            fail(PyExc_ValueError, "k, v [T,n_kv,head_dim] and slots [T] expected");
+    const Strided sk = token_rows(k, "k"), sv = token_rows(v, "v");
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    const int32_t *ps = T ? int_ptr(slots, "slots") : nullptr;
+    void *st = handle(a[9]);
+    call("moin_kv_append", [&] { return moin_kv_append(ctx, &p, sk.p, sv.p, sk.stride, sv.stride, T, ps, st); });
+    Py_RETURN_NONE;
+}
+
+// kv_gather(ctx, data, n_pages, page_tokens, n_kv, head_dim, slots, stream) -> (k, v)
+PyObject *kv_gather(PyObject *const *a)
+{
+    const at::Tensor &slots = tensor(a[6], "slots");
+    const moin_kv_pages p = kv_pages(a[1], a[2], a[3], a[4], a[5]);
+    const int64_t T = slots.numel();
+    Out r[2];
+    for (Out &o : r) o.t = empty({T, p.n_kv, p.head_dim}, at::kBFloat16, slots);
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    const int32_t *ps = T ? int_ptr(slots, "slots") : nullptr;
+    void *pk = T ? dev_ptr(r[0].t, "k") : nullptr, *pv = T ? dev_ptr(r[1].t, "v") : nullptr, *st = handle(a[7]);
+    call("moin_kv_gather", [&] { return moin_kv_gather(ctx, &p, ps, T, pk, pv, st); });
+    return tuple(r, 2);
+}
+
+// kv_attention(ctx, plan, plan.T, plan.S, data, n_pages, page_tokens, n_kv, head_dim, q, block_table, scale, window, y_dtype, out, want_lse, stream)
+//   -> (y, lse or None)
+PyObject *kv_attention(PyObject *const *a)
+{
+    const at::Tensor &q = tensor(a[9], "q"), &table = tensor(a[10], "block_table");
+    const moin_kv_pages p = kv_pages(a[4], a[5], a[6], a[7], a[8]);
+    const int64_t T = integer(a[2]);
+    if (q.dim() != 3 || q.size(0) != T || q.size(2) != p.head_dim) fail(PyExc_ValueError, "q [T,n_heads,head_dim] (T as planned) expected");
+    if (table.dim() != 2 || table.size(0) != integer(a[3])) fail(PyExc_ValueError, "block_table [S,max_pages] (S as planned) expected");
+    const Strided sq = token_rows(q, "q");
+    const at::ScalarType yt = y_type(a[13]);
+    Out r[2];
+    if (a[14] == Py_None) r[0].t = empty({T, q.size(1), q.size(2)}, yt, q);
+    else {
+        r[0].is(a[14]);
+        r[0].t = tensor(a[14], "out");
+        if (r[0].t.sizes() != q.sizes() || r[0].t.scalar_type() != yt) fail(PyExc_ValueError, "out has the wrong shape or dtype");
+    }
+    if (a[15] == Py_True) r[1].t = empty({T, q.size(1)}, at::kFloat, q);
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    const moin_kv_plan *plan = static_cast<moin_kv_plan *>(handle(a[1]));
+    const int32_t heads = size32(q.size(1)), mp = size32(table.size(1)), window = integer32(a[12]);
+    const float scale = real(a[11]);
+    const int32_t *pt = table.numel() ? int_ptr(table, "block_table") : nullptr;
+    void *py = T ? dev_ptr(r[0].t, "out") : nullptr, *st = handle(a[16]);
+    float *pl = T && r[1].defined() ? static_cast<float *>(dev_ptr(r[1].t, "lse")) : nullptr;
+    call("moin_kv_attention", [&] {
+        return moin_kv_attention(ctx, plan, &p, sq.p, sq.stride, heads, pt, mp, scale, window, py, y_enum(yt), pl, st);
+    });
+    return tuple(r, 2);
+}
+
+struct Packed {
+    const void *p;
+    int32_t d_out, d_in;
+};
+Packed packed(PyObject *data, PyObject *d_out, PyObject *d_in)
+{
+    const at::Tensor &t = tensor(data, "W4");
+    const Packed w{dev_ptr(t, "W4", at::kByte), integer32(d_out), integer32(d_in)};
+    if (t.numel() == 0 || t.numel() != moin_mx4_bytes(w.d_out, w.d_in)) fail(PyExc_ValueError, "W4 does not have the bytes of a [d_out,d_in] weight");
+    return w;
+}
+
+// mx4_linear(ctx, x, W4, d_out, d_in, y_dtype, out, stream)
+PyObject *mx4_linear(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[1], "x");
+    const Packed w = packed(a[2], a[3], a[4]);
+    if (x.dim() != 2 || x.size(1) != w.d_in) fail(PyExc_ValueError, "x [T,d_in] expected");
+    const at::ScalarType yt = y_type(a[5]);
+    const int64_t T = x.size(0);
+    Out y = y_out(x, w.d_out, yt, a[6]);
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    const void *px = T ? dev_ptr(x, "x", at::kBFloat16) : nullptr;
+    void *py = T ? dev_ptr(y.t, "y") : nullptr, *st = handle(a[7]);
+    call("moin_mx4_linear", [&] { return moin_mx4_linear(ctx, px, T, w.p, w.d_in, w.d_out, py, y_enum(yt), st); });
+    return y.object();
+}
+
+// lora_linear_mx4_planned(ctx, plan, plan.T, plan.E, x, W4, d_out, d_in, A, B, scale, y_dtype, out, stream)
+PyObject *lora_linear_mx4_planned(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[4], "x");
+    const Packed w = packed(a[5], a[6], a[7]);
+    if (x.dim() != 2 || x.size(1) != w.d_in || x.size(0) != integer(a[2])) fail(PyExc_ValueError, "x [T,d_in] (T as planned) expected");
+    int32_t E = 0, r = 0;
+    if (a[8] != Py_None && a[9] != Py_None) {
+        const at::Tensor &A = tensor(a[8], "A_stack"), &B = tensor(a[9], "B_stack");
+        if (A.dim() != 3 || B.dim() != 3 || A.size(2) != w.d_in || B.size(0) != A.size(0) || B.size(1) != w.d_out || B.size(2) != A.size(1))
+            fail(PyExc_ValueError, "A_stack [E,r,d_in] / B_stack [E,d_out,r] shape mismatch");
+        E = size32(A.size(0));
+        r = size32(A.size(1));
+    }
+    if (E && E != integer(a[3])) fail(PyExc_ValueError, "stack holds a different number of experts than the plan was built for");
+    const at::ScalarType yt = y_type(a[11]);
+    const int64_t T = x.size(0);
+    Out y = y_out(x, w.d_out, yt, a[12]);
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    const moin_plan *plan = static_cast<moin_plan *>(handle(a[1]));
+    const void *px = T ? dev_ptr(x, "x", at::kBFloat16) : nullptr;
+    const void *pA = dev_ptr_or_null(a[8], "A_stack", at::kBFloat16), *pB = dev_ptr_or_null(a[9], "B_stack", at::kBFloat16);
+    const float scale = real(a[10]);
+    void *py = T ? dev_ptr(y.t, "y") : nullptr, *st = handle(a[13]);
+    call("moin_lora_linear_mx4_planned", [&] {
+        return moin_lora_linear_mx4_planned(ctx, plan, px, w.p, pA, pB, w.d_in, w.d_out, r, scale, py, y_enum(yt), st);
+    });
+    return y.object();
+}
+
 // set_error(type): what a status other than success is raised as
 PyObject *set_error(PyObject *const *a)
 {
@@ -590,6 +785,8 @@ PyMethodDef methods[] = {
     MOIN_ENTRY(route, 10), MOIN_ENTRY(route_topk, 7), MOIN_ENTRY(route_plan, 14), MOIN_ENTRY(plan_build, 8),
     MOIN_ENTRY(lora_linear, 12), MOIN_ENTRY(lora_linear_planned, 12), MOIN_ENTRY(lora_linear_mx_planned, 16),
     MOIN_ENTRY(lora_linear_planned_shared, 12), MOIN_ENTRY(merge_adapters, 8), MOIN_ENTRY(set_error, 1),
+    MOIN_ENTRY(kv_plan_build, 15), MOIN_ENTRY(kv_append, 10), MOIN_ENTRY(kv_gather, 8), MOIN_ENTRY(kv_attention, 17),
+    MOIN_ENTRY(mx4_linear, 8), MOIN_ENTRY(lora_linear_mx4_planned, 14),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_moin_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

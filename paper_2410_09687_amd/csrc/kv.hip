@@ -1,0 +1,351 @@
+// The paged MXFP4 cache's bookkeeping and its writes: block tables and slot maps from the requests' lengths, pages given
+// back, tokens appended, tokens read back.
+#include "kv.h"
+#include "mxfp4.h"
+
+namespace moin {
+
+constexpr int KV_PLAN_THREADS = 1024, KV_PLAN_WAVES = KV_PLAN_THREADS / 64;
+constexpr int KV_SLOT_CHUNK = 2048;   // tokens of a request per workgroup of the second launch
+
+// Inclusive scans over the workgroup, two quantities at once; `total` gets the workgroup's sums.
+struct Scan2 {
+    long long a;
+    int b;
+};
+__device__ __forceinline__ Scan2 block_scan(Scan2 v, Scan2 *lds, Scan2 &total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const long long a = __shfl_up(v.a, d);
+        const int b = __shfl_up(v.b, d);
+        if (lane >= d) {
+            v.a += a;
+            v.b += b;
+        }
+    }
+    lds_barrier();   // (what an earlier scan left has been read)
+    if (lane == 63) lds[wave] = v;
+    lds_barrier();
+    Scan2 before{0, 0};
+    total = Scan2{0, 0};
+#pragma unroll
+    for (int w = 0; w < KV_PLAN_WAVES; ++w) {
+        const Scan2 x = lds[w];
+        if (w < wave) {
+            before.a += x.a;
+            before.b += x.b;
+        }
+        total.a += x.a;
+        total.b += x.b;
+    }
+    v.a += before.a;
+    v.b += before.b;
+    return v;
+}
+
+__device__ __forceinline__ int ceil_shift(int v, int s) { return (v >> s) + ((v & ((1 << s) - 1)) != 0); }
+
+// Slot of a request's token at position `pos`; `dealt` >= 0: the first of its new pages among those the step deals.
+__device__ __forceinline__ int kv_slot(const KvPlanArgs &a, int s, int pos, int log_page, int have, int dealt, int n_free)
+{
+    const int pi = pos >> log_page;
+    const int page = pi >= have ? a.free_pages[n_free - 1 - (dealt + pi - have)] : a.block_table[(int64_t)s * a.max_pages + pi];
+    if (page < 0 || page >= a.n_pages) {
+        atomicOr(a.err_word, ERR_BAD_PAGE);
+        return -1;
+    }
+    return (page << log_page) + (pos & ((1 << log_page) - 1));
+}
+
+__device__ __forceinline__ void kv_write_tile(KvTile *dst, int tok0, int n_tok, int L, int s, int row0, int part, int n_parts, int pslot)
+{
+    int4 *d = reinterpret_cast<int4 *>(dst);
+    d[0] = make_int4(tok0, n_tok, L, s);
+    d[1] = make_int4(row0, part, n_parts, pslot);
+}
+
+// One workgroup walks the requests, 1024 at a time, twice.  First: offsets (a sum over the new tokens), pages to deal (a sum over
+// the pages that each request lacks), which requests are served.  Then, with the keys of all requests known, the
+// size of the parts that fill the chip and everybody's place in the lists.  Up to KV_FEW_TOKENS new tokens a
+// request (decode), it writes slots and table entries itself; else a second launch does, a workgroup for 2048 tokens of a request.
+// Bound by latency: a chain of a dozen trips to memory and barriers.
+__global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, KvPlanArgs a, int log_page, int few_tokens)
+{
+    __shared__ Scan2 lds[KV_PLAN_WAVES];
+    __shared__ int lds_err;
+    const int tid = threadIdx.x;
+    if (tid == 0) lds_err = 0;
+    for (int i = tid; i < v.max_pslots * v.n_kv; i += KV_PLAN_THREADS) v.tickets[i] = 0;
+    int n_free = *a.n_free;
+    int err = 0;
+    if (n_free < 0 || n_free > a.free_cap) {
+        err |= ERR_NO_PAGES;
+        n_free = max(0, min(n_free, a.free_cap));
+    }
+    const long long row_max = (long long)a.max_pages << log_page;
+    long long tok_base = 0;
+    int page_base = 0, taken = 0;
+    long long few_blocks = 0, tile_blocks = 0;   // records that the tiles of either kind walk, one kv head
+    for (int s0 = 0; s0 < v.S; s0 += KV_PLAN_THREADS) {
+        const int s = s0 + tid;
+        const bool in = s < v.S;
+        const int kv = in ? a.kv_lens[s] : 0, n0 = in ? a.new_lens[s] : 0;
+        const bool sane = kv >= 0 && n0 >= 0 && n0 <= v.max_new && (long long)max(kv, 0) + n0 <= row_max;
+        const int have = ceil_shift(max(kv, 0), log_page);
+        const int need = sane ? ceil_shift(kv + n0, log_page) - have : 0;
+        Scan2 total;
+        const Scan2 up = block_scan(Scan2{max(n0, 0), need}, lds, total);
+        const long long end = tok_base + up.a, begin = end - max(n0, 0);
+        const int dealt = page_base + up.b - need;
+        const bool whole = end <= v.T;
+        const bool served = sane && whole && (need == 0 || dealt + need <= n_free);
+        if (in) {
+            if (!sane || !whole) err |= ERR_BAD_LENGTHS;
+            else if (!served) err |= ERR_NO_PAGES;
+            const int tok0 = (int)min(begin, (long long)v.T), n = (int)(min(end, (long long)v.T) - tok0);
+            a.seq_offsets[s] = tok0;
+            if (s == v.S - 1) {
+                a.seq_offsets[v.S] = tok0 + n;
+                if (end != v.T) err |= ERR_BAD_LENGTHS;
+                for (int64_t t = end; t < v.T; ++t) a.slots[t] = -1;   // tokens of no request
+            }
+            a.kv_lens_out[s] = served ? kv + n0 : max(kv, 0);
+            v.req[s] = make_int4(max(kv, 0), served ? dealt : -1, need, n);
+            // (a request that is not served has no keys: its rows come out as zeros)
+            const int64_t rows = (int64_t)n * v.group;
+            const int blocks = served ? ceil_shift(kv + n0, 6) : 0;
+            if (rows > KV_FEW_ROWS) tile_blocks += (rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS * blocks;
+            else if (rows > 0) few_blocks += blocks;
+            if (served && need > 0) taken = dealt + need;
+            if (few_tokens || n > v.max_new) {   // (more than the second launch covers: not served)
+                for (int i = 0; i < n; ++i)
+                    a.slots[tok0 + i] = served ? kv_slot(a, s, kv + i, log_page, have, dealt, n_free) : -1;
+            }
+            if (few_tokens && served) {
+                for (int j = 0; j < need; ++j)
+                    a.block_table[(int64_t)s * a.max_pages + have + j] = a.free_pages[n_free - 1 - (dealt + j)];
+            }
+        }
+        tok_base += total.a;
+        page_base += total.b;
+    }
+    // sums over the workgroup (served requests are a prefix of those that want pages: the last one's end is what is taken)
+    Scan2 sums, t2;
+    block_scan(Scan2{few_blocks, 0}, lds, sums);
+    const long long few_all = sums.a;
+    block_scan(Scan2{tile_blocks, 0}, lds, sums);
+    const long long tile_all = sums.a;
+    lds_barrier();
+    __shared__ int lds_taken;
+    if (tid == 0) lds_taken = 0;
+    lds_barrier();
+    if (taken) atomicMax(&lds_taken, taken);
+    if (err) atomicOr(&lds_err, err);
+    lds_barrier();
+    if (tid == 0) {
+        *a.n_free_out = n_free - lds_taken;
+        v.head[2] = n_free;
+        if (lds_err) atomicOr(a.err_word, lds_err);
+    }
+    // parts: so large that the launch has about its target of workgroups, over all kv heads
+    const int few_goal = max(1, KV_FEW_TARGET / v.n_kv), tile_goal = max(1, KV_TILE_TARGET / v.n_kv);
+    const int few_chunk = (int)max((long long)KV_FEW_MIN, (few_all + few_goal - 1) / few_goal);
+    const int tile_chunk = (int)max((long long)KV_TILE_MIN, (tile_all + tile_goal - 1) / tile_goal);
+    int few_base = 0, tile_base = 0, ps_base = 0;
+    for (int s0 = 0; s0 < v.S; s0 += KV_PLAN_THREADS) {
+        const int s = s0 + tid;
+        const bool in = s < v.S;
+        int tok0 = 0, n = 0, L = 0;
+        if (in) {   // (what this thread wrote in the first walk)
+            const int4 q = v.req[s];
+            tok0 = a.seq_offsets[s];
+            n = q.w;
+            L = q.y >= 0 ? q.x + n : 0;
+        }
+        const int64_t rows = (int64_t)n * v.group;
+        const bool few = rows > 0 && rows <= KV_FEW_ROWS, tiled = rows > KV_FEW_ROWS;
+        const int blocks = ceil_shift(L, 6);
+        const int n_tiles = tiled ? (int)((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS) : few ? 1 : 0;
+        const int chunk = tiled ? tile_chunk : few_chunk;
+        const int parts = max(1, (blocks + chunk - 1) / chunk);
+        const int recs = n_tiles * parts;
+        const int ps = parts > 1 ? recs : 0;
+        const Scan2 up = block_scan(Scan2{((long long)(tiled ? recs : 0) << 32) | (unsigned)(few ? recs : 0), ps}, lds, t2);
+        const int few_at = few_base + (int)(unsigned)up.a - (few ? recs : 0);
+        const int tile_at = tile_base + (int)(up.a >> 32) - (tiled ? recs : 0);
+        const int ps_at = ps_base + up.b - ps;
+        if (few && v.has_few && few_at + recs <= v.max_few && ps_at + ps <= v.max_pslots)
+            for (int p = 0; p < parts; ++p) kv_write_tile(v.few + few_at + p, tok0, n, L, s, 0, p, parts, ps_at);
+        if (in) {
+            v.req[s].w = tiled ? tile_at : -1;
+            v.req_tiles[s] = make_int2(parts, ps_at);
+        }
+        if (few_tokens && tiled && v.has_tile && tile_at + recs <= v.max_tile && ps_at + ps <= v.max_pslots)
+            for (int t = 0; t < n_tiles; ++t)   // the last rows see the most keys: their tiles first
+                for (int p = 0; p < parts; ++p)
+                    kv_write_tile(v.tile + tile_at + t * parts + p, tok0, n, L, s, (n_tiles - 1 - t) * KV_TILE_ROWS, p, parts,
+                                  ps_at + (parts > 1 ? t * parts : 0));
+        few_base += (int)(unsigned)t2.a;
+        tile_base += (int)(t2.a >> 32);
+        ps_base += t2.b;
+    }
+    if (tid == 0) {
+        v.head[0] = min(few_base, v.max_few);
+        v.head[1] = min(tile_base, v.max_tile);
+    }
+}
+
+// Slots, table entries and tiles of requests with many new tokens: workgroup (request, chunk of 2048 tokens).
+__global__ __launch_bounds__(256) void kv_slots_kernel(KvPlanView v, KvPlanArgs a, int log_page)
+{
+    const int s = blockIdx.x, c = blockIdx.y, nc = gridDim.y, tid = threadIdx.x;
+    const int tok0 = a.seq_offsets[s], n = a.seq_offsets[s + 1] - tok0;
+    const int4 q = v.req[s];
+    const int n_free = v.head[2], kv = q.x, dealt = q.y, have = ceil_shift(kv, log_page);
+    const bool served = dealt >= 0;
+    const int end = min(n, (c + 1) * KV_SLOT_CHUNK);
+    for (int i = c * KV_SLOT_CHUNK + tid; i < end; i += 256)
+        a.slots[tok0 + i] = served ? kv_slot(a, s, kv + i, log_page, have, dealt, n_free) : -1;
+    if (served) {
+        for (int j = c * 256 + tid; j < q.z; j += nc * 256)
+            a.block_table[(int64_t)s * a.max_pages + have + j] = a.free_pages[n_free - 1 - (dealt + j)];
+    }
+    if (q.w < 0 || !v.has_tile) return;
+    const int L = served ? kv + n : 0;
+    const int2 t2 = v.req_tiles[s];
+    const int parts = t2.x, n_tiles = (int)(((int64_t)n * v.group + KV_TILE_ROWS - 1) / KV_TILE_ROWS), recs = n_tiles * parts;
+    if (q.w + recs > v.max_tile || (parts > 1 && t2.y + recs > v.max_pslots)) return;
+    for (int r = c * 256 + tid; r < recs; r += nc * 256) {
+        const int t = r / parts, p = r - t * parts;
+        kv_write_tile(v.tile + q.w + r, tok0, n, L, s, (n_tiles - 1 - t) * KV_TILE_ROWS, p, parts, t2.y + (parts > 1 ? t * parts : 0));
+    }
+}
+
+static int log2_of(int v)
+{
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+}
+
+hipError_t launch_kv_plan(const KvPlanView &v, const KvPlanArgs &a, hipStream_t stream)
+{
+    const int few_tokens = v.max_new <= KV_FEW_TOKENS, log_page = log2_of(a.page_tokens);
+    hipLaunchKernelGGL(kv_plan_kernel, dim3(1), dim3(KV_PLAN_THREADS), 0, stream, v, a, log_page, few_tokens);
+    if (!few_tokens)
+        hipLaunchKernelGGL(kv_slots_kernel, dim3((unsigned)v.S, (unsigned)((v.max_new + KV_SLOT_CHUNK - 1) / KV_SLOT_CHUNK)), dim3(256), 0,
+                           stream, v, a, log_page);
+    return hipGetLastError();
+}
+
+// Pages of finished requests go back on the stack, in the requests' order; their rows of the table become -1, their lengths 0.
+__global__ __launch_bounds__(KV_PLAN_THREADS) void kv_release_kernel(const int *finished, int S, int *kv_lens, int *block_table, int max_pages,
+                                                                     int log_page, int *free_pages, int *n_free, int free_cap, int n_pages,
+                                                                     int *err_word)
+{
+    __shared__ Scan2 lds[KV_PLAN_WAVES];
+    __shared__ int2 range[KV_PLAN_THREADS];
+    const int tid = threadIdx.x;
+    int base = *n_free;
+    const int before = base;
+    bool bad = base < 0 || base > free_cap;
+    base = max(0, min(base, free_cap));
+    for (int s0 = 0; s0 < S; s0 += KV_PLAN_THREADS) {
+        const int s = s0 + tid;
+        const bool done = s < S && finished[s] != 0;
+        const int kv = done ? kv_lens[s] : 0;
+        const int pages = done ? min(ceil_shift(max(kv, 0), log_page), max_pages) : 0;
+        if (done && (kv < 0 || ceil_shift(max(kv, 0), log_page) > max_pages)) bad = true;
+        Scan2 total;
+        const Scan2 up = block_scan(Scan2{0, pages}, lds, total);
+        range[tid] = make_int2(base + up.b - pages, pages);
+        if (done) kv_lens[s] = 0;
+        lds_barrier();
+        for (int w = tid >> 6; w < min(KV_PLAN_THREADS, S - s0); w += KV_PLAN_WAVES) {   // a wave per request
+            const int2 r = range[w];
+            for (int j = tid & 63; j < r.y; j += 64) {
+                int *entry = block_table + (int64_t)(s0 + w) * max_pages + j;
+                const int page = *entry;
+                if (r.x + j < free_cap) free_pages[r.x + j] = page;
+                if (r.x + j >= free_cap || page < 0 || page >= n_pages) bad = true;
+                *entry = -1;
+            }
+        }
+        base = min(base + total.b, free_cap);
+    }
+    __syncthreads();
+    if (tid == 0 && base != before) *n_free = base;
+    if (bad) atomicOr(err_word, ERR_BAD_PAGE);
+}
+
+hipError_t launch_kv_release(const int *finished, int S, int *kv_lens, int *block_table, int max_pages, int page_tokens, int *free_pages,
+                             int *n_free, int free_cap, int n_pages, int *err_word, hipStream_t stream)
+{
+    hipLaunchKernelGGL(kv_release_kernel, dim3(1), dim3(KV_PLAN_THREADS), 0, stream, finished, S, kv_lens, block_table, max_pages,
+                       log2_of(page_tokens), free_pages, n_free, free_cap, n_pages, err_word);
+    return hipGetLastError();
+}
+
+// A thread takes eight channels of a key or value: 16 bytes of bf16, four bytes of codes; the four threads of a block of 32 are
+// neighbours.  Units run over the channels of a token first, keys before values.
+template <bool APPEND>
+__global__ __launch_bounds__(256) void kv_copy_kernel(KvPages p, char *k, char *v, int64_t k_stride, int64_t v_stride, int64_t units,
+                                                      int per_token, const int *__restrict__ slots, int *err_word)
+{
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;   // (units are a multiple of four per token: no block is cut)
+    if (u >= units) return;
+    const int64_t t = u / per_token;
+    int c = (int)(u - t * per_token);
+    const int half = per_token / 2;
+    const bool is_v = c >= half;
+    if (is_v) c -= half;
+    const int D8 = p.D / 8, h = c / D8, c8 = c - h * D8;
+    const int slot = slots[t], log_page = p.log_blocks + 6;
+    char *row = is_v ? v + t * v_stride * 2 : k + t * k_stride * 2;
+    uint4 *at = reinterpret_cast<uint4 *>(row) + c;
+    if (slot < 0 || (slot >> log_page) >= p.n_pages) {
+        if (slot != -1) atomicOr(err_word, ERR_BAD_PAGE);
+        if constexpr (!APPEND) *at = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const int in_page = slot & ((1 << log_page) - 1), tok = in_page & 63, i = tok >> 4, m = tok & 15, b = c8 >> 2;
+    char *rec = p.data + (int64_t)(slot >> log_page) * p.page_bytes() +
+                ((int64_t)((h << p.log_blocks) + (in_page >> 6))) * kv_record_bytes(p.D);
+    char *codes = is_v ? rec + 32 * p.D + (i * D8 + c8) * 64 + m * 4 : rec + (i * (p.D / 32) + b) * 256 + m * 16 + (c8 & 3) * 4;
+    uint8_t *scale = reinterpret_cast<uint8_t *>(rec) + (is_v ? 66 : 64) * p.D + b * 64 + m * 4 + i;
+    if constexpr (APPEND) {
+        const uint4 x = *at;
+        uint32_t amax = bf16x8_amax(x);
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 1));
+        amax = max(amax, (uint32_t)__shfl_xor((int)amax, 2));
+        const uint32_t E = mx4_scale_byte(amax);
+        *reinterpret_cast<uint32_t *>(codes) = mx4_encode(x, bits_f32(E << 23));
+        if ((c8 & 3) == 0) *scale = (uint8_t)E;
+    } else {
+        *at = mx4_decode(*reinterpret_cast<const uint32_t *>(codes), bits_f32((uint32_t)*scale << 23));
+    }
+}
+
+hipError_t launch_kv_append(const KvPages &p, const void *k, const void *v, int64_t k_stride, int64_t v_stride, int64_t T,
+                            const int *slots, int *err_word, hipStream_t stream)
+{
+    const int per_token = 2 * p.n_kv * p.D / 8;
+    const int64_t units = T * per_token;
+    hipLaunchKernelGGL(kv_copy_kernel<true>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, stream, p,
+                       const_cast<char *>(static_cast<const char *>(k)), const_cast<char *>(static_cast<const char *>(v)), k_stride,
+                       v_stride, units, per_token, slots, err_word);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_gather(const KvPages &p, void *k, void *v, int64_t T, const int *slots, int *err_word, hipStream_t stream)
+{
+    const int per_token = 2 * p.n_kv * p.D / 8;
+    const int64_t units = T * per_token;
+    hipLaunchKernelGGL(kv_copy_kernel<false>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, stream, p, static_cast<char *>(k),
+                       static_cast<char *>(v), (int64_t)p.n_kv * p.D, (int64_t)p.n_kv * p.D, units, per_token, slots, err_word);
+    return hipGetLastError();
+}
+
+}  // namespace moin

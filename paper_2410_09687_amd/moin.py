@@ -27,7 +27,7 @@ MOIN_ROUTE_SAME_CENTROIDS = 2
  K_KMEANS_SORT, K_KMEANS_SUM, K_KMEANS_FINAL) = range(11)
 KERNEL_NAMES = ["plan", "shrink", "linear", "route", "route_aux", "decode_shrink", "decode_expand",
                 "decode_base", "kmeans_sort", "kmeans_sum", "kmeans_final", "mx_quant", "mx_linear",
-                "probe_mfma", "probe_read"]
+                "probe_mfma", "probe_read", "kv_plan", "kv_append", "kv_attend", "mx4_linear"]
 
 EXPORTS = [
     "moin_create", "moin_destroy", "moin_strerror", "moin_check", "moin_route", "moin_histogram",
@@ -41,12 +41,20 @@ EXPORTS = [
     "moin_lora_linear_planned_shared", "moin_route_topk", "moin_merge_adapters",
     "moin_reserve_workspace", "moin_workspace_bytes", "moin_plan_reserve", "moin_route_static",
     "moin_cache_set_overlap", "moin_route_plan",
+    "moin_mx4_bytes", "moin_mx4_quantize", "moin_mx4_dequantize", "moin_mx4_linear", "moin_lora_linear_mx4_planned",
+    "moin_kv_page_bytes", "moin_kv_plan_create", "moin_kv_plan_destroy", "moin_kv_plan_build", "moin_kv_release", "moin_kv_append",
+    "moin_kv_gather", "moin_kv_attention",
 ]
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
 CACHE_STATS = ["batches", "seq_hits", "seq_misses", "loads", "evictions", "overflows", "bytes"]
 
 _lib = None
 _native = None   # the module of csrc/binding.cpp, once load() has run
+
+
+class _KVPagesStruct(ctypes.Structure):   # moin_kv_pages
+    _fields_ = [("data", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("n_kv", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class MoinError(RuntimeError):
@@ -98,7 +106,6 @@ def load() -> ctypes.CDLL:
     lib.moin_workspace_bytes.argtypes = [vp]
     lib.moin_plan_reserve.argtypes = [vp, vp, i32, i64, i32, vp]
     lib.moin_probe_out_len.argtypes = [vp]
-    lib.moin_probe_out_len.restype = c.c_int64
     lib.moin_probe_mfma_bf16.argtypes = [vp, vp, i64, i32, vp, c.POINTER(c.c_double), vp]
     lib.moin_probe_mfma_mxfp8.argtypes = [vp, vp, i64, i32, vp, c.POINTER(c.c_double), vp]
     lib.moin_probe_read.argtypes = [vp, vp, i64, vp, vp]
@@ -125,11 +132,27 @@ def load() -> ctypes.CDLL:
     lib.moin_timing_enable.argtypes = [vp, c.c_int]
     lib.moin_timing_reset.argtypes = [vp]
     lib.moin_timing_read.argtypes = [vp, c.c_int, c.POINTER(c.c_double), c.POINTER(i64)]
+    lib.moin_mx4_bytes.argtypes = [i64, i64]
+    lib.moin_mx4_quantize.argtypes = [vp, vp, i64, i64, vp, vp]
+    lib.moin_mx4_dequantize.argtypes = [vp, vp, i64, i64, vp, vp]
+    lib.moin_mx4_linear.argtypes = [vp, vp, i64, vp, i32, i32, vp, c.c_int, vp]
+    lib.moin_lora_linear_mx4_planned.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, i32, c.c_float, vp, c.c_int, vp]
+    lib.moin_kv_page_bytes.argtypes = [i32, i32, i32]
+    lib.moin_kv_plan_create.argtypes = [vp, c.POINTER(vp)]
+    lib.moin_kv_plan_destroy.argtypes = [vp]
+    lib.moin_kv_plan_destroy.restype = None
+    lib.moin_kv_plan_build.argtypes = [vp, vp, vp, vp, i32, i64, i32, i32, i32, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp]
+    lib.moin_kv_release.argtypes = [vp, vp, i32, vp, i32, i32, vp, i32, vp, i32, vp, vp]
+    kvp = c.POINTER(_KVPagesStruct)
+    lib.moin_kv_append.argtypes = [vp, kvp, vp, vp, i64, i64, i64, vp, vp]
+    lib.moin_kv_gather.argtypes = [vp, kvp, vp, i64, vp, vp, vp]
+    lib.moin_kv_attention.argtypes = [vp, vp, kvp, vp, i64, i32, vp, i32, c.c_float, i32, vp, c.c_int, vp, vp]
+    sizes = ("moin_probe_out_len", "moin_workspace_bytes", "moin_mx4_bytes", "moin_kv_page_bytes")
     for name in EXPORTS:
-        if name not in ("moin_destroy", "moin_plan_destroy", "moin_strerror", "moin_cache_destroy",
-                        "moin_probe_out_len", "moin_workspace_bytes"):
+        if name not in ("moin_destroy", "moin_plan_destroy", "moin_strerror", "moin_cache_destroy", "moin_kv_plan_destroy", *sizes):
             getattr(lib, name).restype = c.c_int
-    lib.moin_workspace_bytes.restype = c.c_int64
+    for name in sizes:
+        getattr(lib, name).restype = c.c_int64
     from . import _moin_binding   # (finds libmoin.so beside itself, the one opened above)
     _moin_binding.set_error(MoinError)
     _native = _moin_binding
@@ -594,3 +617,151 @@ class Cache:
             self.close()
         except Exception:
             pass
+
+
+# ---- serving in four bits --------------------------------------------------------------------------------
+
+class MX4Weight:
+    """A weight ``[d_out, d_in]`` in MXFP4: ``data`` (uint8), the records of ``moin_mx4_quantize``."""
+
+    def __init__(self, data: torch.Tensor, d_out: int, d_in: int):
+        if data.dtype != torch.uint8 or data.numel() == 0 or data.numel() != load().moin_mx4_bytes(int(d_out), int(d_in)):
+            raise ValueError("data: the uint8 records of a [d_out,d_in] weight expected")
+        self.data, self.d_out, self.d_in = data, int(d_out), int(d_in)
+
+
+def moin_mx4_quantize(ctx: Context, W: torch.Tensor, stream=None) -> MX4Weight:
+    """A bf16 weight ``[d_out, d_in]`` (``d_in`` a multiple of 8) in MXFP4: blocks of 32 E2M1 values that share a power of two."""
+    if W.dim() != 2 or W.shape[0] == 0 or W.shape[1] == 0 or W.shape[1] % 8:
+        raise ValueError("W [d_out,d_in] with d_in a positive multiple of 8 expected")
+    d_out, d_in = W.shape
+    nbytes = int(load().moin_mx4_bytes(d_out, d_in))
+    if nbytes == 0:
+        raise ValueError("W: sizes that are not supported")
+    data = torch.empty(nbytes, dtype=torch.uint8, device=W.device)
+    _ck(load().moin_mx4_quantize(ctx._h, _dev_ptr(W, "W", torch.bfloat16), d_out, d_in, _dev_ptr(data, "data"),
+                                 _stream_ptr(stream)), "moin_mx4_quantize")
+    return MX4Weight(data, d_out, d_in)
+
+
+def moin_mx4_dequantize(ctx: Context, W4: MX4Weight, stream=None) -> torch.Tensor:
+    """The bf16 values that a weight's codes stand for."""
+    W = torch.empty((W4.d_out, W4.d_in), dtype=torch.bfloat16, device=W4.data.device)
+    _ck(load().moin_mx4_dequantize(ctx._h, _dev_ptr(W4.data, "W4", torch.uint8), W4.d_out, W4.d_in, _dev_ptr(W, "W"),
+                                   _stream_ptr(stream)), "moin_mx4_dequantize")
+    return W
+
+
+def moin_mx4_linear(ctx: Context, x: torch.Tensor, W4: MX4Weight, y_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """``y = x dq(W4)^T``, without adapters."""
+    load()
+    return _native.mx4_linear(ctx._h.value, x, W4.data, W4.d_out, W4.d_in, y_dtype, out, _stream_ptr(stream))
+
+
+def moin_lora_linear_mx4_planned(ctx: Context, plan: Plan, x: torch.Tensor, W4: MX4Weight, A_stack: Optional[torch.Tensor],
+                                 B_stack: Optional[torch.Tensor], scale: float, y_dtype=torch.bfloat16,
+                                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``moin_lora_linear_planned`` on a 4-bit base."""
+    load()
+    return _native.lora_linear_mx4_planned(ctx._h.value, plan._h.value, plan.T, plan.E, x, W4.data, W4.d_out, W4.d_in, A_stack,
+                                           B_stack, float(scale), y_dtype, out, _stream_ptr(stream))
+
+
+class KVPages:
+    """A paged cache of keys and values in MXFP4 (one layer's): ``data`` (uint8), ``n_kv`` heads of ``head_dim`` (64, 128, 256)
+    channels, pages of ``page_tokens`` (64, 128, 256) tokens."""
+
+    def __init__(self, data: torch.Tensor, n_kv: int, head_dim: int, page_tokens: int = 64):
+        nbytes = self.page_bytes(n_kv, head_dim, page_tokens)
+        if data.dtype != torch.uint8 or data.numel() == 0 or data.numel() % nbytes:
+            raise ValueError(f"data: uint8, a positive multiple of a page's {nbytes} bytes expected")
+        self.data, self.n_kv, self.head_dim, self.page_tokens = data, int(n_kv), int(head_dim), int(page_tokens)
+        self.n_pages = data.numel() // nbytes
+
+    @staticmethod
+    def page_bytes(n_kv: int, head_dim: int, page_tokens: int = 64) -> int:
+        nbytes = int(load().moin_kv_page_bytes(int(page_tokens), int(n_kv), int(head_dim)))
+        if nbytes == 0:
+            raise ValueError("page_tokens and head_dim: 64, 128 or 256, at least one kv head expected")
+        return nbytes
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv: int, head_dim: int, page_tokens: int = 64, device="cuda"):
+        nbytes = cls.page_bytes(n_kv, head_dim, page_tokens)
+        return cls(torch.empty((int(n_pages), nbytes), dtype=torch.uint8, device=device), n_kv, head_dim, page_tokens)
+
+
+class KVPlan:
+    """A step of the paged cache: which pages and slots its new tokens take and how its attention is dealt over the chip.  Built
+    once per step, used by every layer."""
+
+    def __init__(self, ctx: Context):
+        self.ctx = ctx
+        self._h = ctypes.c_void_p()
+        _ck(load().moin_kv_plan_create(ctx._h, ctypes.byref(self._h)), "moin_kv_plan_create")
+        self.T = self.S = 0
+
+    def build(self, kv_lens: torch.Tensor, new_lens: torch.Tensor, T: int, block_table: torch.Tensor, free_pages: torch.Tensor,
+              n_free: torch.Tensor, *, n_pages: int, page_tokens: int, n_heads: int, n_kv: int, max_new: Optional[int] = None,
+              out=None, stream=None):
+        """Deals pages to the requests' ``new_lens`` tokens (``T`` in all, at most ``max_new`` each) and returns ``(seq_offsets
+        [S+1], kv_lens [S], slots [T], n_free [1])`` as they are after the step; ``block_table`` [S, max_pages] is filled in place.
+        ``out``: the four preallocated (``kv_lens`` and ``n_free`` may be the inputs).  All int32 on the device."""
+        load()
+        r = _native.kv_plan_build(self.ctx._h.value, self._h.value, kv_lens, new_lens, int(T),
+                                  int(T if max_new is None else max_new), int(n_heads), int(n_kv), int(page_tokens), int(n_pages),
+                                  block_table, free_pages, n_free, out, _stream_ptr(stream))
+        self.T, self.S = int(T), kv_lens.numel()
+        return r
+
+    def close(self):
+        if getattr(self, "_h", None) is not None and self._h:
+            load().moin_kv_plan_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def moin_kv_release(ctx: Context, finished: torch.Tensor, kv_lens: torch.Tensor, block_table: torch.Tensor,
+                    free_pages: torch.Tensor, n_free: torch.Tensor, *, n_pages: int, page_tokens: int, stream=None) -> None:
+    """Gives the pages of requests with ``finished`` (int32 [S]) not 0 back to ``free_pages`` / ``n_free``, in place."""
+    S = finished.numel()
+    if kv_lens.numel() != S or block_table.dim() != 2 or block_table.shape[0] != S or n_free.numel() != 1:
+        raise ValueError("finished [S], kv_lens [S], block_table [S,max_pages] and n_free [1] expected")
+    i32 = torch.int32
+    _ck(load().moin_kv_release(ctx._h, _dev_ptr(finished, "finished", i32) if S else None, S,
+                               _dev_ptr(kv_lens, "kv_lens", i32) if S else None, int(page_tokens), int(n_pages),
+                               _dev_ptr(block_table, "block_table", i32) if S else None, block_table.shape[1],
+                               _dev_ptr(free_pages, "free_pages", i32) if free_pages.numel() else None, free_pages.numel(),
+                               _dev_ptr(n_free, "n_free", i32), _stream_ptr(stream)), "moin_kv_release")
+
+
+def moin_kv_append(ctx: Context, pages: KVPages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+    """Quantises ``k``, ``v`` [T, n_kv, head_dim] (bf16; rows of tokens may be strided, as columns of one projection's output are)
+    into ``slots`` [T]; -1 is skipped."""
+    load()
+    _native.kv_append(ctx._h.value, pages.data, pages.n_pages, pages.page_tokens, pages.n_kv, pages.head_dim, k, v, slots,
+                      _stream_ptr(stream))
+
+
+def moin_kv_gather(ctx: Context, pages: KVPages, slots: torch.Tensor, stream=None):
+    """The keys and values that ``slots`` [T] hold: ``(k, v)``, bf16 [T, n_kv, head_dim]; zeros for -1."""
+    load()
+    return _native.kv_gather(ctx._h.value, pages.data, pages.n_pages, pages.page_tokens, pages.n_kv, pages.head_dim, slots,
+                             _stream_ptr(stream))
+
+
+def moin_kv_attention(ctx: Context, plan: KVPlan, pages: KVPages, q: torch.Tensor, block_table: torch.Tensor,
+                      scale: Optional[float] = None, window: int = 0, y_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None,
+                      want_lse: bool = False, stream=None):
+    """Causal attention of the step's tokens ``q`` [T, n_heads, head_dim] (bf16) over the cache, their own keys appended before:
+    ``(y, lse or None)``.  ``scale``: 1 / sqrt(head_dim) by default.  ``window`` > 0: the last so many keys alone."""
+    load()
+    return _native.kv_attention(ctx._h.value, plan._h.value, plan.T, plan.S, pages.data, pages.n_pages, pages.page_tokens, pages.n_kv,
+                                pages.head_dim, q, block_table, float(pages.head_dim ** -0.5 if scale is None else scale), int(window),
+                                y_dtype, out, bool(want_lse), _stream_ptr(stream))
