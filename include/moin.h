@@ -553,10 +553,10 @@ int moin_merge_adapters(moin_ctx *ctx, const void *A_stack, const void *B_stack,
  *   moin_lora_linear_mx4_planned
  *                        moin_lora_linear_planned on such a base: y = x dq(W4)^T +
  *                        scale * act(x A_e^T) B_e^T.
- * x, stacks, y, sizes, workspace and errors as in moin_lora_linear_planned.  Up to 256 tokens
- * (gathered ones, where there are adapters) are multiplied with the codes; beyond, the
- * call turns the weight into bf16 in the context's workspace (2 d_in d_out bytes more) and
- * the results are, bit for bit, those of a bf16 weight with these values. */
+ * x, stacks, y, sizes, workspace and errors as in moin_lora_linear_planned.  Calls without
+ * adapters and batches that the decode path gathers by expert are multiplied with the codes; on the
+ * prefill path the call turns the weight into bf16 in the context's workspace (2 d_in d_out bytes
+ * more) and the results are, bit for bit, those of a bf16 weight with these values. */
 int64_t moin_mx4_bytes(int64_t rows, int64_t cols);
 int moin_mx4_quantize(moin_ctx *ctx, const void *src, int64_t rows, int64_t cols, void *packed, void *stream);
 int moin_mx4_dequantize(moin_ctx *ctx, const void *packed, int64_t rows, int64_t cols, void *dst, void *stream);

@@ -20,6 +20,7 @@ hipError_t prepare_decode_kernels();
 hipError_t prepare_kmeans_kernels();
 hipError_t prepare_mx_kernels();
 hipError_t prepare_plan_kernels();
+hipError_t prepare_mx4_kernels();
 hipError_t prepare_kernels()
 {
     hipError_t e = prepare_linear_kernels();
@@ -28,6 +29,7 @@ hipError_t prepare_kernels()
     if ((e = prepare_kmeans_kernels()) != hipSuccess) return e;
     if ((e = prepare_mx_kernels()) != hipSuccess) return e;
     if ((e = prepare_plan_kernels()) != hipSuccess) return e;
+    if ((e = prepare_mx4_kernels()) != hipSuccess) return e;
     return prepare_route_kernels();
 }
 }  // namespace moin
@@ -498,26 +500,28 @@ int linear_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, con
     a.u_hi = a.u_lo = nullptr;
 
     const bool gathered = gathered_pays(pv, d_in, a.r);
-    // W in MXFP4: a few gathered tokens are multiplied with the codes; for more the weight is turned into bf16 (exactly, so that
-    // the results are those of a bf16 weight with these values), at the workspace's start, ahead of everything else there
-    const bool direct = mx4 && gathered && mx4_direct_pays(pv.T, d_in, d_out);
+    // W in MXFP4: gathered tokens, and calls without adapters, are multiplied with the codes.  For row tiles with adapters, whose two
+    // products share their accumulators, the weight is turned into bf16 (exactly, so that the results are those of a bf16 weight
+    // with these values), at the workspace's start, ahead of everything else there.
+    const bool direct = mx4 && (gathered || a.r == 0);
     const size_t w_bytes = mx4 && !direct ? align_up((size_t)d_out * (size_t)d_in * 2, 256) : 0;
     const auto reserve = [&](size_t bytes) -> int {
-        const size_t keep = a.r > 0 ? linear_ws_most(pv, 1, d_in, &d_out, r) : 0;
-        const int rc = ensure_ws(ctx, w_bytes + bytes, stream, false, w_bytes + keep);
+        const int rc = ensure_ws(ctx, w_bytes + bytes, stream, false, w_bytes + linear_ws_most(pv, 1, d_in, &d_out, r));
         if (rc != MOIN_OK || !w_bytes) return rc;
         const hipError_t e = timed(ctx, MOIN_K_MX4_LINEAR, stream, [&] { return launch_mx4_dequantize(W, d_out, d_in, ctx->ws, stream); });
         a.W = ctx->ws;
         return e == hipSuccess ? MOIN_OK : MOIN_EHIP;
     };
+    if (direct && a.r == 0)
+        return timed(ctx, MOIN_K_MX4_LINEAR, stream, [&] { return launch_mx4_linear(x, W, y, a.y_f32, pv.T, d_in, d_out, stream); }) == hipSuccess
+                   ? MOIN_OK
+                   : MOIN_EHIP;
     a.ldu = gathered ? a.r : prefill_ldu(a);
     const size_t u_bytes = align_up((size_t)pv.T * (size_t)a.ldu * 2, 256);
     if (!gathered) {
-        if (a.r > 0 || w_bytes) {
-            const int rc = reserve(a.r > 0 ? 2 * u_bytes : 0);
-            if (rc != MOIN_OK) return rc;
-        }
         if (a.r > 0) {
+            const int rc = reserve(2 * u_bytes);
+            if (rc != MOIN_OK) return rc;
             a.u_hi = static_cast<char *>(ctx->ws) + w_bytes;
             a.u_lo = static_cast<char *>(a.u_hi) + u_bytes;
             if (timed(ctx, MOIN_K_SHRINK, stream, [&] { return launch_prefill_shrink(pv, a, stream); }) !=
@@ -543,14 +547,7 @@ int linear_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, con
     pp.tile_rank = pv.plain_rank; pp.n_tiles = pv.plain_n; pp.max_tiles = pv.max_plain;
     if (a.r == 0) {
         // no adapters anywhere in the call: the base GEMM writes y itself
-        if (w_bytes) {
-            const int rc = reserve(0);
-            if (rc != MOIN_OK) return rc;
-        }
-        if (direct) {
-            if (timed(ctx, MOIN_K_MX4_LINEAR, stream, [&] { return launch_mx4_linear(x, W, y, a.y_f32, pv.T, d_in, d_out, stream); }) != hipSuccess)
-                return MOIN_EHIP;
-        } else if (big) {
+        if (big) {
             LinearArgs ab = a;
             if (timed(ctx, MOIN_K_LINEAR, stream, [&] { return launch_prefill_linear(pp, ab, stream); }) != hipSuccess)
                 return MOIN_EHIP;
@@ -1607,23 +1604,9 @@ int moin_mx4_linear(moin_ctx *ctx, const void *x, int64_t T, const void *W4, int
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return MOIN_EHIP;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (mx4_direct_pays(T, d_in, d_out))
-        return timed(ctx, MOIN_K_MX4_LINEAR, st, [&] { return launch_mx4_linear(x, W4, y, y_dt == MOIN_F32, T, d_in, d_out, st); }) == hipSuccess
-                   ? MOIN_OK
-                   : MOIN_EHIP;
-    const int rc = ensure_ws(ctx, align_up((size_t)d_out * (size_t)d_in * 2, 256), st);
-    if (rc != MOIN_OK) return rc;
-    if (timed(ctx, MOIN_K_MX4_LINEAR, st, [&] { return launch_mx4_dequantize(W4, d_out, d_in, ctx->ws, st); }) != hipSuccess) return MOIN_EHIP;
-    LinearArgs a{};
-    a.x = x;
-    a.W = ctx->ws;
-    a.y = y;
-    a.y_f32 = y_dt == MOIN_F32;
-    a.d_in = d_in;
-    a.d_out = d_out;
-    PlanView pv{};
-    pv.T = T;
-    return timed(ctx, MOIN_K_DECODE_BASE, st, [&] { return launch_decode_base_only(pv, a, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+    return timed(ctx, MOIN_K_MX4_LINEAR, st, [&] { return launch_mx4_linear(x, W4, y, y_dt == MOIN_F32, T, d_in, d_out, st); }) == hipSuccess
+               ? MOIN_OK
+               : MOIN_EHIP;
 }
 
 int moin_lora_linear_mx4_planned(moin_ctx *ctx, const moin_plan *plan, const void *x, const void *W4, const void *A_stack, const void *B_stack,

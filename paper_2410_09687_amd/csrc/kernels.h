@@ -278,13 +278,10 @@ hipError_t launch_merge_adapters(const void *A_stack, const void *B_stack, int E
                                  const int *ids, const float *weights, int n, int r_out, void *A_out, void *B_out,
                                  int *err_word, hipStream_t stream);
 
-// Base weights in MXFP4 (mx4.hip): bytes of a weight's records; to and from bf16; y = x dq(W)^T straight from the codes, which pays for
-// so few tokens (beyond, the weight is turned into bf16 and the prefill kernels take it).
-constexpr int MX4_DIRECT_MAX_T = 256;
+// Base weights in MXFP4 (mx4.hip): bytes of a weight's records; to and from bf16; y = x dq(W)^T straight from the codes.
 int64_t mx4_bytes(int64_t rows, int64_t cols);
 hipError_t launch_mx4_quantize(const void *src, int64_t rows, int64_t cols, void *dst, hipStream_t stream);
 hipError_t launch_mx4_dequantize(const void *src, int64_t rows, int64_t cols, void *dst, hipStream_t stream);
-bool mx4_direct_pays(int64_t T, int d_in, int d_out);
 hipError_t launch_mx4_linear(const void *x, const void *W, void *y, int y_f32, int64_t T, int d_in, int d_out, hipStream_t stream);
 
 // on-box ceilings (probe.hip): out holds probe_out_len() elements

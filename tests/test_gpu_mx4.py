@@ -61,7 +61,7 @@ def check(y, x, W, extra=None):
 
 
 @pytest.mark.parametrize("y_dtype", [BF16, F32])
-@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 33, 64, 65, 200, 256, 257, 300])
+@pytest.mark.parametrize("T", [1, 2, 4, 5, 15, 16, 17, 32, 33, 64, 65, 200, 256, 300, 1100])
 @pytest.mark.parametrize("d_out,d_in", [(8, 8), (256, 256), (136, 1000), (1416, 520), (24, 5632)])
 def test_linear(T, d_out, d_in, y_dtype):
     W, x = weight(d_in, d_out, d_in), inputs(T, T, d_in)
@@ -70,6 +70,19 @@ def test_linear(T, d_out, d_in, y_dtype):
     ctx().check()
     check(y, f64(x), fb.held(padded(f64(W)))[:, :d_in])
     assert torch.equal(y, moin.moin_mx4_linear(ctx(), x, W4, y_dtype=y_dtype))
+
+
+@pytest.mark.parametrize("T", [1, 16, 24, 70])
+@pytest.mark.parametrize("d_out,d_in", [(4112, 264), (16400, 136), (16400, 1032)])
+def test_wide_weights(T, d_out, d_in):
+    """More rows than the shapes for few tiles take, and rows of codes that are not whole records."""
+    W, x = weight(d_in, d_out, d_in), inputs(T, T, d_in)
+    W4 = moin.moin_mx4_quantize(ctx(), W)
+    held = moin.moin_mx4_dequantize(ctx(), W4)
+    y = moin.moin_mx4_linear(ctx(), x, W4, y_dtype=F32)
+    want = x.double() @ held.double().t().contiguous()
+    spread = x.double().abs() @ held.double().abs().t().contiguous()
+    assert ((y.double() - want).abs() <= d_in * 2.0 ** -24 * spread).all()
 
 
 def batch(T, S, E, seed):
@@ -105,8 +118,8 @@ def test_with_adapters(T, S, d_out, d_in, r, y_dtype):
         wide = 2 * (np.abs(fx[rows]) @ np.abs(fA[e]).T) @ np.abs(fB[e]).T
         off_by[rows] = 2 * 2.0 ** -16 * np.abs(u) @ np.abs(fB[e]).T + (d_in + 2 * r + 8) * 2.0 ** -24 * wide
     check(y, fx, fb.held(padded(f64(W)))[:, :d_in], (term, off_by))
-    # beyond the calls that read the codes themselves, the bits of a bf16 weight with these values
-    if T > 256:
+    # on the prefill path, the bits of a bf16 weight with these values
+    if T > 1024 and T > 128 * S:
         full = moin.moin_mx4_dequantize(ctx(), W4)
         assert torch.equal(y, moin.moin_lora_linear_planned(ctx(), plan, x, full, A, B, 2.0, y_dtype=y_dtype))
     # no adapters at all
@@ -155,28 +168,47 @@ def test_graph_and_stream():
 
 def test_a_first_call_that_needs_the_weight_in_bf16_is_refused_under_capture():
     own = moin.Context(0)
-    W4, x = moin.moin_mx4_quantize(own, weight(10, 256, 256)), inputs(10, 400, 256)
-    y = torch.empty((400, 256), dtype=BF16, device="cuda")
+    W4, x = moin.moin_mx4_quantize(own, weight(10, 256, 256)), inputs(10, 2000, 256)
+    A, B = inputs(11, 16, 256).view(2, 8, 256), inputs(12, 512, 8).view(2, 256, 8)
+    plan = moin.Plan(own).build(torch.tensor([0, 700, 2000], dtype=I32).cuda(), torch.tensor([1, 0], dtype=I32).cuda(), 2000, 2)
+    run = lambda: moin.moin_lora_linear_mx4_planned(own, plan, x, W4, A, B, 1.0, out=y)   # noqa: E731
+    y = torch.empty((2000, 256), dtype=BF16, device="cuda")
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g, stream=side):
             with pytest.raises(moin.MoinError) as e:
-                moin.moin_mx4_linear(own, x, W4, out=y)
+                run()
             assert e.value.code == -6
             torch.zeros(1, device="cuda")
     torch.cuda.synchronize()
-    want = moin.moin_mx4_linear(own, x, W4)
+    want = run().clone()
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g):
-        moin.moin_mx4_linear(own, x, W4, out=y)
+        run()
     for _ in range(3):
         y.zero_()
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want)
     del g
+    plan.close()
     own.close()
+
+
+def test_infinities_stay_where_they_are():
+    """An infinite activation makes infinities and, where the weight is 0, NaN, also in the last columns of rows that are not whole blocks."""
+    for T in (1, 10, 40):
+        W = weight(13, 64, 520)
+        W[3, 519] = 0
+        W[4, 519] = 0.25
+        x = inputs(13, T, 520)
+        x[0, 519] = float("inf")
+        W4 = moin.moin_mx4_quantize(ctx(), W)
+        y = moin.moin_mx4_linear(ctx(), x, W4, y_dtype=F32)
+        held = moin.moin_mx4_dequantize(ctx(), W4)[:, 519]
+        assert torch.equal(torch.isnan(y[0]), held == 0)
+        assert (y[0][held > 0] == float("inf")).all() and (y[0][held < 0] == -float("inf")).all() and torch.isfinite(y[1:]).all()
 
 
 def test_refusals():
