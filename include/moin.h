@@ -638,7 +638,7 @@ int moin_kv_gather(moin_ctx *ctx, const moin_kv_pages *pages, const int32_t *slo
  *   y [T, n_heads, head_dim] out, bf16 or fp32;  lse [T, n_heads] fp32 out or NULL: m + log(sum)
  * A row that sees no key is zeros, its lse -inf.  scale > 0 and finite.  A block of NaNs makes the
  * rows that see it NaN, and no others.  Scores and sums are fp32; the weights enter the second
- * product as bf16, for fp32 results as the sum of two bf16.  A call repeated gives the same bits.
+ * product as bf16, for fp32 results as the sum of three bf16.  A call repeated gives the same bits.
  * `plan` is of moin_kv_plan_build with the same n_heads and n_kv and the block_table it filled;
  * pages that the cache does not have raise the sticky data fault and count as unseen.
  * Workspace: partial results of keys that are walked in parts.  Errors: MOIN_EINVAL (null, a plan that

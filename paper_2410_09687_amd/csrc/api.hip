@@ -1705,7 +1705,9 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
     hipStream_t st = static_cast<hipStream_t>(stream);
     v.max_new = (int)std::min<int64_t>(max_new, T);
     v.has_tile = (int64_t)v.max_new * group > KV_FEW_ROWS;
-    v.has_few = group <= KV_FEW_ROWS && (S > 1 || !v.has_tile);
+    // (tokens that every request has at least, as none has more than max_new)
+    const int64_t least = T - (int64_t)(S - 1) * v.max_new;
+    v.has_few = least * group <= KV_FEW_ROWS && group <= KV_FEW_ROWS;
     // parts of at least 1 / goal of a list's records each: no more than the goal beside the tiles themselves, and
     // tiles of several parts have at most twice that many
     const int few_goal = std::max(1, KV_FEW_TARGET / n_kv), tile_goal = std::max(1, KV_TILE_TARGET / n_kv);

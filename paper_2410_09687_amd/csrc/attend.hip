@@ -13,7 +13,7 @@
 //      of eight accumulators.  (D = 64: words m % 8, the nibbles of half m / 8.)
 // Codes become bf16 exactly, two a conversion, the block's scale in the same instruction; V's pairs of channels are then regrouped into pairs
 // of keys, one v_perm a pair.  Scores, statistics and sums are fp32; the weights exp(s - m) are rounded to bf16 for the second product, for
-// fp32 results as the sum of two bf16.
+// fp32 results as the sum of three bf16.
 //
 // Bound by memory where a request adds one token (68 D bytes a record and kv head against 4 D flops a row and key); by the vector
 // unit's softmax in prompts.
@@ -37,40 +37,43 @@ struct Record {
     uint4 vs[SB];
 };
 
+// Where in a record a lane's pieces lie.
 template <int D>
-__device__ __forceinline__ void load_record(Record<D> &r, const char *rec, int lane)
+struct Places {
+    uint32_t k, v, ks, vs;
+    __device__ __forceinline__ explicit Places(int lane)
+    {
+        const uint32_t m = lane & 15, g = lane >> 4;
+        k = D == 64 ? (g >> 1) * 256 + m * 16 + (g & 1) * 8 : g * 256 + m * 16;
+        ks = 64 * D + (D == 64 ? g >> 1 : g) * 64 + m * 4;
+        v = 32 * D + (D == 64 ? m & 7 : m) * 64 + g * 16;
+        vs = 66 * D + (D == 64 ? (m & 7) >> 2 : m >> 2) * 64 + g * 16;
+    }
+};
+
+template <int D>
+__device__ __forceinline__ void load_record(Record<D> &r, const char *rec, const Places<D> &at)
 {
-    const int m = lane & 15, g = lane >> 4;
-    if constexpr (D == 64) {
-        const char *kp = rec + (g >> 1) * 256 + m * 16 + (g & 1) * 8;
+#pragma unroll
+    for (int b = 0; b < Record<D>::SB; ++b) {
+        r.ks[b] = *reinterpret_cast<const uint32_t *>(rec + (at.ks + b * 256));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint2 x = *reinterpret_cast<const uint2 *>(kp + i * 512);
-            r.k[i][0] = x.x;
-            r.k[i][1] = x.y;
-        }
-        r.ks[0] = *reinterpret_cast<const uint32_t *>(rec + 64 * D + (g >> 1) * 64 + m * 4);
-        const char *vp = rec + 32 * D + (m & 7) * 64 + g * 16;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.v[i][0] = *reinterpret_cast<const uint4 *>(vp + i * 512);
-        r.vs[0] = *reinterpret_cast<const uint4 *>(rec + 66 * D + ((m & 7) >> 2) * 64 + g * 16);
-    } else {
-#pragma unroll
-        for (int b = 0; b < Record<D>::SB; ++b) {
-            const char *kp = rec + (b * 4 + g) * 256 + m * 16;
-            const char *vp = rec + 32 * D + (b * 16 + m) * 64 + g * 16;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 x = *reinterpret_cast<const uint4 *>(kp + i * 8 * D);
+            if constexpr (D == 64) {
+                const uint2 x = *reinterpret_cast<const uint2 *>(rec + (at.k + i * 8 * D));
+                r.k[i][0] = x.x;
+                r.k[i][1] = x.y;
+            } else {
+                const uint4 x = *reinterpret_cast<const uint4 *>(rec + (at.k + i * 8 * D + b * 1024));
                 r.k[i][4 * b] = x.x;
                 r.k[i][4 * b + 1] = x.y;
                 r.k[i][4 * b + 2] = x.z;
                 r.k[i][4 * b + 3] = x.w;
-                r.v[i][b] = *reinterpret_cast<const uint4 *>(vp + i * 8 * D);
             }
-            r.ks[b] = *reinterpret_cast<const uint32_t *>(rec + 64 * D + (b * 4 + g) * 64 + m * 4);
-            r.vs[b] = *reinterpret_cast<const uint4 *>(rec + 66 * D + (b * 4 + (m >> 2)) * 64 + g * 16);
         }
+        r.vs[b] = *reinterpret_cast<const uint4 *>(rec + (at.vs + b * 256));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[i][b] = *reinterpret_cast<const uint4 *>(rec + (at.v + i * 8 * D + b * 1024));
     }
 }
 
@@ -119,82 +122,84 @@ struct Columns {
     f32x4_t o[NT][NJ];
     float m[NT], l[NT];    // maximum so far, in units of log2 e / scale; this lane's share of the sum
 
-    // One record.  MASKED: row nt of this lane sees keys [lo[nt], hi[nt]) alone, the request has keys up to `end`; tok: the record's first token.
-    template <bool MASKED>
-    __device__ __forceinline__ void step(Record<D> &r, int n_cols, float c, int tok, const int *lo, const int *hi, int end, int lane)
+    // One record.  masked: row nt of this lane sees keys [lo[nt], hi[nt]) alone, the request has keys up to `end`; tok: the record's first
+    // token.
+    __device__ __forceinline__ void step(Record<D> &r, int n_cols, float c, int tok, bool masked, const int *lo, const int *hi, int end, int lane)
     {
         const int g = lane >> 4;
-        f32x4_t s[NT][4];
+        bf16x8_t k[4][KD];   // (one column: each is needed once and decoded where it is)
+        auto decode = [&](int i) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bf16x8_t a[KD];
+            for (int j = 0; j < KD; ++j) k[i][j] = __builtin_bit_cast(bf16x8_t, mx4_decode(r.k[i][j], mx4_scale(r.ks[j / 4], i)));
+        };
+        if constexpr (NT > 1) {
 #pragma unroll
-            for (int j = 0; j < KD; ++j)
-                a[j] = __builtin_bit_cast(bf16x8_t, mx4_decode(r.k[i][j], mx4_scale(r.ks[j / 4], i)));
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                if (nt > 0 && nt >= n_cols) continue;
-                s[nt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < KD; ++j) s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[j], q[nt][j], s[nt][i], 0, 0, 0);
-            }
+            for (int i = 0; i < 4; ++i) decode(i);
         }
-        uint32_t p_hi[NT][4][2], p_lo[NT][4][2];   // [tile][keys 0 1, 2 3]
+        constexpr int NP = Y32 ? 3 : 1;
+        uint32_t p[NP][NT][4][2];   // the weights as a sum of NP bf16: [tile][keys 0 1, 2 3]
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             if (nt > 0 && nt >= n_cols) continue;
-            if constexpr (MASKED) {
+            f32x4_t s[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (NT == 1) decode(i);
+                s[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < KD; ++j) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], q[nt][j], s[i], 0, 0, 0);
+            }
+            if (masked) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = tok + i * 16 + g * 4 + e;
-                        s[nt][i][e] = key >= lo[nt] && key < hi[nt] ? s[nt][i][e] : NEG_INF;
+                        s[i][e] = key >= lo[nt] && key < hi[nt] ? s[i][e] : NEG_INF;
                     }
             }
             float top = m[nt];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, fmaxf(s[nt][i][0], s[nt][i][1])), fmaxf(s[nt][i][2], s[nt][i][3]));
+            for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, fmaxf(s[i][0], s[i][1])), fmaxf(s[i][2], s[i][3]));
             top = max4(top);
             // (nothing seen so far: any finite number will do as the maximum)
             const float base = top == NEG_INF ? 0.f : top * c;
-            const float shrink = __builtin_amdgcn_exp2f(fmaf(m[nt], c, -base));   // exp2(-inf) = 0 for the first keys
-            m[nt] = top;
+            if (__ballot(top > m[nt])) {   // (rare after the first records)
+                const float shrink = __builtin_amdgcn_exp2f(fmaf(m[nt], c, -base));   // exp2(-inf) = 0 for the first keys
+                l[nt] *= shrink;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) o[nt][j] *= shrink;
+                m[nt] = top;
+            }
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    w[e] = __builtin_amdgcn_exp2f(fmaf(s[nt][i][e], c, -base));
+                    w[e] = __builtin_amdgcn_exp2f(fmaf(s[i][e], c, -base));
                     sum += w[e];
                 }
-                p_hi[nt][i][0] = pack_bf16x2(w[0], w[1]);
-                p_hi[nt][i][1] = pack_bf16x2(w[2], w[3]);
-                if constexpr (Y32) {
-                    p_lo[nt][i][0] = pack_bf16x2(w[0] - bits_f32(p_hi[nt][i][0] << 16), w[1] - bits_f32(p_hi[nt][i][0] & 0xFFFF0000u));
-                    p_lo[nt][i][1] = pack_bf16x2(w[2] - bits_f32(p_hi[nt][i][1] << 16), w[3] - bits_f32(p_hi[nt][i][1] & 0xFFFF0000u));
+#pragma unroll
+                for (int u = 0; u < NP; ++u) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t hi2 = pack_bf16x2(w[2 * h], w[2 * h + 1]);
+                        p[u][nt][i][h] = hi2;
+                        w[2 * h] -= bits_f32(hi2 << 16);
+                        w[2 * h + 1] -= bits_f32(hi2 & 0xFFFF0000u);
+                    }
                 }
             }
-            l[nt] = fmaf(l[nt], shrink, sum);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) o[nt][j] *= shrink;
+            l[nt] += sum;
         }
-        if constexpr (MASKED) mask_values(r, n_cols, tok, lo, hi, end, lane);
+        if (masked) mask_values(r, n_cols, tok, lo, hi, end, lane);
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-            bf16x8_t ph[NT], pl[NT];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                if (nt > 0 && nt >= n_cols) continue;
-                ph[nt] = operand(p_hi[nt][2 * a][0], p_hi[nt][2 * a][1], p_hi[nt][2 * a + 1][0], p_hi[nt][2 * a + 1][1]);
-                if constexpr (Y32)
-                    pl[nt] = operand(p_lo[nt][2 * a][0], p_lo[nt][2 * a][1], p_lo[nt][2 * a + 1][0], p_lo[nt][2 * a + 1][1]);
-            }
 #pragma unroll
             for (int b = 0; b < SB; ++b) {
-                constexpr int NP = D == 64 ? 2 : 4;   // pairs of channels of a word
-                uint32_t x[8][NP];                    // [key][pair]
+                constexpr int PAIRS = D == 64 ? 2 : 4;   // pairs of channels of a word
+                uint32_t x[8][PAIRS];                    // [key][pair]
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int i = 2 * a + e / 4;
@@ -209,18 +214,18 @@ struct Columns {
                     }
                 }
 #pragma unroll
-                for (int p = 0; p < NP; ++p) {
-                    const bf16x8_t even = operand(lows(x[0][p], x[1][p]), lows(x[2][p], x[3][p]), lows(x[4][p], x[5][p]), lows(x[6][p], x[7][p]));
-                    const bf16x8_t odd = operand(highs(x[0][p], x[1][p]), highs(x[2][p], x[3][p]), highs(x[4][p], x[5][p]), highs(x[6][p], x[7][p]));
-                    const int j = b * 8 + 2 * p;
+                for (int u = 0; u < PAIRS; ++u) {
+                    const bf16x8_t even = operand(lows(x[0][u], x[1][u]), lows(x[2][u], x[3][u]), lows(x[4][u], x[5][u]), lows(x[6][u], x[7][u]));
+                    const bf16x8_t odd = operand(highs(x[0][u], x[1][u]), highs(x[2][u], x[3][u]), highs(x[4][u], x[5][u]), highs(x[6][u], x[7][u]));
+                    const int j = b * 8 + 2 * u;
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         if (nt > 0 && nt >= n_cols) continue;
-                        o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, ph[nt], o[nt][j], 0, 0, 0);
-                        o[nt][j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, ph[nt], o[nt][j + 1], 0, 0, 0);
-                        if constexpr (Y32) {
-                            o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pl[nt], o[nt][j], 0, 0, 0);
-                            o[nt][j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pl[nt], o[nt][j + 1], 0, 0, 0);
+#pragma unroll
+                        for (int z = 0; z < NP; ++z) {
+                            const bf16x8_t pz = operand(p[z][nt][2 * a][0], p[z][nt][2 * a][1], p[z][nt][2 * a + 1][0], p[z][nt][2 * a + 1][1]);
+                            o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pz, o[nt][j], 0, 0, 0);
+                            o[nt][j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pz, o[nt][j + 1], 0, 0, 0);
                         }
                     }
                 }
@@ -285,7 +290,6 @@ struct AttendK {
     KvPlanView v;
     AttendArgs a;
     int list;              // 0: the tiles of few rows, 1: the others
-    int bound;             // records of the launch's list at most
 };
 
 // Output row of the request's tokens: group rows of a token are query heads of the kv head.
@@ -295,8 +299,16 @@ __device__ __forceinline__ int64_t y_row(const KvTile &t, int row, int group, in
     return ((int64_t)t.tok0 + i) * (n_kv * group) + h * group + (row - i * group);
 }
 
-__device__ __forceinline__ void put_agent(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ float get_agent(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+// Partial results cross from one XCD's L2 to another's: device-scope accesses, two floats each (p 8-byte aligned).
+__device__ __forceinline__ void put_agent(float *p, float a, float b)
+{
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(p), (uint64_t)f32_bits(b) << 32 | f32_bits(a), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_agent(const float *p)
+{
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t *>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(bits_f32((uint32_t)v), bits_f32((uint32_t)(v >> 32)));
+}
 
 template <int N>
 __device__ __forceinline__ void store_y(const AttendArgs &a, int64_t row, int D, int ch, const float (&x)[N])
@@ -315,21 +327,33 @@ __device__ __forceinline__ void store_y(const AttendArgs &a, int64_t row, int D,
 
 constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
 
-// SPLIT: the four waves share the tile's 16 NT rows and take its records in turn.  Otherwise each has 16 NT rows of its own.
-template <int D, int NT, bool Y32, bool SPLIT>
-__global__ __launch_bounds__(256) void attend_kernel(AttendK p)
+// Waves per SIMD that the registers are to leave room for.
+template <int D, int NT>
+constexpr int min_waves()
 {
-    constexpr int ROWS = SPLIT ? 16 * NT : 64 * NT, CH = D / 16;   // CH: channels of a row per thread in the joins
+    return NT > 1 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : D == 128 ? 2 : 1;
+}
+
+// CW groups of KW waves; a group has 16 NT rows of the tile, its waves take the records in turn.
+template <int D, int NT, int CW, int KW, bool Y32>
+__global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_kernel(AttendK p)
+{
+    constexpr bool SPLIT = KW > 1;
+    constexpr int ROWS = 16 * NT * CW, CH = D / 16;   // CH: channels of a row per thread in the joins
     constexpr int LDO = D + 4;
-    __shared__ float lds_o[SPLIT ? 4 : 1][16][LDO];
-    __shared__ float lds_ml[4][16][2];
+    __shared__ float lds_o[SPLIT ? KW : 1][16][LDO];
+    __shared__ float lds_ml[KW][16][2];
     __shared__ int lds_last;
     const KvPlanView &v = p.v;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kw = wave % KW, cw = wave / KW, n = lane & 15, g = lane >> 4;
     const int rec_id = blockIdx.x / v.n_kv, h = blockIdx.x - rec_id * v.n_kv;
+    KvTile t = (p.list ? v.tile : v.few)[rec_id];   // (beside the list's length, not after it)
     if (rec_id >= v.head[p.list]) return;
-    const KvTile t = (p.list ? v.tile : v.few)[rec_id];
     const int group = v.group, rows = t.n_tok * group, pos0 = t.kv_len - t.n_tok;
+    // (a tile of the plan may be several workgroups', of ROWS rows each)
+    const int sub = blockIdx.y;
+    t.row0 += sub * ROWS;
+    if (t.row0 >= rows) return;
     const int row_end = min(rows, t.row0 + ROWS);
     // positions of the tile's first and last token
     const int first = pos0 + t.row0 / group, last = pos0 + (row_end - 1) / group;
@@ -339,7 +363,7 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK p)
     const int b0 = b_lo + (int)((int64_t)n_blocks * t.part / t.n_parts), b1 = b_lo + (int)((int64_t)n_blocks * (t.part + 1) / t.n_parts);
 
     Columns<D, NT, Y32> w;
-    const int wrow0 = SPLIT ? t.row0 : t.row0 + wave * 16 * NT;
+    const int wrow0 = t.row0 + cw * 16 * NT;
     const int n_cols = max(0, min(NT, (row_end - wrow0 + 15) >> 4));
     int lo[NT], hi[NT];
 #pragma unroll
@@ -366,30 +390,44 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK p)
     const int lb = p.a.pages.log_blocks;
     const int64_t page_bytes = p.a.pages.page_bytes();
     const char *heads = p.a.pages.data + (((int64_t)h * kv_record_bytes(D)) << lb);
-    constexpr int STEP = SPLIT ? 4 : 1;
-    auto page_of = [&](int b) { return uniform(table[min(b, b1 - 1) >> lb]); };
+    constexpr int STEP = KW;
     auto record_of = [&](int b, int page) {
         return heads + (int64_t)page * page_bytes + (b & ((1 << lb) - 1)) * kv_record_bytes(D);
     };
-    const int first_b = b0 + (SPLIT ? wave : 0);
+    const int n_pages = p.a.pages.n_pages, first_b = b0 + kw;
     if (first_b < b1 && n_cols > 0) {
-        Record<D> cur, nxt;
-        int page = page_of(first_b), page_next = page_of(first_b + STEP);
-        bool ok = page >= 0 && page < p.a.pages.n_pages;
-        load_record<D>(cur, record_of(first_b, ok ? page : 0), lane);
-        bool bad = !ok;
-        for (int b = first_b; b < b1; b += STEP) {
-            const bool ok_next = page_next >= 0 && page_next < p.a.pages.n_pages;
-            load_record<D>(nxt, record_of(min(b + STEP, b1 - 1), ok_next ? page_next : 0), lane);
-            page_next = page_of(b + 2 * STEP);
-            const int tok = b * 64;
-            if (ok) {
-                if (tok >= last - window + 1 && tok + 63 <= first) w.template step<false>(cur, n_cols, c, tok, lo, hi, t.kv_len, lane);
-                else w.template step<true>(cur, n_cols, c, tok, lo, hi, t.kv_len, lane);
+        Record<D> r0, r1;
+        const Places<D> at(lane);
+        bool bad = false;
+        // 64 records of the wave at a time, whose pages lie one to a lane: a read of the table among the loads below would have to wait for
+        // every load that is on its way ahead of it.
+        for (int c0 = first_b; c0 < b1; c0 += 64 * STEP) {
+            const int pages = table[min(c0 + lane * STEP, b1 - 1) >> lb];
+            // Starts the loads of record b, the i-th of the 64; whether its page exists.
+            auto start = [&](Record<D> &r, int i, int b) {
+                const int page = __builtin_amdgcn_readlane(pages, i);
+                const bool ok = page >= 0 && page < n_pages;
+                load_record<D>(r, record_of(min(b, b1 - 1), ok ? page : 0), at);
+                bad |= !ok;
+                return ok;
+            };
+            auto take = [&](Record<D> &r, int b, bool ok) {
+                const int tok = b * 64;
+                const bool whole = tok >= last - window + 1 && tok + 63 <= first;
+                if (ok) w.step(r, n_cols, c, tok, !whole, lo, hi, t.kv_len, lane);
+            };
+            const int count = min(64, (b1 - c0 + STEP - 1) / STEP);
+            bool ok0 = start(r0, 0, c0), ok1;
+            for (int i = 0, b = c0;;) {
+                ok1 = start(r1, min(i + 1, count - 1), b + STEP);
+                take(r0, b, ok0);
+                b += STEP;
+                if (++i >= count) break;
+                ok0 = start(r0, min(i + 1, count - 1), b + STEP);
+                take(r1, b, ok1);
+                b += STEP;
+                if (++i >= count) break;
             }
-            cur = nxt;
-            ok = ok_next;
-            bad |= b + STEP < b1 && !ok;
         }
         if (bad && lane == 0) atomicOr(p.a.err_word, ERR_BAD_PAGE);
     }
@@ -397,41 +435,42 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK p)
     for (int nt = 0; nt < NT; ++nt) w.l[nt] = sum4(w.l[nt]);
 
     const int ps = t.pslot + t.part;
-    float *part_o = p.a.partial + ((int64_t)ps * v.n_kv + h) * KV_TILE_ROWS * (D + 2);
+    float *part_o = p.a.partial + (((int64_t)ps * v.n_kv + h) * KV_TILE_ROWS + sub * ROWS) * (D + 2);
     const bool whole = t.n_parts == 1;
     if constexpr (SPLIT) {
         const int row = tid >> 4, ch = (tid & 15) * CH;
-        for (int nt = 0; nt < NT; ++nt) {
-            if (nt * 16 >= row_end - t.row0) break;
-            if (nt) __syncthreads();
+        for (int ct = 0; ct < CW * NT; ++ct) {
+            if (ct * 16 >= row_end - t.row0) break;
+            if (ct) __syncthreads();
 #pragma unroll
-            for (int k = 0; k < NT; ++k)
-                if (k == nt) {
+            for (int nt = 0; nt < NT; ++nt)
+                if (cw * NT + nt == ct) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
                         for (int j = 0; j < D / 16; ++j)
-                            lds_o[wave][n][o_channel<D>(g * 4 + e) + (D == 256 ? (j >> 3) * 128 + (j & 7) : j)] = w.o[k][j][e];
+                            lds_o[kw][n][o_channel<D>(g * 4 + e) + (D == 256 ? (j >> 3) * 128 + (j & 7) : j)] = w.o[nt][j][e];
                     if (g == 0) {
-                        lds_ml[wave][n][0] = w.m[k];
-                        lds_ml[wave][n][1] = w.l[k];
+                        lds_ml[kw][n][0] = w.m[nt];
+                        lds_ml[kw][n][1] = w.l[nt];
                     }
                 }
             __syncthreads();
+            if (tid >= 256) continue;
             float m = NEG_INF, l = 0.f, x[CH];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) m = fmaxf(m, lds_ml[u][row][0]);
+            for (int u = 0; u < KW; ++u) m = fmaxf(m, lds_ml[u][row][0]);
 #pragma unroll
             for (int i = 0; i < CH; ++i) x[i] = 0.f;
             const float base = m == NEG_INF ? 0.f : m * c;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < KW; ++u) {
                 const float f = __builtin_amdgcn_exp2f(fmaf(lds_ml[u][row][0], c, -base));
                 l = fmaf(lds_ml[u][row][1], f, l);
 #pragma unroll
                 for (int i = 0; i < CH; ++i) x[i] = fmaf(lds_o[u][row][ch + i], f, x[i]);
             }
-            const int r = t.row0 + nt * 16 + row;
+            const int r = t.row0 + ct * 16 + row;
             if (r >= row_end) continue;
             if (whole) {
                 const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
@@ -441,19 +480,16 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK p)
                 store_y(p.a, at, D, ch, x);
                 if (p.a.lse && ch == 0) p.a.lse[at] = l > 0.f || l != l ? (m * c + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
             } else {
-                float *o = part_o + (nt * 16 + row) * (D + 2);
+                float *o = part_o + (ct * 16 + row) * (D + 2);
 #pragma unroll
-                for (int i = 0; i < CH; ++i) put_agent(o + 2 + ch + i, x[i]);
-                if (ch == 0) {
-                    put_agent(o, m);
-                    put_agent(o + 1, l);
-                }
+                for (int i = 0; i < CH; i += 2) put_agent(o + 2 + ch + i, x[i], x[i + 1]);
+                if (ch == 0) put_agent(o, m, l);
             }
         }
     } else {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int local = wave * 16 * NT + nt * 16 + n, r = t.row0 + local;
+            const int local = cw * 16 * NT + nt * 16 + n, r = t.row0 + local;
             if (r >= row_end) continue;
             const float l = w.l[nt], inv = whole ? (l > 0.f || l != l ? 1.f / l : 0.f) : 1.f;
             const int64_t at = y_row(t, r, group, v.n_kv, h);
@@ -470,13 +506,12 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK p)
                     if (whole) store_y(p.a, at, D, ch, x);
                     else
 #pragma unroll
-                        for (int j = 0; j < N; ++j) put_agent(o + 2 + ch + j, x[j]);
+                        for (int j = 0; j < N; j += 2) put_agent(o + 2 + ch + j, x[j], x[j + 1]);
                 }
             }
             if (g == 0) {
                 if (!whole) {
-                    put_agent(o, w.m[nt]);
-                    put_agent(o + 1, l);
+                    put_agent(o, w.m[nt], l);
                 } else if (p.a.lse) {
                     p.a.lse[at] = l > 0.f || l != l ? (w.m[nt] * c + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
                 }
@@ -488,7 +523,7 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK p)
     // workgroup waits for its own before it reports, and nobody's L2 has to be written back.
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    int *ticket = v.tickets + (int64_t)t.pslot * v.n_kv + h;
+    int *ticket = v.tickets + (int64_t)(t.pslot + sub) * v.n_kv + h;   // (two parts or more: as many places)
     if (tid == 0) {
         lds_last = atomicAdd(ticket, 1) == t.n_parts - 1;
         if (lds_last) *ticket = 0;   // clean for the next call
@@ -496,21 +531,57 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK p)
     __syncthreads();
     if (!lds_last) return;
     const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
-    const float *first_part = p.a.partial + ((int64_t)t.pslot * v.n_kv + h) * KV_TILE_ROWS * (D + 2);
+    const float *first_part = p.a.partial + (((int64_t)t.pslot * v.n_kv + h) * KV_TILE_ROWS + sub * ROWS) * (D + 2);
+    // 16 rows at a time: the factors of their parts into LDS (16 threads a row, each several parts), then the rows, four parts'
+    // loads at a time.
+    constexpr int THREADS = 64 * CW * KW;
+    static_assert(THREADS == 256, "the join's threads: 16 rows of 16");
+    __shared__ float factor[16][KV_MAX_PARTS + 1];
+    const int row = tid >> 4, sl = tid & 15;
     for (int r0 = 0; r0 < row_end - t.row0; r0 += 16) {
-        const int local = r0 + (tid >> 4), ch = (tid & 15) * CH;
-        if (t.row0 + local >= row_end) continue;
-        const float *o = first_part + local * (D + 2);
+        const int local = r0 + row, ch = sl * CH;
+        const bool real = t.row0 + local < row_end;
+        const float *o = first_part + (real ? local : 0) * (D + 2);
         float m = NEG_INF, l = 0.f, x[CH];
-        for (int u = 0; u < t.n_parts; ++u) m = fmaxf(m, get_agent(o + u * part_step));
+        float2 ml[KV_MAX_PARTS / 16];
+#pragma unroll
+        for (int u = 0; u < KV_MAX_PARTS / 16; ++u)
+            ml[u] = u * 16 + sl < t.n_parts ? get_agent(o + (u * 16 + sl) * part_step) : make_float2(NEG_INF, 0.f);
+#pragma unroll
+        for (int u = 0; u < KV_MAX_PARTS / 16; ++u) m = fmaxf(m, ml[u].x);
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+        const float base = m == NEG_INF ? 0.f : m * c;
+        if (r0) lds_barrier();
+#pragma unroll
+        for (int u = 0; u < KV_MAX_PARTS / 16; ++u) {
+            const float f = __builtin_amdgcn_exp2f(fmaf(ml[u].x, c, -base));
+            factor[row][u * 16 + sl] = f;
+            l = fmaf(ml[u].y, f, l);
+        }
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) l += __shfl_xor(l, d);
+        lds_barrier();
+        if (!real) continue;
 #pragma unroll
         for (int i = 0; i < CH; ++i) x[i] = 0.f;
-        const float base = m == NEG_INF ? 0.f : m * c;
-        for (int u = 0; u < t.n_parts; ++u) {
-            const float f = __builtin_amdgcn_exp2f(fmaf(get_agent(o + u * part_step), c, -base));
-            l = fmaf(get_agent(o + u * part_step + 1), f, l);
+        o += 2 + ch;
+        for (int u0 = 0; u0 < t.n_parts; u0 += 4) {
+            float2 v4[4][CH / 2];
 #pragma unroll
-            for (int i = 0; i < CH; ++i) x[i] = fmaf(get_agent(o + u * part_step + 2 + ch + i), f, x[i]);
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < CH / 2; ++i) v4[u][i] = get_agent(o + min(u0 + u, t.n_parts - 1) * part_step + 2 * i);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (u0 + u >= t.n_parts) break;
+                const float f = factor[row][u0 + u];
+#pragma unroll
+                for (int i = 0; i < CH / 2; ++i) {
+                    x[2 * i] = fmaf(v4[u][i].x, f, x[2 * i]);
+                    x[2 * i + 1] = fmaf(v4[u][i].y, f, x[2 * i + 1]);
+                }
+            }
         }
         const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll
@@ -521,22 +592,27 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendK p)
     }
 }
 
+template <int D, int NT, int CW, int KW, bool Y32>
+void launch_as(const AttendK &p, int records, int rows, hipStream_t stream)
+{
+    constexpr int ROWS = 16 * NT * CW;
+    static_assert(KV_TILE_ROWS / ROWS <= 2 || KW > 1, "workgroups of a tile");
+    hipLaunchKernelGGL((attend_kernel<D, NT, CW, KW, Y32>), dim3((unsigned)records * p.v.n_kv, (unsigned)(rows / ROWS)), dim3(64 * CW * KW), 0,
+                       stream, p);
+}
+
 template <int D, bool Y32>
 hipError_t launch_d(const KvPlanView &v, const AttendArgs &a, hipStream_t stream)
 {
-    AttendK p{v, a, 0, 0};
+    constexpr bool WIDE = D == 256;   // two columns of accumulators would leave no registers for the rest
+    AttendK p{v, a, 0};
     if (v.has_few) {
-        p.bound = v.max_few;
-        const dim3 grid((unsigned)v.max_few * v.n_kv);
-        if (std::min(v.max_new * (int64_t)v.group, (int64_t)KV_FEW_ROWS) <= 16)
-            hipLaunchKernelGGL((attend_kernel<D, 1, Y32, true>), grid, dim3(256), 0, stream, p);
-        else
-            hipLaunchKernelGGL((attend_kernel<D, 2, Y32, true>), grid, dim3(256), 0, stream, p);
+        if (std::min(v.max_new * (int64_t)v.group, (int64_t)KV_FEW_ROWS) <= 16) launch_as<D, 1, 1, 4, Y32>(p, v.max_few, 16, stream);
+        else launch_as<D, WIDE ? 1 : 2, WIDE ? 2 : 1, WIDE ? 2 : 4, Y32>(p, v.max_few, KV_FEW_ROWS, stream);
     }
     if (v.has_tile) {
         p.list = 1;
-        p.bound = v.max_tile;
-        hipLaunchKernelGGL((attend_kernel<D, 2, Y32, false>), dim3((unsigned)v.max_tile * v.n_kv), dim3(256), 0, stream, p);
+        launch_as<D, WIDE ? 1 : 2, 4, 1, Y32>(p, v.max_tile, KV_TILE_ROWS, stream);
     }
     return hipGetLastError();
 }

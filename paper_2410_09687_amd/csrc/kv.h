@@ -32,8 +32,9 @@ struct KvPages {
 constexpr int KV_FEW_ROWS = 32, KV_TILE_ROWS = 128;
 constexpr int KV_FEW_TOKENS = 8;   // up to here (new tokens of a request) the plan is one launch
 // Workgroups aimed at per launch where the keys allow, and the fewest records of a part.
-constexpr int KV_FEW_TARGET = 1024, KV_FEW_MIN = 4;
+constexpr int KV_FEW_TARGET = 512, KV_FEW_MIN = 4;
 constexpr int KV_TILE_TARGET = 512, KV_TILE_MIN = 8;
+constexpr int KV_MAX_PARTS = 128;  // of a tile
 
 struct KvTile {            // one workgroup's work, per kv head
     int tok0, n_tok;       // the request's tokens in the batch

@@ -169,7 +169,7 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
         const int blocks = ceil_shift(L, 6);
         const int n_tiles = tiled ? (int)((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS) : few ? 1 : 0;
         const int chunk = tiled ? tile_chunk : few_chunk;
-        const int parts = max(1, (blocks + chunk - 1) / chunk);
+        const int parts = min(KV_MAX_PARTS, max(1, (blocks + chunk - 1) / chunk));
         const int recs = n_tiles * parts;
         const int ps = parts > 1 ? recs : 0;
         const Scan2 up = block_scan(Scan2{((long long)(tiled ? recs : 0) << 32) | (unsigned)(few ? recs : 0), ps}, lds, t2);
