@@ -601,7 +601,7 @@ int64_t moin_kv_page_bytes(int32_t page_tokens, int32_t n_kv, int32_t head_dim);
  * The plan serves one stream at a time.  Grows like moin_plan ("HIP graphs" above): a build for the
  * largest S, T and max_new prepares captured ones only of the same sizes or fewer requests and tokens.
  * Errors: MOIN_EINVAL (null, negative or unsupported sizes, T * n_heads / n_kv or
- * S * max_pages at 2^31 and more), MOIN_ENOMEM, MOIN_ECAPTURE. */
+ * S * max_pages * page_tokens / 64 at 2^31 and more), MOIN_ENOMEM, MOIN_ECAPTURE. */
 typedef struct moin_kv_plan moin_kv_plan;
 int moin_kv_plan_create(moin_ctx *ctx, moin_kv_plan **out);
 void moin_kv_plan_destroy(moin_kv_plan *plan);

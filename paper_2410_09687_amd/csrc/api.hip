@@ -1696,7 +1696,8 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
         plan->built = 1;
         return MOIN_OK;
     }
-    if (max_pages < 1 || (int64_t)S * max_pages > 0x7fffffffLL || (int64_t)max_pages * page_tokens > 0x7fffffffLL) return MOIN_EINVAL;
+    if (max_pages < 1 || (int64_t)S * max_pages * (page_tokens / KV_BLOCK) > 0x7fffffffLL || (int64_t)max_pages * page_tokens > 0x7fffffffLL)
+        return MOIN_EINVAL;
     if (!kv_lens || !new_lens || !block_table || (!free_pages && free_cap > 0) || !n_free || !n_free_out || !kv_lens_out || !seq_offsets ||
         (!slots && T > 0))
         return MOIN_EINVAL;

@@ -327,7 +327,12 @@ __device__ __forceinline__ void store_y(const AttendArgs &a, int64_t row, int D,
 
 constexpr float LN2 = 0.69314718055994530942f, LOG2E = 1.44269504088896340736f;
 
-// Waves per SIMD that the registers are to leave room for.
+// (a row that saw nothing has a sum of zero; NaN stays)
+__device__ __forceinline__ float inverse(float l) { return l == 0.f ? 0.f : 1.f / l; }
+__device__ __forceinline__ float log_sum(float m, float l, float c) { return l == 0.f ? NEG_INF : (m * c + __builtin_amdgcn_logf(l)) * LN2; }
+
+// Waves per SIMD that the registers are to leave room for.  (D = 64: four spill, 43 -> 55 us for 256 requests; D = 128: three spill,
+// 65 -> 80 us for two long ones.)
 template <int D, int NT>
 constexpr int min_waves()
 {
@@ -347,8 +352,10 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_ker
     const KvPlanView &v = p.v;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kw = wave % KW, cw = wave / KW, n = lane & 15, g = lane >> 4;
     const int rec_id = blockIdx.x / v.n_kv, h = blockIdx.x - rec_id * v.n_kv;
-    KvTile t = (p.list ? v.tile : v.few)[rec_id];   // (beside the list's length, not after it)
+    const int4 *line = reinterpret_cast<const int4 *>((p.list ? v.tile : v.few) + rec_id);
+    const int4 ta = line[0], tb = line[1];   // (beside the list's length, not after it)
     if (rec_id >= v.head[p.list]) return;
+    KvTile t{uniform(ta.x), uniform(ta.y), uniform(ta.z), uniform(ta.w), uniform(tb.x), uniform(tb.y), uniform(tb.z), uniform(tb.w)};
     const int group = v.group, rows = t.n_tok * group, pos0 = t.kv_len - t.n_tok;
     // (a tile of the plan may be several workgroups', of ROWS rows each)
     const int sub = blockIdx.y;
@@ -473,12 +480,12 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_ker
             const int r = t.row0 + ct * 16 + row;
             if (r >= row_end) continue;
             if (whole) {
-                const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+                const float inv = inverse(l);
 #pragma unroll
                 for (int i = 0; i < CH; ++i) x[i] *= inv;
                 const int64_t at = y_row(t, r, group, v.n_kv, h);
                 store_y(p.a, at, D, ch, x);
-                if (p.a.lse && ch == 0) p.a.lse[at] = l > 0.f || l != l ? (m * c + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
+                if (p.a.lse && ch == 0) p.a.lse[at] = log_sum(m, l, c);
             } else {
                 float *o = part_o + (ct * 16 + row) * (D + 2);
 #pragma unroll
@@ -491,7 +498,7 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_ker
         for (int nt = 0; nt < NT; ++nt) {
             const int local = cw * 16 * NT + nt * 16 + n, r = t.row0 + local;
             if (r >= row_end) continue;
-            const float l = w.l[nt], inv = whole ? (l > 0.f || l != l ? 1.f / l : 0.f) : 1.f;
+            const float l = w.l[nt], inv = whole ? (inverse(l)) : 1.f;
             const int64_t at = y_row(t, r, group, v.n_kv, h);
             float *o = part_o + local * (D + 2);
 #pragma unroll
@@ -513,7 +520,7 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_ker
                 if (!whole) {
                     put_agent(o, w.m[nt], l);
                 } else if (p.a.lse) {
-                    p.a.lse[at] = l > 0.f || l != l ? (w.m[nt] * c + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
+                    p.a.lse[at] = log_sum(w.m[nt], l, c);
                 }
             }
         }
@@ -532,7 +539,7 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_ker
     if (!lds_last) return;
     const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
     const float *first_part = p.a.partial + (((int64_t)t.pslot * v.n_kv + h) * KV_TILE_ROWS + sub * ROWS) * (D + 2);
-    // 16 rows at a time: the factors of their parts into LDS (16 threads a row, each several parts), then the rows, four parts'
+    // 16 rows at a time: the factors of their parts into LDS (16 threads a row, each several parts), then the rows, several parts'
     // loads at a time.
     constexpr int THREADS = 64 * CW * KW;
     static_assert(THREADS == 256, "the join's threads: 16 rows of 16");
@@ -543,21 +550,16 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_ker
         const bool real = t.row0 + local < row_end;
         const float *o = first_part + (real ? local : 0) * (D + 2);
         float m = NEG_INF, l = 0.f, x[CH];
-        float2 ml[KV_MAX_PARTS / 16];
-#pragma unroll
-        for (int u = 0; u < KV_MAX_PARTS / 16; ++u)
-            ml[u] = u * 16 + sl < t.n_parts ? get_agent(o + (u * 16 + sl) * part_step) : make_float2(NEG_INF, 0.f);
-#pragma unroll
-        for (int u = 0; u < KV_MAX_PARTS / 16; ++u) m = fmaxf(m, ml[u].x);
+        for (int u = sl; u < t.n_parts; u += 16) m = fmaxf(m, get_agent(o + u * part_step).x);
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
         const float base = m == NEG_INF ? 0.f : m * c;
         if (r0) lds_barrier();
-#pragma unroll
-        for (int u = 0; u < KV_MAX_PARTS / 16; ++u) {
-            const float f = __builtin_amdgcn_exp2f(fmaf(ml[u].x, c, -base));
-            factor[row][u * 16 + sl] = f;
-            l = fmaf(ml[u].y, f, l);
+        for (int u = sl; u < t.n_parts; u += 16) {
+            const float2 ml = get_agent(o + u * part_step);
+            const float f = __builtin_amdgcn_exp2f(fmaf(ml.x, c, -base));
+            factor[row][u] = f;
+            l = fmaf(ml.y, f, l);
         }
 #pragma unroll
         for (int d = 1; d < 16; d <<= 1) l += __shfl_xor(l, d);
@@ -566,29 +568,30 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_ker
 #pragma unroll
         for (int i = 0; i < CH; ++i) x[i] = 0.f;
         o += 2 + ch;
-        for (int u0 = 0; u0 < t.n_parts; u0 += 4) {
-            float2 v4[4][CH / 2];
+        constexpr int AHEAD = 64 / CH;   // parts whose loads are on their way together
+        for (int u0 = 0; u0 < t.n_parts; u0 += AHEAD) {
+            float2 ahead[AHEAD][CH / 2];
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-                for (int i = 0; i < CH / 2; ++i) v4[u][i] = get_agent(o + min(u0 + u, t.n_parts - 1) * part_step + 2 * i);
+                for (int i = 0; i < CH / 2; ++i)
+                    ahead[u][i] = u0 + u < t.n_parts ? get_agent(o + (u0 + u) * part_step + 2 * i) : make_float2(0.f, 0.f);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                if (u0 + u >= t.n_parts) break;
-                const float f = factor[row][u0 + u];
+            for (int u = 0; u < AHEAD; ++u) {
+                const float f = u0 + u < t.n_parts ? factor[row][u0 + u] : 0.f;
 #pragma unroll
                 for (int i = 0; i < CH / 2; ++i) {
-                    x[2 * i] = fmaf(v4[u][i].x, f, x[2 * i]);
-                    x[2 * i + 1] = fmaf(v4[u][i].y, f, x[2 * i + 1]);
+                    x[2 * i] = fmaf(ahead[u][i].x, f, x[2 * i]);
+                    x[2 * i + 1] = fmaf(ahead[u][i].y, f, x[2 * i + 1]);
                 }
             }
         }
-        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+        const float inv = inverse(l);
 #pragma unroll
         for (int i = 0; i < CH; ++i) x[i] *= inv;
         const int64_t at = y_row(t, t.row0 + local, group, v.n_kv, h);
         store_y(p.a, at, D, ch, x);
-        if (p.a.lse && ch == 0) p.a.lse[at] = l > 0.f || l != l ? (m * c + __builtin_amdgcn_logf(l)) * LN2 : NEG_INF;
+        if (p.a.lse && ch == 0) p.a.lse[at] = log_sum(m, l, c);
     }
 }
 

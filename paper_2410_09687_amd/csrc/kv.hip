@@ -153,48 +153,75 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
     const int few_goal = max(1, KV_FEW_TARGET / v.n_kv), tile_goal = max(1, KV_TILE_TARGET / v.n_kv);
     const int few_chunk = (int)max((long long)KV_FEW_MIN, (few_all + few_goal - 1) / few_goal);
     const int tile_chunk = (int)max((long long)KV_TILE_MIN, (tile_all + tile_goal - 1) / tile_goal);
-    int few_base = 0, tile_base = 0, ps_base = 0;
+    // Tiles of few rows are listed by the length of their parts, longest first (in 64 steps; who is first in a step is left to chance and
+    // shows in no result): the last workgroups to begin are then short ones.
+    __shared__ int place[64];
+    if (tid < 64) place[tid] = 0;
+    lds_barrier();
+    auto work_of = [&](int s, int &tok0, int &n, int &L) {   // (what this thread wrote in the first walk)
+        const int4 q = v.req[s];
+        tok0 = a.seq_offsets[s];
+        n = q.w;
+        L = q.y >= 0 ? q.x + n : 0;
+    };
+    auto parts_of = [&](int L, int size) { return min(KV_MAX_PARTS, max(1, (ceil_shift(L, 6) + size - 1) / size)); };
+    auto step_of = [&](int L, int parts) { return 63 - min(63, (ceil_shift(L, 6) + parts - 1) / parts * 63 / few_chunk); };
+    auto is_few = [&](int n) { return n > 0 && (int64_t)n * v.group <= KV_FEW_ROWS; };
+    if (v.has_few) {
+        for (int s = tid; s < v.S; s += KV_PLAN_THREADS) {
+            int tok0, n, L;
+            work_of(s, tok0, n, L);
+            if (!is_few(n)) continue;
+            const int parts = parts_of(L, few_chunk);
+            atomicAdd(&place[step_of(L, parts)], parts);
+        }
+        lds_barrier();
+        if (tid < 64) {
+            const int own = place[tid];
+            int up = own;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int x = __shfl_up(up, d);
+                if (tid >= d) up += x;
+            }
+            place[tid] = up - own;
+            if (tid == 63) v.head[0] = min(up, v.max_few);
+        }
+        lds_barrier();
+    } else if (tid == 0) {
+        v.head[0] = 0;
+    }
+    int tile_base = 0, ps_base = 0;
     for (int s0 = 0; s0 < v.S; s0 += KV_PLAN_THREADS) {
         const int s = s0 + tid;
         const bool in = s < v.S;
         int tok0 = 0, n = 0, L = 0;
-        if (in) {   // (what this thread wrote in the first walk)
-            const int4 q = v.req[s];
-            tok0 = a.seq_offsets[s];
-            n = q.w;
-            L = q.y >= 0 ? q.x + n : 0;
-        }
+        if (in) work_of(s, tok0, n, L);
         const int64_t rows = (int64_t)n * v.group;
-        const bool few = rows > 0 && rows <= KV_FEW_ROWS, tiled = rows > KV_FEW_ROWS;
-        const int blocks = ceil_shift(L, 6);
+        const bool few = is_few(n) && v.has_few, tiled = rows > KV_FEW_ROWS && v.has_tile;
         const int n_tiles = tiled ? (int)((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS) : few ? 1 : 0;
-        const int chunk = tiled ? tile_chunk : few_chunk;
-        const int parts = min(KV_MAX_PARTS, max(1, (blocks + chunk - 1) / chunk));
-        const int recs = n_tiles * parts;
-        const int ps = parts > 1 ? recs : 0;
-        const Scan2 up = block_scan(Scan2{((long long)(tiled ? recs : 0) << 32) | (unsigned)(few ? recs : 0), ps}, lds, t2);
-        const int few_at = few_base + (int)(unsigned)up.a - (few ? recs : 0);
-        const int tile_at = tile_base + (int)(up.a >> 32) - (tiled ? recs : 0);
-        const int ps_at = ps_base + up.b - ps;
-        if (few && v.has_few && few_at + recs <= v.max_few && ps_at + ps <= v.max_pslots)
-            for (int p = 0; p < parts; ++p) kv_write_tile(v.few + few_at + p, tok0, n, L, s, 0, p, parts, ps_at);
+        const int parts = parts_of(L, tiled ? tile_chunk : few_chunk);
+        const int recs = n_tiles * parts, ps = parts > 1 ? recs : 0;
+        const Scan2 up = block_scan(Scan2{tiled ? recs : 0, ps}, lds, t2);
+        const int tile_at = tile_base + (int)up.a - (tiled ? recs : 0), ps_at = ps_base + up.b - ps;
+        if (few) {
+            const int at = atomicAdd(&place[step_of(L, parts)], parts);
+            if (at + parts <= v.max_few && ps_at + ps <= v.max_pslots)
+                for (int p = 0; p < parts; ++p) kv_write_tile(v.few + at + p, tok0, n, L, s, 0, p, parts, ps_at);
+        }
         if (in) {
             v.req[s].w = tiled ? tile_at : -1;
             v.req_tiles[s] = make_int2(parts, ps_at);
         }
-        if (few_tokens && tiled && v.has_tile && tile_at + recs <= v.max_tile && ps_at + ps <= v.max_pslots)
+        if (few_tokens && tiled && tile_at + recs <= v.max_tile && ps_at + ps <= v.max_pslots)
             for (int t = 0; t < n_tiles; ++t)   // the last rows see the most keys: their tiles first
                 for (int p = 0; p < parts; ++p)
                     kv_write_tile(v.tile + tile_at + t * parts + p, tok0, n, L, s, (n_tiles - 1 - t) * KV_TILE_ROWS, p, parts,
                                   ps_at + (parts > 1 ? t * parts : 0));
-        few_base += (int)(unsigned)t2.a;
-        tile_base += (int)(t2.a >> 32);
+        tile_base += (int)t2.a;
         ps_base += t2.b;
     }
-    if (tid == 0) {
-        v.head[0] = min(few_base, v.max_few);
-        v.head[1] = min(tile_base, v.max_tile);
-    }
+    if (tid == 0) v.head[1] = min(tile_base, v.max_tile);
 }
 
 // Slots, table entries and tiles of requests with many new tokens: workgroup (request, chunk of 2048 tokens).
