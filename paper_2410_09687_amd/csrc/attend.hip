@@ -17,6 +17,8 @@
 //
 // Bound by memory where a request adds one token (68 D bytes a record and kv head against 4 D flops a row and key); by the vector
 // unit's softmax in prompts.
+#include <type_traits>
+
 #include "kv.h"
 #include "mxfp4.h"
 
@@ -114,6 +116,27 @@ __device__ __forceinline__ float sum4(float v)
     return bits_f32(a[0]) + bits_f32(a[1]);
 }
 
+__device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale, int u)   // u: a constant once unrolled
+{
+    return u == 0 ? mx4_pair<0>(codes, scale) : u == 1 ? mx4_pair<1>(codes, scale) : u == 2 ? mx4_pair<2>(codes, scale) : mx4_pair<3>(codes, scale);
+}
+
+// V^T operands of channels 2 u and 2 u + 1 of the lane's words: the 4 keys of its group in two tiles of 16 (words c0, c1, scale words vs
+// byte i and i + 1).
+template <int D>
+__device__ __forceinline__ void value_operands(const uint4 &c0, const uint4 &c1, const uint4 &vs, int i, int u, int lane, bf16x8_t &even, bf16x8_t &odd)
+{
+    uint32_t x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        uint32_t codes = word(e < 4 ? c0 : c1, e & 3);
+        if constexpr (D == 64) codes >>= (lane & 8) * 2;
+        x[e] = pair_of(codes, mx4_scale(word(vs, e & 3), i + e / 4), u);
+    }
+    even = operand(lows(x[0], x[1]), lows(x[2], x[3]), lows(x[4], x[5]), lows(x[6], x[7]));
+    odd = operand(highs(x[0], x[1]), highs(x[2], x[3]), highs(x[4], x[5]), highs(x[6], x[7]));
+}
+
 // A wave's columns (16 NT rows of queries) over the records that it walks.
 template <int D, int NT, bool Y32>
 struct Columns {
@@ -122,45 +145,43 @@ struct Columns {
     f32x4_t o[NT][NJ];
     float m[NT], l[NT];    // maximum so far, in units of log2 e / scale; this lane's share of the sum
 
-    // One record.  masked: row nt of this lane sees keys [lo[nt], hi[nt]) alone, the request has keys up to `end`; tok: the record's first
-    // token.
-    __device__ __forceinline__ void step(Record<D> &r, int n_cols, float c, int tok, bool masked, const int *lo, const int *hi, int end, int lane)
+    // One record.  keys(i, a): K operands of its tile i; values(h, u, even, odd): V^T operands of accumulators 2 u and 2 u + 1 for tiles 2 h and
+    // 2 h + 1.  masked: row nt of this lane sees keys [lo[nt], hi[nt]) alone; tok: the record's first token.
+    template <class Keys, class Values>
+    __device__ __forceinline__ void step(const Keys &keys, const Values &values, int n_cols, float c, int tok, bool masked, const int *lo, const int *hi,
+                                         int lane)
     {
         const int g = lane >> 4;
-        bf16x8_t k[4][KD];   // (one column: each is needed once and decoded where it is)
-        auto decode = [&](int i) {
+        f32x4_t s[NT][4];
 #pragma unroll
-            for (int j = 0; j < KD; ++j) k[i][j] = __builtin_bit_cast(bf16x8_t, mx4_decode(r.k[i][j], mx4_scale(r.ks[j / 4], i)));
-        };
-        if constexpr (NT > 1) {
+        for (int i = 0; i < 4; ++i) {
+            bf16x8_t k[KD];
+            keys(i, k);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) decode(i);
+            for (int nt = 0; nt < NT; ++nt) {
+                if (nt > 0 && nt >= n_cols) continue;
+                s[nt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < KD; ++j) s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j], q[nt][j], s[nt][i], 0, 0, 0);
+            }
         }
         constexpr int NP = Y32 ? 3 : 1;
         uint32_t p[NP][NT][4][2];   // the weights as a sum of NP bf16: [tile][keys 0 1, 2 3]
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             if (nt > 0 && nt >= n_cols) continue;
-            f32x4_t s[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (NT == 1) decode(i);
-                s[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < KD; ++j) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], q[nt][j], s[i], 0, 0, 0);
-            }
             if (masked) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int key = tok + i * 16 + g * 4 + e;
-                        s[i][e] = key >= lo[nt] && key < hi[nt] ? s[i][e] : NEG_INF;
+                        s[nt][i][e] = key >= lo[nt] && key < hi[nt] ? s[nt][i][e] : NEG_INF;
                     }
             }
             float top = m[nt];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, fmaxf(s[i][0], s[i][1])), fmaxf(s[i][2], s[i][3]));
+            for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, fmaxf(s[nt][i][0], s[nt][i][1])), fmaxf(s[nt][i][2], s[nt][i][3]));
             top = max4(top);
             // (nothing seen so far: any finite number will do as the maximum)
             const float base = top == NEG_INF ? 0.f : top * c;
@@ -177,7 +198,7 @@ struct Columns {
                 float w[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    w[e] = __builtin_amdgcn_exp2f(fmaf(s[i][e], c, -base));
+                    w[e] = __builtin_amdgcn_exp2f(fmaf(s[nt][i][e], c, -base));
                     sum += w[e];
                 }
 #pragma unroll
@@ -193,50 +214,46 @@ struct Columns {
             }
             l[nt] += sum;
         }
-        if (masked) mask_values(r, n_cols, tok, lo, hi, end, lane);
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int b = 0; b < SB; ++b) {
-                constexpr int PAIRS = D == 64 ? 2 : 4;   // pairs of channels of a word
-                uint32_t x[8][PAIRS];                    // [key][pair]
+            for (int u = 0; u < NJ / 2; ++u) {
+                bf16x8_t even, odd;
+                values(h, u, even, odd);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int i = 2 * a + e / 4;
-                    uint32_t codes = word(r.v[i][b], e & 3);
-                    const float scale = mx4_scale(word(r.vs[b], e & 3), i);
-                    if constexpr (D == 64) codes >>= (lane & 8) * 2;
-                    x[e][0] = mx4_pair<0>(codes, scale);
-                    x[e][1] = mx4_pair<1>(codes, scale);
-                    if constexpr (D != 64) {
-                        x[e][2] = mx4_pair<2>(codes, scale);
-                        x[e][3] = mx4_pair<3>(codes, scale);
-                    }
-                }
+                for (int nt = 0; nt < NT; ++nt) {
+                    if (nt > 0 && nt >= n_cols) continue;
 #pragma unroll
-                for (int u = 0; u < PAIRS; ++u) {
-                    const bf16x8_t even = operand(lows(x[0][u], x[1][u]), lows(x[2][u], x[3][u]), lows(x[4][u], x[5][u]), lows(x[6][u], x[7][u]));
-                    const bf16x8_t odd = operand(highs(x[0][u], x[1][u]), highs(x[2][u], x[3][u]), highs(x[4][u], x[5][u]), highs(x[6][u], x[7][u]));
-                    const int j = b * 8 + 2 * u;
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        if (nt > 0 && nt >= n_cols) continue;
-#pragma unroll
-                        for (int z = 0; z < NP; ++z) {
-                            const bf16x8_t pz = operand(p[z][nt][2 * a][0], p[z][nt][2 * a][1], p[z][nt][2 * a + 1][0], p[z][nt][2 * a + 1][1]);
-                            o[nt][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pz, o[nt][j], 0, 0, 0);
-                            o[nt][j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pz, o[nt][j + 1], 0, 0, 0);
-                        }
+                    for (int z = 0; z < NP; ++z) {
+                        const bf16x8_t pz = operand(p[z][nt][2 * h][0], p[z][nt][2 * h][1], p[z][nt][2 * h + 1][0], p[z][nt][2 * h + 1][1]);
+                        o[nt][2 * u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pz, o[nt][2 * u], 0, 0, 0);
+                        o[nt][2 * u + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pz, o[nt][2 * u + 1], 0, 0, 0);
                     }
                 }
             }
-        }
+    }
+
+    // The same on a record in this wave's own registers.
+    __device__ __forceinline__ void step(Record<D> &r, int n_cols, float c, int tok, bool masked, const int *lo, const int *hi, int end, int lane)
+    {
+        if (masked) mask_values(r.vs, n_cols, tok, lo, hi, end, lane);
+        step(
+            [&](int i, bf16x8_t (&k)[KD]) {
+#pragma unroll
+                for (int j = 0; j < KD; ++j) k[j] = __builtin_bit_cast(bf16x8_t, mx4_decode(r.k[i][j], mx4_scale(r.ks[j / 4], i)));
+            },
+            [&](int h, int u, bf16x8_t &even, bf16x8_t &odd) {
+                constexpr int PAIRS = D == 64 ? 2 : 4;   // pairs of channels of a word
+                const int b = u / PAIRS;
+                value_operands<D>(r.v[2 * h][b], r.v[2 * h + 1][b], r.vs[b], 2 * h, u % PAIRS, lane, even, odd);
+            },
+            n_cols, c, tok, masked, lo, hi, lane);
     }
 
     // The values of a record that not every row sees: what lies beyond the request's keys may hold anything and a block may
     // stand for NaN, and 0 times that is not 0 in the product.  Their scales become 2^-127; a row that does see a block of NaNs gets
     // its channels' NaN here, from a product of what is seen with what is NaN.
-    __device__ __forceinline__ void mask_values(Record<D> &r, int n_cols, int tok, const int *lo, const int *hi, int end, int lane)
+    __device__ __forceinline__ void mask_values(uint4 (&vs)[SB], int n_cols, int tok, const int *lo, const int *hi, int end, int lane)
     {
         const int g = lane >> 4;
 #pragma unroll
@@ -244,7 +261,7 @@ struct Columns {
             uint32_t nan[4], any = 0;   // [key e]: byte i is 255 where the block stands for NaN and the request has the key
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                uint32_t w = word(r.vs[b], e), bad = 0;
+                uint32_t w = word(vs[b], e), bad = 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint32_t byte = 255u << (8 * i);
@@ -254,10 +271,10 @@ struct Columns {
                 }
                 nan[e] = bad;
                 any |= bad;
-                if (e == 0) r.vs[b].x = w;
-                else if (e == 1) r.vs[b].y = w;
-                else if (e == 2) r.vs[b].z = w;
-                else r.vs[b].w = w;
+                if (e == 0) vs[b].x = w;
+                else if (e == 1) vs[b].y = w;
+                else if (e == 2) vs[b].z = w;
+                else vs[b].w = w;
             }
             if (__ballot(any != 0) == 0) continue;
 #pragma unroll
@@ -568,24 +585,29 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_ker
 #pragma unroll
         for (int i = 0; i < CH; ++i) x[i] = 0.f;
         o += 2 + ch;
-        constexpr int AHEAD = 64 / CH;   // parts whose loads are on their way together
-        for (int u0 = 0; u0 < t.n_parts; u0 += AHEAD) {
+        // several parts' loads on their way together
+        auto add = [&](int u0, auto ahead_c) {
+            constexpr int AHEAD = decltype(ahead_c)::value;
             float2 ahead[AHEAD][CH / 2];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-                for (int i = 0; i < CH / 2; ++i)
-                    ahead[u][i] = u0 + u < t.n_parts ? get_agent(o + (u0 + u) * part_step + 2 * i) : make_float2(0.f, 0.f);
+                for (int i = 0; i < CH / 2; ++i) ahead[u][i] = get_agent(o + min(u0 + u, t.n_parts - 1) * part_step + 2 * i);
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u) {
-                const float f = u0 + u < t.n_parts ? factor[row][u0 + u] : 0.f;
+                if (u0 + u >= t.n_parts) break;
+                const float f = factor[row][u0 + u];
 #pragma unroll
                 for (int i = 0; i < CH / 2; ++i) {
                     x[2 * i] = fmaf(ahead[u][i].x, f, x[2 * i]);
                     x[2 * i + 1] = fmaf(ahead[u][i].y, f, x[2 * i + 1]);
                 }
             }
-        }
+        };
+        if (t.n_parts <= 8)
+            for (int u0 = 0; u0 < t.n_parts; u0 += 4) add(u0, std::integral_constant<int, 4>());
+        else
+            for (int u0 = 0; u0 < t.n_parts; u0 += 64 / CH) add(u0, std::integral_constant<int, 64 / CH>());
         const float inv = inverse(l);
 #pragma unroll
         for (int i = 0; i < CH; ++i) x[i] *= inv;
