@@ -121,21 +121,60 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t codes, float scale, int u) 
     return u == 0 ? mx4_pair<0>(codes, scale) : u == 1 ? mx4_pair<1>(codes, scale) : u == 2 ? mx4_pair<2>(codes, scale) : mx4_pair<3>(codes, scale);
 }
 
-// V^T operands of channels 2 u and 2 u + 1 of the lane's words: the 4 keys of its group in two tiles of 16 (words c0, c1, scale words vs
-// byte i and i + 1).
-template <int D>
-__device__ __forceinline__ void value_operands(const uint4 &c0, const uint4 &c1, const uint4 &vs, int i, int u, int lane, bf16x8_t &even, bf16x8_t &odd)
+// V^T operands of two channels, byte u of the lane's words shifted down by `shift`: the 4 keys of its group in two tiles of 16 (words c0 and
+// c1, whose scales are bytes i and i + 1 of vs).
+__device__ __forceinline__ void value_operands(const uint4 &c0, const uint4 &c1, const uint4 &vs, int i, int shift, int u, bf16x8_t &even, bf16x8_t &odd)
 {
     uint32_t x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        uint32_t codes = word(e < 4 ? c0 : c1, e & 3);
-        if constexpr (D == 64) codes >>= (lane & 8) * 2;
-        x[e] = pair_of(codes, mx4_scale(word(vs, e & 3), i + e / 4), u);
+        x[e] = pair_of(word(e < 4 ? c0 : c1, e & 3) >> shift, mx4_scale(word(vs, e & 3), i + e / 4), u);
     }
     even = operand(lows(x[0], x[1]), lows(x[2], x[3]), lows(x[4], x[5]), lows(x[6], x[7]));
     odd = operand(highs(x[0], x[1]), highs(x[2], x[3]), highs(x[4], x[5]), highs(x[6], x[7]));
 }
+
+struct AttendK {
+    KvPlanView v;
+    AttendArgs a;
+    int list;              // 0: the tiles of few rows, 1: the others
+};
+
+// A workgroup's work: rows [t.row0, row_end) of a request's tile, one kv head, records [b0, b1).
+struct Work {
+    KvTile t;
+    int h, sub, row_end;
+    int pos0, first, last;   // positions of the request's first new token, and of the rows' first and last
+    int window, b0, b1;
+
+    // False: nothing to do.  (A tile of the plan may be several workgroups', of `height` rows each.)
+    __device__ __forceinline__ bool find(const AttendK &p, int height)
+    {
+        const KvPlanView &v = p.v;
+        const int rec_id = blockIdx.x / v.n_kv;
+        h = blockIdx.x - rec_id * v.n_kv;
+        const int4 *line = reinterpret_cast<const int4 *>((p.list ? v.tile : v.few) + rec_id);
+        const int4 ta = line[0], tb = line[1];   // (beside the list's length, not after it)
+        if (rec_id >= v.head[p.list]) return false;
+        t = KvTile{uniform(ta.x), uniform(ta.y), uniform(ta.z), uniform(ta.w), uniform(tb.x), uniform(tb.y), uniform(tb.z), uniform(tb.w)};
+        const int rows = t.n_tok * v.group;
+        sub = blockIdx.y;
+        t.row0 += sub * height;
+        if (t.row0 >= rows) return false;
+        row_end = min(rows, t.row0 + height);
+        pos0 = t.kv_len - t.n_tok;
+        first = pos0 + t.row0 / v.group;
+        last = pos0 + (row_end - 1) / v.group;
+        window = min(p.a.window > 0 ? p.a.window : 0x7fffffff, t.kv_len + 1);   // (no further: no position minus it overflows)
+        const int lo_all = max(0, first - window + 1), hi_all = max(0, last + 1);
+        const int b_lo = lo_all >> 6, n_blocks = hi_all > lo_all ? ((hi_all + 63) >> 6) - b_lo : 0;
+        b0 = b_lo + (int)((int64_t)n_blocks * t.part / t.n_parts);
+        b1 = b_lo + (int)((int64_t)n_blocks * (t.part + 1) / t.n_parts);
+        return true;
+    }
+    // Every row sees all of record b.
+    __device__ __forceinline__ bool whole(int b) const { return b * 64 >= last - window + 1 && b * 64 + 63 <= first; }
+};
 
 // A wave's columns (16 NT rows of queries) over the records that it walks.
 template <int D, int NT, bool Y32>
@@ -143,7 +182,32 @@ struct Columns {
     static constexpr int KD = Record<D>::KD, SB = Record<D>::SB, NJ = D / 16;
     bf16x8_t q[NT][KD];
     f32x4_t o[NT][NJ];
-    float m[NT], l[NT];    // maximum so far, in units of log2 e / scale; this lane's share of the sum
+    float m[NT], l[NT];    // reference of the weights, in units of log2 e / scale: the largest score so far or near it; this lane's share of the sum
+
+    // The rows row0 .. of the workgroup's: their queries, and the keys [lo, hi) that each sees.
+    __device__ __forceinline__ void begin(const AttendArgs &a, const Work &k, int row0, int group, int n_kv, int *lo, int *hi, int lane)
+    {
+        const int n = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int row = row0 + nt * 16 + n;
+            const bool real = row < k.row_end;
+            const int i = real ? row / group : 0, pos = k.pos0 + i;
+            lo[nt] = real ? max(0, pos - k.window + 1) : 0;
+            hi[nt] = real ? max(0, pos + 1) : 0;
+            m[nt] = NEG_INF;
+            l[nt] = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) o[nt][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            const char *x = static_cast<const char *>(a.q) +
+                            ((k.t.tok0 + i) * a.q_stride + (int64_t)(k.h * group + (real ? row - i * group : 0)) * D) * 2;
+#pragma unroll
+            for (int j = 0; j < KD; ++j) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(x + k_channel<D>(j, g) * 2);
+                q[nt][j] = __builtin_bit_cast(bf16x8_t, real ? u : make_uint4(0, 0, 0, 0));
+            }
+        }
+    }
 
     // One record.  keys(i, a): K operands of its tile i; values(h, u, even, odd): V^T operands of accumulators 2 u and 2 u + 1 for tiles 2 h and
     // 2 h + 1.  masked: row nt of this lane sees keys [lo[nt], hi[nt]) alone; tok: the record's first token.
@@ -182,16 +246,17 @@ struct Columns {
             float top = m[nt];
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, fmaxf(s[nt][i][0], s[nt][i][1])), fmaxf(s[nt][i][2], s[nt][i][3]));
-            top = max4(top);
-            // (nothing seen so far: any finite number will do as the maximum)
-            const float base = top == NEG_INF ? 0.f : top * c;
-            if (__ballot(top > m[nt])) {   // (rare after the first records)
-                const float shrink = __builtin_amdgcn_exp2f(fmaf(m[nt], c, -base));   // exp2(-inf) = 0 for the first keys
+            // Any reference near the maximum does: it moves only where a weight would pass 2^8 (with the exact maximum, one of 16 rows has
+            // a new one in nearly every record of a prompt).  Nothing seen so far: m = -inf, any first key moves it.
+            if (__ballot((top - m[nt]) * c > 8.f)) {
+                top = max4(top);
+                const float shrink = m[nt] == top ? 1.f : __builtin_amdgcn_exp2f((m[nt] - top) * c);   // exp2(-inf) = 0 for the first keys
                 l[nt] *= shrink;
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) o[nt][j] *= shrink;
                 m[nt] = top;
             }
+            const float base = m[nt] == NEG_INF ? 0.f : m[nt] * c;
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -245,7 +310,7 @@ struct Columns {
             [&](int h, int u, bf16x8_t &even, bf16x8_t &odd) {
                 constexpr int PAIRS = D == 64 ? 2 : 4;   // pairs of channels of a word
                 const int b = u / PAIRS;
-                value_operands<D>(r.v[2 * h][b], r.v[2 * h + 1][b], r.vs[b], 2 * h, u % PAIRS, lane, even, odd);
+                value_operands(r.v[2 * h][b], r.v[2 * h + 1][b], r.vs[b], 2 * h, D == 64 ? (lane & 8) * 2 : 0, u % PAIRS, even, odd);
             },
             n_cols, c, tok, masked, lo, hi, lane);
     }
@@ -303,12 +368,6 @@ struct Columns {
     }
 };
 
-struct AttendK {
-    KvPlanView v;
-    AttendArgs a;
-    int list;              // 0: the tiles of few rows, 1: the others
-};
-
 // Output row of the request's tokens: group rows of a token are query heads of the kv head.
 __device__ __forceinline__ int64_t y_row(const KvTile &t, int row, int group, int n_kv, int h)
 {
@@ -356,211 +415,29 @@ constexpr int min_waves()
     return NT > 1 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : D == 128 ? 2 : 1;
 }
 
-// CW groups of KW waves; a group has 16 NT rows of the tile, its waves take the records in turn.
-template <int D, int NT, int CW, int KW, bool Y32>
-__global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_kernel(AttendK p)
+// The end of a workgroup of 256 threads whose tile has several parts, its own left in `partial`: the one of the tile that reports last
+// joins them, in their order.  What the parts leave are device-scope stores: a workgroup waits for its own before it reports, and
+// nobody's L2 has to be written back.
+template <int D, int ROWS>
+__device__ __forceinline__ void join_parts(const AttendK &p, const Work &k, float c, float (*factor)[KV_MAX_PARTS + 1], int *flag)
 {
-    constexpr bool SPLIT = KW > 1;
-    constexpr int ROWS = 16 * NT * CW, CH = D / 16;   // CH: channels of a row per thread in the joins
-    constexpr int LDO = D + 4;
-    __shared__ float lds_o[SPLIT ? KW : 1][16][LDO];
-    __shared__ float lds_ml[KW][16][2];
-    __shared__ int lds_last;
     const KvPlanView &v = p.v;
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kw = wave % KW, cw = wave / KW, n = lane & 15, g = lane >> 4;
-    const int rec_id = blockIdx.x / v.n_kv, h = blockIdx.x - rec_id * v.n_kv;
-    const int4 *line = reinterpret_cast<const int4 *>((p.list ? v.tile : v.few) + rec_id);
-    const int4 ta = line[0], tb = line[1];   // (beside the list's length, not after it)
-    if (rec_id >= v.head[p.list]) return;
-    KvTile t{uniform(ta.x), uniform(ta.y), uniform(ta.z), uniform(ta.w), uniform(tb.x), uniform(tb.y), uniform(tb.z), uniform(tb.w)};
-    const int group = v.group, rows = t.n_tok * group, pos0 = t.kv_len - t.n_tok;
-    // (a tile of the plan may be several workgroups', of ROWS rows each)
-    const int sub = blockIdx.y;
-    t.row0 += sub * ROWS;
-    if (t.row0 >= rows) return;
-    const int row_end = min(rows, t.row0 + ROWS);
-    // positions of the tile's first and last token
-    const int first = pos0 + t.row0 / group, last = pos0 + (row_end - 1) / group;
-    const int window = min(p.a.window > 0 ? p.a.window : 0x7fffffff, t.kv_len + 1);   // (no further: no position minus it overflows)
-    const int lo_all = max(0, first - window + 1), hi_all = max(0, last + 1);
-    const int b_lo = lo_all >> 6, n_blocks = hi_all > lo_all ? ((hi_all + 63) >> 6) - b_lo : 0;
-    const int b0 = b_lo + (int)((int64_t)n_blocks * t.part / t.n_parts), b1 = b_lo + (int)((int64_t)n_blocks * (t.part + 1) / t.n_parts);
-
-    Columns<D, NT, Y32> w;
-    const int wrow0 = t.row0 + cw * 16 * NT;
-    const int n_cols = max(0, min(NT, (row_end - wrow0 + 15) >> 4));
-    int lo[NT], hi[NT];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        const int row = wrow0 + nt * 16 + n;
-        const bool real = row < row_end;
-        const int i = real ? row / group : 0, pos = pos0 + i;
-        lo[nt] = real ? max(0, pos - window + 1) : 0;
-        hi[nt] = real ? max(0, pos + 1) : 0;
-        w.m[nt] = NEG_INF;
-        w.l[nt] = 0.f;
-#pragma unroll
-        for (int j = 0; j < Columns<D, NT, Y32>::NJ; ++j) w.o[nt][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        const char *q = static_cast<const char *>(p.a.q) +
-                        ((t.tok0 + i) * p.a.q_stride + (int64_t)(h * group + (real ? row - i * group : 0)) * D) * 2;
-#pragma unroll
-        for (int j = 0; j < Columns<D, NT, Y32>::KD; ++j) {
-            const uint4 x = *reinterpret_cast<const uint4 *>(q + k_channel<D>(j, g) * 2);
-            w.q[nt][j] = __builtin_bit_cast(bf16x8_t, real ? x : make_uint4(0, 0, 0, 0));
-        }
-    }
-    const float c = p.a.scale * LOG2E;
-    const int *table = p.a.block_table + (int64_t)t.req * p.a.max_pages;
-    const int lb = p.a.pages.log_blocks;
-    const int64_t page_bytes = p.a.pages.page_bytes();
-    const char *heads = p.a.pages.data + (((int64_t)h * kv_record_bytes(D)) << lb);
-    constexpr int STEP = KW;
-    auto record_of = [&](int b, int page) {
-        return heads + (int64_t)page * page_bytes + (b & ((1 << lb) - 1)) * kv_record_bytes(D);
-    };
-    const int n_pages = p.a.pages.n_pages, first_b = b0 + kw;
-    if (first_b < b1 && n_cols > 0) {
-        Record<D> r0, r1;
-        const Places<D> at(lane);
-        bool bad = false;
-        // 64 records of the wave at a time, whose pages lie one to a lane: a read of the table among the loads below would have to wait for
-        // every load that is on its way ahead of it.
-        for (int c0 = first_b; c0 < b1; c0 += 64 * STEP) {
-            const int pages = table[min(c0 + lane * STEP, b1 - 1) >> lb];
-            // Starts the loads of record b, the i-th of the 64; whether its page exists.
-            auto start = [&](Record<D> &r, int i, int b) {
-                const int page = __builtin_amdgcn_readlane(pages, i);
-                const bool ok = page >= 0 && page < n_pages;
-                load_record<D>(r, record_of(min(b, b1 - 1), ok ? page : 0), at);
-                bad |= !ok;
-                return ok;
-            };
-            auto take = [&](Record<D> &r, int b, bool ok) {
-                const int tok = b * 64;
-                const bool whole = tok >= last - window + 1 && tok + 63 <= first;
-                if (ok) w.step(r, n_cols, c, tok, !whole, lo, hi, t.kv_len, lane);
-            };
-            const int count = min(64, (b1 - c0 + STEP - 1) / STEP);
-            bool ok0 = start(r0, 0, c0), ok1;
-            for (int i = 0, b = c0;;) {
-                ok1 = start(r1, min(i + 1, count - 1), b + STEP);
-                take(r0, b, ok0);
-                b += STEP;
-                if (++i >= count) break;
-                ok0 = start(r0, min(i + 1, count - 1), b + STEP);
-                take(r1, b, ok1);
-                b += STEP;
-                if (++i >= count) break;
-            }
-        }
-        if (bad && lane == 0) atomicOr(p.a.err_word, ERR_BAD_PAGE);
-    }
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) w.l[nt] = sum4(w.l[nt]);
-
-    const int ps = t.pslot + t.part;
-    float *part_o = p.a.partial + (((int64_t)ps * v.n_kv + h) * KV_TILE_ROWS + sub * ROWS) * (D + 2);
-    const bool whole = t.n_parts == 1;
-    if constexpr (SPLIT) {
-        const int row = tid >> 4, ch = (tid & 15) * CH;
-        for (int ct = 0; ct < CW * NT; ++ct) {
-            if (ct * 16 >= row_end - t.row0) break;
-            if (ct) __syncthreads();
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-                if (cw * NT + nt == ct) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int j = 0; j < D / 16; ++j)
-                            lds_o[kw][n][o_channel<D>(g * 4 + e) + (D == 256 ? (j >> 3) * 128 + (j & 7) : j)] = w.o[nt][j][e];
-                    if (g == 0) {
-                        lds_ml[kw][n][0] = w.m[nt];
-                        lds_ml[kw][n][1] = w.l[nt];
-                    }
-                }
-            __syncthreads();
-            if (tid >= 256) continue;
-            float m = NEG_INF, l = 0.f, x[CH];
-#pragma unroll
-            for (int u = 0; u < KW; ++u) m = fmaxf(m, lds_ml[u][row][0]);
-#pragma unroll
-            for (int i = 0; i < CH; ++i) x[i] = 0.f;
-            const float base = m == NEG_INF ? 0.f : m * c;
-#pragma unroll
-            for (int u = 0; u < KW; ++u) {
-                const float f = __builtin_amdgcn_exp2f(fmaf(lds_ml[u][row][0], c, -base));
-                l = fmaf(lds_ml[u][row][1], f, l);
-#pragma unroll
-                for (int i = 0; i < CH; ++i) x[i] = fmaf(lds_o[u][row][ch + i], f, x[i]);
-            }
-            const int r = t.row0 + ct * 16 + row;
-            if (r >= row_end) continue;
-            if (whole) {
-                const float inv = inverse(l);
-#pragma unroll
-                for (int i = 0; i < CH; ++i) x[i] *= inv;
-                const int64_t at = y_row(t, r, group, v.n_kv, h);
-                store_y(p.a, at, D, ch, x);
-                if (p.a.lse && ch == 0) p.a.lse[at] = log_sum(m, l, c);
-            } else {
-                float *o = part_o + (ct * 16 + row) * (D + 2);
-#pragma unroll
-                for (int i = 0; i < CH; i += 2) put_agent(o + 2 + ch + i, x[i], x[i + 1]);
-                if (ch == 0) put_agent(o, m, l);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int local = cw * 16 * NT + nt * 16 + n, r = t.row0 + local;
-            if (r >= row_end) continue;
-            const float l = w.l[nt], inv = whole ? (inverse(l)) : 1.f;
-            const int64_t at = y_row(t, r, group, v.n_kv, h);
-            float *o = part_o + local * (D + 2);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-#pragma unroll
-                for (int b = 0; b < (D == 256 ? 2 : 1); ++b) {
-                    constexpr int N = D == 64 ? 4 : 8;
-                    float x[N];
-#pragma unroll
-                    for (int j = 0; j < N; ++j) x[j] = w.o[nt][b * 8 + j][e] * inv;
-                    const int ch = o_channel<D>(g * 4 + e) + b * 128;
-                    if (whole) store_y(p.a, at, D, ch, x);
-                    else
-#pragma unroll
-                        for (int j = 0; j < N; j += 2) put_agent(o + 2 + ch + j, x[j], x[j + 1]);
-                }
-            }
-            if (g == 0) {
-                if (!whole) {
-                    put_agent(o, w.m[nt], l);
-                } else if (p.a.lse) {
-                    p.a.lse[at] = log_sum(w.m[nt], l, c);
-                }
-            }
-        }
-    }
-    if (whole) return;
-    // The tile's workgroup that reports last joins the parts, in their order.  What the parts leave are device-scope stores: a
-    // workgroup waits for its own before it reports, and nobody's L2 has to be written back.
+    const KvTile &t = k.t;
+    const int tid = threadIdx.x, group = v.group, h = k.h, sub = k.sub, row_end = k.row_end;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     int *ticket = v.tickets + (int64_t)(t.pslot + sub) * v.n_kv + h;   // (two parts or more: as many places)
     if (tid == 0) {
-        lds_last = atomicAdd(ticket, 1) == t.n_parts - 1;
-        if (lds_last) *ticket = 0;   // clean for the next call
+        *flag = atomicAdd(ticket, 1) == t.n_parts - 1;
+        if (*flag) *ticket = 0;   // clean for the next call
     }
     __syncthreads();
-    if (!lds_last) return;
+    if (!*flag) return;
+    constexpr int CH = D / 16;   // channels of a row per thread
     const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
     const float *first_part = p.a.partial + (((int64_t)t.pslot * v.n_kv + h) * KV_TILE_ROWS + sub * ROWS) * (D + 2);
     // 16 rows at a time: the factors of their parts into LDS (16 threads a row, each several parts), then the rows, several parts'
     // loads at a time.
-    constexpr int THREADS = 64 * CW * KW;
-    static_assert(THREADS == 256, "the join's threads: 16 rows of 16");
-    __shared__ float factor[16][KV_MAX_PARTS + 1];
     const int row = tid >> 4, sl = tid & 15;
     for (int r0 = 0; r0 < row_end - t.row0; r0 += 16) {
         const int local = r0 + row, ch = sl * CH;
@@ -617,13 +494,281 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_ker
     }
 }
 
+// Where the records of a request's kv head lie.
+struct Records {
+    const int *table;
+    const char *head;
+    int64_t page_bytes;
+    int log_blocks, n_pages, record;
+
+    __device__ __forceinline__ Records(const AttendArgs &a, const Work &k)
+        : table(a.block_table + (int64_t)k.t.req * a.max_pages),
+          head(a.pages.data + (((int64_t)k.h * kv_record_bytes(a.pages.D)) << a.pages.log_blocks)),
+          page_bytes(a.pages.page_bytes()), log_blocks(a.pages.log_blocks), n_pages(a.pages.n_pages), record(kv_record_bytes(a.pages.D))
+    {
+    }
+    // Record b; `ok`: its page exists (else one of page 0).
+    __device__ __forceinline__ const char *at(int b, int page, bool &ok) const
+    {
+        ok = page >= 0 && page < n_pages;
+        return head + (int64_t)(ok ? page : 0) * page_bytes + (b & ((1 << log_blocks) - 1)) * record;
+    }
+};
+
+// Tiles of few rows: CW groups of KW waves; a group has 16 NT rows of the tile, its waves take the records in turn and decode them in
+// their registers.
 template <int D, int NT, int CW, int KW, bool Y32>
-void launch_as(const AttendK &p, int records, int rows, hipStream_t stream)
+__global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_few_kernel(AttendK p)
+{
+    constexpr int ROWS = 16 * NT * CW, CH = D / 16;   // CH: channels of a row per thread in the joins
+    constexpr int LDO = D + 4;
+    static_assert(CW * KW == 4, "the join's threads: 16 rows of 16");
+    __shared__ float lds_o[KW][16][LDO];
+    __shared__ float lds_ml[KW][16][2];
+    __shared__ float factor[16][KV_MAX_PARTS + 1];
+    __shared__ int lds_last;
+    const KvPlanView &v = p.v;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kw = wave % KW, cw = wave / KW, n = lane & 15, g = lane >> 4;
+    Work k;
+    if (!k.find(p, ROWS)) return;
+    const KvTile &t = k.t;
+    const int wrow0 = t.row0 + cw * 16 * NT;
+    const int n_cols = max(0, min(NT, (k.row_end - wrow0 + 15) >> 4));
+    Columns<D, NT, Y32> w;
+    int lo[NT], hi[NT];
+    w.begin(p.a, k, wrow0, v.group, v.n_kv, lo, hi, lane);
+    const float c = p.a.scale * LOG2E;
+    const Records recs(p.a, k);
+    const int b1 = k.b1, first_b = k.b0 + kw;
+    if (first_b < b1 && n_cols > 0) {
+        Record<D> r0, r1;
+        const Places<D> at(lane);
+        bool bad = false;
+        // 64 records of the wave at a time, whose pages lie one to a lane: a read of the table among the loads below would have to wait for
+        // every load that is on its way ahead of it.
+        for (int c0 = first_b; c0 < b1; c0 += 64 * KW) {
+            const int pages = recs.table[min(c0 + lane * KW, b1 - 1) >> recs.log_blocks];
+            // Starts the loads of record b, the i-th of the 64; whether its page exists.
+            auto start = [&](Record<D> &r, int i, int b) {
+                bool ok;
+                load_record<D>(r, recs.at(min(b, b1 - 1), __builtin_amdgcn_readlane(pages, i), ok), at);
+                bad |= !ok;
+                return ok;
+            };
+            auto take = [&](Record<D> &r, int b, bool ok) {
+                if (ok) w.step(r, n_cols, c, b * 64, !k.whole(b), lo, hi, t.kv_len, lane);
+            };
+            const int count = min(64, (b1 - c0 + KW - 1) / KW);
+            bool ok0 = start(r0, 0, c0), ok1;
+            for (int i = 0, b = c0;;) {
+                ok1 = start(r1, min(i + 1, count - 1), b + KW);
+                take(r0, b, ok0);
+                b += KW;
+                if (++i >= count) break;
+                ok0 = start(r0, min(i + 1, count - 1), b + KW);
+                take(r1, b, ok1);
+                b += KW;
+                if (++i >= count) break;
+            }
+        }
+        if (bad && lane == 0) atomicOr(p.a.err_word, ERR_BAD_PAGE);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) w.l[nt] = sum4(w.l[nt]);
+
+    float *part_o = p.a.partial + (((int64_t)(t.pslot + t.part) * v.n_kv + k.h) * KV_TILE_ROWS + k.sub * ROWS) * (D + 2);
+    const bool alone = t.n_parts == 1;
+    const int row = tid >> 4, ch = (tid & 15) * CH;
+    for (int ct = 0; ct < CW * NT; ++ct) {
+        if (ct * 16 >= k.row_end - t.row0) break;
+        if (ct) __syncthreads();
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+            if (cw * NT + nt == ct) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int j = 0; j < D / 16; ++j)
+                        lds_o[kw][n][o_channel<D>(g * 4 + e) + (D == 256 ? (j >> 3) * 128 + (j & 7) : j)] = w.o[nt][j][e];
+                if (g == 0) {
+                    lds_ml[kw][n][0] = w.m[nt];
+                    lds_ml[kw][n][1] = w.l[nt];
+                }
+            }
+        __syncthreads();
+        float m = NEG_INF, l = 0.f, x[CH];
+#pragma unroll
+        for (int u = 0; u < KW; ++u) m = fmaxf(m, lds_ml[u][row][0]);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) x[i] = 0.f;
+        const float base = m == NEG_INF ? 0.f : m * c;
+#pragma unroll
+        for (int u = 0; u < KW; ++u) {
+            const float f = __builtin_amdgcn_exp2f(fmaf(lds_ml[u][row][0], c, -base));
+            l = fmaf(lds_ml[u][row][1], f, l);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[i] = fmaf(lds_o[u][row][ch + i], f, x[i]);
+        }
+        const int r = t.row0 + ct * 16 + row;
+        if (r >= k.row_end) continue;
+        if (alone) {
+            const float inv = inverse(l);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[i] *= inv;
+            const int64_t y = y_row(t, r, v.group, v.n_kv, k.h);
+            store_y(p.a, y, D, ch, x);
+            if (p.a.lse && ch == 0) p.a.lse[y] = log_sum(m, l, c);
+        } else {
+            float *o = part_o + (ct * 16 + row) * (D + 2);
+#pragma unroll
+            for (int i = 0; i < CH; i += 2) put_agent(o + 2 + ch + i, x[i], x[i + 1]);
+            if (ch == 0) put_agent(o, m, l);
+        }
+    }
+    if (!alone) join_parts<D, ROWS>(p, k, c, factor, &lds_last);
+}
+
+// Tiles of many rows: every one of the four waves has 32 rows and walks all of the records, a quarter of which it decodes into LDS for
+// all, one record ahead.
+template <int D, bool Y32>
+__global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(AttendK p)
+{
+    using Wave = Columns<D, 2, Y32>;
+    constexpr int KD = Wave::KD, SB = Wave::SB, NJ = Wave::NJ, FRAGS = 4 * KD + 2 * NJ;
+    constexpr int MINE = NJ / 4;   // pairs of accumulators of each half whose V operands a wave decodes
+    struct Operands {
+        uint4 k[4][KD][64], v[2][NJ][64];
+    };
+    static_assert(sizeof(Operands) == FRAGS * 1024, "");
+    __shared__ union {
+        Operands ops[2];
+        float factor[16][KV_MAX_PARTS + 1];
+    } lds;
+    __shared__ int lds_last;
+    const KvPlanView &v = p.v;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 15, g = lane >> 4;
+    Work k;
+    if (!k.find(p, KV_TILE_ROWS)) return;
+    const KvTile &t = k.t;
+    const int wrow0 = t.row0 + wave * 32;
+    Wave w;
+    int lo[2], hi[2];
+    w.begin(p.a, k, wrow0, v.group, v.n_kv, lo, hi, lane);
+    const float c = p.a.scale * LOG2E;
+    const Records recs(p.a, k);
+    const int b1 = k.b1;
+    if (k.b0 < b1) {
+        const Places<D> at(lane);
+        // This wave's share of a record: keys 16 wave .. + 15; of the values those of half wave / 2, MINE pairs of accumulators from u0 on.
+        const int half = wave >> 1, u0 = (wave & 1) * MINE;
+        uint32_t kc[KD], ks[SB];
+        uint4 vc[2], vs[SB];
+        auto start = [&](const char *rec) {
+#pragma unroll
+            for (int b = 0; b < SB; ++b) {
+                ks[b] = *reinterpret_cast<const uint32_t *>(rec + (at.ks + b * 256));
+                vs[b] = *reinterpret_cast<const uint4 *>(rec + (at.vs + b * 256));
+                if constexpr (D == 64) {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(rec + (at.k + wave * 8 * D));
+                    kc[0] = x.x;
+                    kc[1] = x.y;
+                } else {
+                    const uint4 x = *reinterpret_cast<const uint4 *>(rec + (at.k + wave * 8 * D + b * 1024));
+                    kc[4 * b] = x.x;
+                    kc[4 * b + 1] = x.y;
+                    kc[4 * b + 2] = x.z;
+                    kc[4 * b + 3] = x.w;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                vc[i] = *reinterpret_cast<const uint4 *>(rec + (at.v + (2 * half + i) * 8 * D + (D == 256 ? wave & 1 : 0) * 1024));
+        };
+        auto decode = [&](Operands &o, int b) {
+            if (!k.whole(b)) w.mask_values(vs, 2, b * 64, lo, hi, t.kv_len, lane);
+#pragma unroll
+            for (int j = 0; j < KD; ++j) o.k[wave][j][lane] = mx4_decode(kc[j], mx4_scale(ks[j / 4] >> (8 * wave), 0));
+            uint4 scales = SB == 2 && (wave & 1) ? vs[SB - 1] : vs[0];
+            scales = make_uint4(scales.x >> (16 * half), scales.y >> (16 * half), scales.z >> (16 * half), scales.w >> (16 * half));
+#pragma unroll
+            for (int u = 0; u < MINE; ++u) {
+                bf16x8_t even, odd;
+                value_operands(vc[0], vc[1], scales, 0, (D == 64 ? (lane & 8) * 2 : 0) + (D == 256 ? 0 : 8 * u0), u, even, odd);
+                o.v[half][2 * (u0 + u)][lane] = __builtin_bit_cast(uint4, even);
+                o.v[half][2 * (u0 + u) + 1][lane] = __builtin_bit_cast(uint4, odd);
+            }
+        };
+        bool bad = false;
+        for (int c0 = k.b0; c0 < b1; c0 += 64) {   // (64 pages at a time, one to a lane, as above)
+            const int pages = recs.table[min(c0 + lane, b1 - 1) >> recs.log_blocks];
+            const int count = min(64, b1 - c0);
+            bool ok, next_ok = false;
+            start(recs.at(c0, __builtin_amdgcn_readlane(pages, 0), ok));
+            decode(lds.ops[0], c0);
+            for (int i = 0; i < count; ++i) {
+                const int b = c0 + i;
+                const bool more = i + 1 < count;
+                if (more) start(recs.at(b + 1, __builtin_amdgcn_readlane(pages, i + 1), next_ok));
+                // Record b is whole in LDS; nobody reads the other half any more.
+                lds_barrier();
+                const Operands &o = lds.ops[i & 1];
+                if (ok)
+                    w.step(
+                        [&](int tile, bf16x8_t (&x)[KD]) {
+#pragma unroll
+                            for (int j = 0; j < KD; ++j) x[j] = __builtin_bit_cast(bf16x8_t, o.k[tile][j][lane]);
+                        },
+                        [&](int hv, int u, bf16x8_t &even, bf16x8_t &odd) {
+                            even = __builtin_bit_cast(bf16x8_t, o.v[hv][2 * u][lane]);
+                            odd = __builtin_bit_cast(bf16x8_t, o.v[hv][2 * u + 1][lane]);
+                        },
+                        2, c, b * 64, !k.whole(b), lo, hi, lane);
+                bad |= !ok;
+                if (more) decode(lds.ops[(i + 1) & 1], b + 1);
+                ok = next_ok;
+            }
+        }
+        if (bad && tid == 0) atomicOr(p.a.err_word, ERR_BAD_PAGE);
+    }
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) w.l[nt] = sum4(w.l[nt]);
+    float *part_o = p.a.partial + (((int64_t)(t.pslot + t.part) * v.n_kv + k.h) * KV_TILE_ROWS) * (D + 2);
+    const bool alone = t.n_parts == 1;
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+        const int local = wave * 32 + nt * 16 + n, r = t.row0 + local;
+        if (r >= k.row_end) continue;
+        const float l = w.l[nt], inv = alone ? inverse(l) : 1.f;
+        const int64_t y = y_row(t, r, v.group, v.n_kv, k.h);
+        float *o = part_o + local * (D + 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+            for (int b = 0; b < SB; ++b) {
+                constexpr int N = D == 64 ? 4 : 8;
+                float x[N];
+#pragma unroll
+                for (int j = 0; j < N; ++j) x[j] = w.o[nt][b * 8 + j][e] * inv;
+                const int ch = o_channel<D>(g * 4 + e) + b * 128;
+                if (alone) store_y(p.a, y, D, ch, x);
+                else
+#pragma unroll
+                    for (int j = 0; j < N; j += 2) put_agent(o + 2 + ch + j, x[j], x[j + 1]);
+            }
+        }
+        if (g == 0) {
+            if (!alone) put_agent(o, w.m[nt], l);
+            else if (p.a.lse) p.a.lse[y] = log_sum(w.m[nt], l, c);
+        }
+    }
+    if (!alone) join_parts<D, KV_TILE_ROWS>(p, k, c, lds.factor, &lds_last);
+}
+
+template <int D, int NT, int CW, int KW, bool Y32>
+void launch_few(const AttendK &p, int rows, hipStream_t stream)
 {
     constexpr int ROWS = 16 * NT * CW;
-    static_assert(KV_TILE_ROWS / ROWS <= 2 || KW > 1, "workgroups of a tile");
-    hipLaunchKernelGGL((attend_kernel<D, NT, CW, KW, Y32>), dim3((unsigned)records * p.v.n_kv, (unsigned)(rows / ROWS)), dim3(64 * CW * KW), 0,
-                       stream, p);
+    hipLaunchKernelGGL((attend_few_kernel<D, NT, CW, KW, Y32>), dim3((unsigned)p.v.max_few * p.v.n_kv, (unsigned)(rows / ROWS)), dim3(256), 0, stream, p);
 }
 
 template <int D, bool Y32>
@@ -632,12 +777,12 @@ hipError_t launch_d(const KvPlanView &v, const AttendArgs &a, hipStream_t stream
     constexpr bool WIDE = D == 256;   // two columns of accumulators would leave no registers for the rest
     AttendK p{v, a, 0};
     if (v.has_few) {
-        if (std::min(v.max_new * (int64_t)v.group, (int64_t)KV_FEW_ROWS) <= 16) launch_as<D, 1, 1, 4, Y32>(p, v.max_few, 16, stream);
-        else launch_as<D, WIDE ? 1 : 2, WIDE ? 2 : 1, WIDE ? 2 : 4, Y32>(p, v.max_few, KV_FEW_ROWS, stream);
+        if (std::min(v.max_new * (int64_t)v.group, (int64_t)KV_FEW_ROWS) <= 16) launch_few<D, 1, 1, 4, Y32>(p, 16, stream);
+        else launch_few<D, WIDE ? 1 : 2, WIDE ? 2 : 1, WIDE ? 2 : 4, Y32>(p, KV_FEW_ROWS, stream);
     }
     if (v.has_tile) {
         p.list = 1;
-        launch_as<D, WIDE ? 1 : 2, 4, 1, Y32>(p, v.max_tile, KV_TILE_ROWS, stream);
+        hipLaunchKernelGGL((attend_tile_kernel<D, Y32>), dim3((unsigned)v.max_tile * v.n_kv), dim3(256), 0, stream, p);
     }
     return hipGetLastError();
 }
