@@ -17,8 +17,6 @@
 //
 // Bound by memory where a request adds one token (68 D bytes a record and kv head against 4 D flops a row and key); by the vector
 // unit's softmax in prompts.
-#include <type_traits>
-
 #include "kv.h"
 #include "mxfp4.h"
 
@@ -195,7 +193,7 @@ struct Columns {
             const int i = real ? row / group : 0, pos = k.pos0 + i;
             lo[nt] = real ? max(0, pos - k.window + 1) : 0;
             hi[nt] = real ? max(0, pos + 1) : 0;
-            m[nt] = NEG_INF;
+            m[nt] = real ? NEG_INF : 0.f;   // (a row that is none never asks for a maximum)
             l[nt] = 0.f;
 #pragma unroll
             for (int j = 0; j < NJ; ++j) o[nt][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -209,110 +207,116 @@ struct Columns {
         }
     }
 
-    // One record.  keys(i, a): K operands of its tile i; values(h, u, even, odd): V^T operands of accumulators 2 u and 2 u + 1 for tiles 2 h and
-    // 2 h + 1.  masked: row nt of this lane sees keys [lo[nt], hi[nt]) alone; tok: the record's first token.
-    template <class Keys, class Values>
-    __device__ __forceinline__ void step(const Keys &keys, const Values &values, int n_cols, float c, int tok, bool masked, const int *lo, const int *hi,
-                                         int lane)
+    static constexpr int NP = Y32 ? 3 : 1;
+    using Scores = f32x4_t[NT][4];          // [.][tile of 16 keys]: this lane's row, its group's four keys
+    using Weights = uint32_t[NP][NT][4][2]; // as a sum of NP bf16, keys 0 1 and 2 3 of a tile's four
+
+    // Scores of tile i, whose K operands are k.
+    __device__ __forceinline__ void score(const bf16x8_t (&k)[KD], Scores &s, int i, int n_cols) const
     {
-        const int g = lane >> 4;
-        f32x4_t s[NT][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bf16x8_t k[KD];
-            keys(i, k);
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt > 0 && nt >= n_cols) continue;
+            s[nt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                if (nt > 0 && nt >= n_cols) continue;
-                s[nt][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < KD; ++j) s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j], q[nt][j], s[nt][i], 0, 0, 0);
-            }
+            for (int j = 0; j < KD; ++j) s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j], q[nt][j], s[nt][i], 0, 0, 0);
         }
-        constexpr int NP = Y32 ? 3 : 1;
-        uint32_t p[NP][NT][4][2];   // the weights as a sum of NP bf16: [tile][keys 0 1, 2 3]
+    }
+    // The softmax of a record: scores to weights.  masked: row nt of this lane sees keys [lo[nt], hi[nt]) alone; tok: the record's first token.
+    __device__ __forceinline__ void weigh(Scores &s, Weights &p, int n_cols, float c, int tok, bool masked, const int *lo, const int *hi, int lane)
+    {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             if (nt > 0 && nt >= n_cols) continue;
             if (masked) {
+                int key = tok + (lane >> 4) * 4;
+                asm volatile("" : "+v"(key));   // (or the sixteen sums move up, in front of the condition)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int key = tok + i * 16 + g * 4 + e;
-                        s[nt][i][e] = key >= lo[nt] && key < hi[nt] ? s[nt][i][e] : NEG_INF;
-                    }
+                    for (int e = 0; e < 4; ++e) s[nt][i][e] = key + i * 16 + e >= lo[nt] && key + i * 16 + e < hi[nt] ? s[nt][i][e] : NEG_INF;
             }
-            float top = m[nt];
+            auto fill = [&]() {
+                const float base = m[nt] == NEG_INF ? 0.f : m[nt] * c;
+                float sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, fmaxf(s[nt][i][0], s[nt][i][1])), fmaxf(s[nt][i][2], s[nt][i][3]));
-            // Any reference near the maximum does: it moves only where a weight would pass 2^8 (with the exact maximum, one of 16 rows has
-            // a new one in nearly every record of a prompt).  Nothing seen so far: m = -inf, any first key moves it.
-            if (__ballot((top - m[nt]) * c > 8.f)) {
+                for (int i = 0; i < 4; ++i) {
+                    float w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        w[e] = __builtin_amdgcn_exp2f(fmaf(s[nt][i][e], c, -base));
+                        sum += w[e];
+                    }
+#pragma unroll
+                    for (int u = 0; u < NP; ++u) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t hi2 = pack_bf16x2(w[2 * h], w[2 * h + 1]);
+                            p[u][nt][i][h] = hi2;
+                            w[2 * h] -= bits_f32(hi2 << 16);
+                            w[2 * h + 1] -= bits_f32(hi2 & 0xFFFF0000u);
+                        }
+                    }
+                }
+                return sum;
+            };
+            // Any reference near the maximum does: it moves only where the weights would pass 2^8, which their sum shows, so that the maximum
+            // itself is rarely taken.  (Taken in every record it is new for one of 16 rows in most records of a prompt.)
+            float sum = fill();
+            if (__ballot(!(sum <= 256.f) || m[nt] == NEG_INF)) {
+                float top = m[nt];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(fmaxf(top, fmaxf(s[nt][i][0], s[nt][i][1])), fmaxf(s[nt][i][2], s[nt][i][3]));
                 top = max4(top);
                 const float shrink = m[nt] == top ? 1.f : __builtin_amdgcn_exp2f((m[nt] - top) * c);   // exp2(-inf) = 0 for the first keys
                 l[nt] *= shrink;
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) o[nt][j] *= shrink;
                 m[nt] = top;
-            }
-            const float base = m[nt] == NEG_INF ? 0.f : m[nt] * c;
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float w[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    w[e] = __builtin_amdgcn_exp2f(fmaf(s[nt][i][e], c, -base));
-                    sum += w[e];
-                }
-#pragma unroll
-                for (int u = 0; u < NP; ++u) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t hi2 = pack_bf16x2(w[2 * h], w[2 * h + 1]);
-                        p[u][nt][i][h] = hi2;
-                        w[2 * h] -= bits_f32(hi2 << 16);
-                        w[2 * h + 1] -= bits_f32(hi2 & 0xFFFF0000u);
-                    }
-                }
+                sum = fill();
             }
             l[nt] += sum;
         }
+    }
+    // Values of tiles 2 h and 2 h + 1 into accumulators 2 u and 2 u + 1, whose V^T operands are even and odd.
+    __device__ __forceinline__ void add(const Weights &p, int h, int u, bf16x8_t even, bf16x8_t odd, int n_cols)
+    {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt > 0 && nt >= n_cols) continue;
+#pragma unroll
+            for (int z = 0; z < NP; ++z) {
+                const bf16x8_t pz = operand(p[z][nt][2 * h][0], p[z][nt][2 * h][1], p[z][nt][2 * h + 1][0], p[z][nt][2 * h + 1][1]);
+                o[nt][2 * u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pz, o[nt][2 * u], 0, 0, 0);
+                o[nt][2 * u + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pz, o[nt][2 * u + 1], 0, 0, 0);
+            }
+        }
+    }
+
+    // A record in this wave's own registers.  masked: not every row sees all of it; end: keys that the request has.
+    __device__ __forceinline__ void step(Record<D> &r, int n_cols, float c, int tok, bool masked, const int *lo, const int *hi, int end, int lane)
+    {
+        if (masked) mask_values(r.vs, n_cols, tok, lo, hi, end, lane);
+        Scores s;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf16x8_t k[KD];
+#pragma unroll
+            for (int j = 0; j < KD; ++j) k[j] = __builtin_bit_cast(bf16x8_t, mx4_decode(r.k[i][j], mx4_scale(r.ks[j / 4], i)));
+            score(k, s, i, n_cols);
+        }
+        Weights p;
+        weigh(s, p, n_cols, c, tok, masked, lo, hi, lane);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int u = 0; u < NJ / 2; ++u) {
-                bf16x8_t even, odd;
-                values(h, u, even, odd);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    if (nt > 0 && nt >= n_cols) continue;
-#pragma unroll
-                    for (int z = 0; z < NP; ++z) {
-                        const bf16x8_t pz = operand(p[z][nt][2 * h][0], p[z][nt][2 * h][1], p[z][nt][2 * h + 1][0], p[z][nt][2 * h + 1][1]);
-                        o[nt][2 * u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, pz, o[nt][2 * u], 0, 0, 0);
-                        o[nt][2 * u + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, pz, o[nt][2 * u + 1], 0, 0, 0);
-                    }
-                }
-            }
-    }
-
-    // The same on a record in this wave's own registers.
-    __device__ __forceinline__ void step(Record<D> &r, int n_cols, float c, int tok, bool masked, const int *lo, const int *hi, int end, int lane)
-    {
-        if (masked) mask_values(r.vs, n_cols, tok, lo, hi, end, lane);
-        step(
-            [&](int i, bf16x8_t (&k)[KD]) {
-#pragma unroll
-                for (int j = 0; j < KD; ++j) k[j] = __builtin_bit_cast(bf16x8_t, mx4_decode(r.k[i][j], mx4_scale(r.ks[j / 4], i)));
-            },
-            [&](int h, int u, bf16x8_t &even, bf16x8_t &odd) {
                 constexpr int PAIRS = D == 64 ? 2 : 4;   // pairs of channels of a word
                 const int b = u / PAIRS;
+                bf16x8_t even, odd;
                 value_operands(r.v[2 * h][b], r.v[2 * h + 1][b], r.vs[b], 2 * h, D == 64 ? (lane & 8) * 2 : 0, u % PAIRS, even, odd);
-            },
-            n_cols, c, tok, masked, lo, hi, lane);
+                add(p, h, u, even, odd, n_cols);
+            }
     }
 
     // The values of a record that not every row sees: what lies beyond the request's keys may hold anything and a block may
@@ -321,6 +325,12 @@ struct Columns {
     __device__ __forceinline__ void mask_values(uint4 (&vs)[SB], int n_cols, int tok, const int *lo, const int *hi, int end, int lane)
     {
         const int g = lane >> 4;
+        uint32_t full = 0;   // bit 7 of a byte: it is 255
+#pragma unroll
+        for (int b = 0; b < SB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) full |= word(vs[b], e) & ((word(vs[b], e) & 0x7F7F7F7Fu) + 0x01010101u);
+        if (tok + 64 <= end && __ballot((full & 0x80808080u) != 0) == 0) return;   // (a prompt's own triangle, as a rule)
 #pragma unroll
         for (int b = 0; b < SB; ++b) {
             uint32_t nan[4], any = 0;   // [key e]: byte i is 255 where the block stands for NaN and the request has the key
@@ -436,12 +446,76 @@ __device__ __forceinline__ void join_parts(const AttendK &p, const Work &k, floa
     constexpr int CH = D / 16;   // channels of a row per thread
     const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
     const float *first_part = p.a.partial + (((int64_t)t.pslot * v.n_kv + h) * KV_TILE_ROWS + sub * ROWS) * (D + 2);
-    // 16 rows at a time: the factors of their parts into LDS (16 threads a row, each several parts), then the rows, several parts'
-    // loads at a time.
-    const int row = tid >> 4, sl = tid & 15;
-    for (int r0 = 0; r0 < row_end - t.row0; r0 += 16) {
+    const int row = tid >> 4, sl = tid & 15, n_rows = row_end - t.row0;
+    if (t.n_parts <= 8) {
+        // 16 threads a row, everything of four parts on its way at once and of two rows a thread: a trip to memory for 32 rows, where the
+        // form below takes six.
+        constexpr int AHEAD = 4, G = ROWS > 16 ? 2 : 1;
+        const int ch = sl * CH;
+        for (int r0 = 0; r0 < n_rows; r0 += 16 * G) {
+            float m[G], l[G], x[G][CH];
+#pragma unroll
+            for (int z = 0; z < G; ++z) {
+                m[z] = NEG_INF;
+                l[z] = 0.f;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) x[z][i] = 0.f;
+            }
+            for (int u0 = 0; u0 < t.n_parts; u0 += AHEAD) {
+                float2 ml[G][AHEAD], a[G][AHEAD][CH / 2];
+#pragma unroll
+                for (int z = 0; z < G; ++z) {
+                    const float *o = first_part + min(r0 + 16 * z + row, n_rows - 1) * (D + 2);
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        const float *part = o + min(u0 + u, t.n_parts - 1) * part_step;
+                        ml[z][u] = get_agent(part);
+#pragma unroll
+                        for (int i = 0; i < CH / 2; ++i) a[z][u][i] = get_agent(part + 2 + ch + 2 * i);
+                    }
+                }
+#pragma unroll
+                for (int z = 0; z < G; ++z) {
+                    float top = m[z];
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) top = fmaxf(top, ml[z][u].x);   // (the last part more than once: no harm to a maximum)
+                    const float base = top == NEG_INF ? 0.f : top * c;
+                    const float shrink = __builtin_amdgcn_exp2f(fmaf(m[z], c, -base));
+                    m[z] = top;
+                    l[z] *= shrink;
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) x[z][i] *= shrink;
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        if (u0 + u >= t.n_parts) break;
+                        const float f = __builtin_amdgcn_exp2f(fmaf(ml[z][u].x, c, -base));
+                        l[z] = fmaf(ml[z][u].y, f, l[z]);
+#pragma unroll
+                        for (int i = 0; i < CH / 2; ++i) {
+                            x[z][2 * i] = fmaf(a[z][u][i].x, f, x[z][2 * i]);
+                            x[z][2 * i + 1] = fmaf(a[z][u][i].y, f, x[z][2 * i + 1]);
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int z = 0; z < G; ++z) {
+                if (r0 + 16 * z + row >= n_rows) continue;
+                const float inv = inverse(l[z]);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) x[z][i] *= inv;
+                const int64_t at = y_row(t, t.row0 + r0 + 16 * z + row, group, v.n_kv, h);
+                store_y(p.a, at, D, ch, x[z]);
+                if (p.a.lse && ch == 0) p.a.lse[at] = log_sum(m[z], l[z], c);
+            }
+        }
+        return;
+    }
+    // More parts, 16 rows at a time: the factors of their parts into LDS (16 threads a row, each several parts), then the rows, several
+    // parts' loads at a time.
+    for (int r0 = 0; r0 < n_rows; r0 += 16) {
         const int local = r0 + row, ch = sl * CH;
-        const bool real = t.row0 + local < row_end;
+        const bool real = local < n_rows;
         const float *o = first_part + (real ? local : 0) * (D + 2);
         float m = NEG_INF, l = 0.f, x[CH];
         for (int u = sl; u < t.n_parts; u += 16) m = fmaxf(m, get_agent(o + u * part_step).x);
@@ -462,9 +536,8 @@ __device__ __forceinline__ void join_parts(const AttendK &p, const Work &k, floa
 #pragma unroll
         for (int i = 0; i < CH; ++i) x[i] = 0.f;
         o += 2 + ch;
-        // several parts' loads on their way together
-        auto add = [&](int u0, auto ahead_c) {
-            constexpr int AHEAD = decltype(ahead_c)::value;
+        constexpr int AHEAD = 64 / CH;   // parts whose loads are on their way together
+        for (int u0 = 0; u0 < t.n_parts; u0 += AHEAD) {
             float2 ahead[AHEAD][CH / 2];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u)
@@ -480,11 +553,7 @@ __device__ __forceinline__ void join_parts(const AttendK &p, const Work &k, floa
                     x[2 * i + 1] = fmaf(ahead[u][i].y, f, x[2 * i + 1]);
                 }
             }
-        };
-        if (t.n_parts <= 8)
-            for (int u0 = 0; u0 < t.n_parts; u0 += 4) add(u0, std::integral_constant<int, 4>());
-        else
-            for (int u0 = 0; u0 < t.n_parts; u0 += 64 / CH) add(u0, std::integral_constant<int, 64 / CH>());
+        }
         const float inv = inverse(l);
 #pragma unroll
         for (int i = 0; i < CH; ++i) x[i] *= inv;
@@ -708,21 +777,29 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
             for (int i = 0; i < count; ++i) {
                 const int b = c0 + i;
                 const bool more = i + 1 < count;
-                if (more) start(recs.at(b + 1, __builtin_amdgcn_readlane(pages, i + 1), next_ok));
+                // (without a condition: loads under one are waited for where it ends)
+                start(recs.at(more ? b + 1 : b, __builtin_amdgcn_readlane(pages, more ? i + 1 : i), next_ok));
                 // Record b is whole in LDS; nobody reads the other half any more.
                 lds_barrier();
                 const Operands &o = lds.ops[i & 1];
-                if (ok)
-                    w.step(
-                        [&](int tile, bf16x8_t (&x)[KD]) {
+                if (ok) {
+                    const bool masked = !k.whole(b);
+                    typename Wave::Scores s;
 #pragma unroll
-                            for (int j = 0; j < KD; ++j) x[j] = __builtin_bit_cast(bf16x8_t, o.k[tile][j][lane]);
-                        },
-                        [&](int hv, int u, bf16x8_t &even, bf16x8_t &odd) {
-                            even = __builtin_bit_cast(bf16x8_t, o.v[hv][2 * u][lane]);
-                            odd = __builtin_bit_cast(bf16x8_t, o.v[hv][2 * u + 1][lane]);
-                        },
-                        2, c, b * 64, !k.whole(b), lo, hi, lane);
+                    for (int tile = 0; tile < 4; ++tile) {
+                        bf16x8_t x[KD];
+#pragma unroll
+                        for (int j = 0; j < KD; ++j) x[j] = __builtin_bit_cast(bf16x8_t, o.k[tile][j][lane]);
+                        w.score(x, s, tile, 2);
+                    }
+                    typename Wave::Weights x;
+                    w.weigh(s, x, 2, c, b * 64, masked, lo, hi, lane);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int u = 0; u < NJ / 2; ++u)
+                            w.add(x, h, u, __builtin_bit_cast(bf16x8_t, o.v[h][2 * u][lane]), __builtin_bit_cast(bf16x8_t, o.v[h][2 * u + 1][lane]), 2);
+                }
                 bad |= !ok;
                 if (more) decode(lds.ops[(i + 1) & 1], b + 1);
                 ok = next_ok;

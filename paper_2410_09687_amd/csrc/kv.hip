@@ -88,6 +88,7 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
     long long tok_base = 0;
     int page_base = 0, taken = 0;
     long long few_blocks = 0, tile_blocks = 0;   // records that the tiles of either kind walk, one kv head
+    int tiles = 0;
     for (int s0 = 0; s0 < v.S; s0 += KV_PLAN_THREADS) {
         const int s = s0 + tid;
         const bool in = s < v.S;
@@ -116,8 +117,13 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
             // (a request that is not served has no keys: its rows come out as zeros)
             const int64_t rows = (int64_t)n * v.group;
             const int blocks = served ? ceil_shift(kv + n0, 6) : 0;
-            if (rows > KV_FEW_ROWS) tile_blocks += (rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS * blocks;
-            else if (rows > 0) few_blocks += blocks;
+            if (rows > KV_FEW_ROWS) {
+                const int own = (int)min((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS, (int64_t)KV_TILE_TARGET);   // (as many fill the chip alone)
+                tiles += own;
+                tile_blocks += (long long)own * blocks;
+            } else if (rows > 0) {
+                few_blocks += blocks;
+            }
             if (served && need > 0) taken = dealt + need;
             if (few_tokens || n > v.max_new) {   // (more than the second launch covers: not served)
                 for (int i = 0; i < n; ++i)
@@ -135,8 +141,9 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
     Scan2 sums, t2;
     block_scan(Scan2{few_blocks, 0}, lds, sums);
     const long long few_all = sums.a;
-    block_scan(Scan2{tile_blocks, 0}, lds, sums);
+    block_scan(Scan2{tile_blocks, tiles}, lds, sums);
     const long long tile_all = sums.a;
+    const int tiles_all = sums.b;
     lds_barrier();
     __shared__ int lds_taken;
     if (tid == 0) lds_taken = 0;
@@ -152,7 +159,10 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
     // parts: so large that the launch has about its target of workgroups, over all kv heads
     const int few_goal = max(1, KV_FEW_TARGET / v.n_kv), tile_goal = max(1, KV_TILE_TARGET / v.n_kv);
     const int few_chunk = (int)max((long long)KV_FEW_MIN, (few_all + few_goal - 1) / few_goal);
-    const int tile_chunk = (int)max((long long)KV_TILE_MIN, (tile_all + tile_goal - 1) / tile_goal);
+    // (of tiles no more than the target, each one's last part being a shorter one, lest a few begin when the others end: chunks of 400 - 500 tokens
+    // of four requests, 640 workgroups 161 us, 448 120; but at least half of it, for the sake of a long request among many short ones)
+    const int tile_room = max((tile_goal + 1) / 2, tile_goal - tiles_all);
+    const int tile_chunk = (int)max((long long)KV_TILE_MIN, (tile_all + tile_room - 1) / tile_room);
     // Tiles of few rows are listed by the length of their parts, longest first (in 64 steps; who is first in a step is left to chance and
     // shows in no result): the last workgroups to begin are then short ones.
     __shared__ int place[64];
