@@ -425,24 +425,29 @@ constexpr int min_waves()
     return NT > 1 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : D == 128 ? 2 : 1;
 }
 
-// The end of a workgroup of 256 threads whose tile has several parts, its own left in `partial`: the one of the tile that reports last
-// joins them, in their order.  What the parts leave are device-scope stores: a workgroup waits for its own before it reports, and
-// nobody's L2 has to be written back.
+// The end of a workgroup whose tile has several parts, its own left in `partial`: whether it is the last of the tile's to report, which then joins
+// the parts, in their order.  What the parts leave are device-scope stores: a workgroup waits for its own before it reports, and nobody's L2
+// has to be written back.
+__device__ __forceinline__ bool last_of(const KvPlanView &v, const Work &k, int *flag)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    int *ticket = v.tickets + (int64_t)(k.t.pslot + k.sub) * v.n_kv + k.h;   // (two parts or more: as many places)
+    if (threadIdx.x == 0) {
+        *flag = atomicAdd(ticket, 1) == k.t.n_parts - 1;
+        if (*flag) *ticket = 0;   // clean for the next call
+    }
+    __syncthreads();
+    return *flag;
+}
+
+// The join of a tile of few rows, a part's rows one after the other, {m, l, channels} each; 256 threads.
 template <int D, int ROWS>
-__device__ __forceinline__ void join_parts(const AttendK &p, const Work &k, float c, float (*factor)[KV_MAX_PARTS + 1], int *flag)
+__device__ __forceinline__ void join_rows(const AttendK &p, const Work &k, float c, float (*factor)[KV_MAX_PARTS + 1])
 {
     const KvPlanView &v = p.v;
     const KvTile &t = k.t;
     const int tid = threadIdx.x, group = v.group, h = k.h, sub = k.sub, row_end = k.row_end;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    int *ticket = v.tickets + (int64_t)(t.pslot + sub) * v.n_kv + h;   // (two parts or more: as many places)
-    if (tid == 0) {
-        *flag = atomicAdd(ticket, 1) == t.n_parts - 1;
-        if (*flag) *ticket = 0;   // clean for the next call
-    }
-    __syncthreads();
-    if (!*flag) return;
     constexpr int CH = D / 16;   // channels of a row per thread
     const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
     const float *first_part = p.a.partial + (((int64_t)t.pslot * v.n_kv + h) * KV_TILE_ROWS + sub * ROWS) * (D + 2);
@@ -694,7 +699,7 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_few
             if (ch == 0) put_agent(o, m, l);
         }
     }
-    if (!alone) join_parts<D, ROWS>(p, k, c, factor, &lds_last);
+    if (!alone && last_of(v, k, &lds_last)) join_rows<D, ROWS>(p, k, c, factor);
 }
 
 // Tiles of many rows: every one of the four waves has 32 rows and walks all of the records, a quarter of which it decodes into LDS for
@@ -709,10 +714,7 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
         uint4 k[4][KD][64], v[2][NJ][64];
     };
     static_assert(sizeof(Operands) == FRAGS * 1024, "");
-    __shared__ union {
-        Operands ops[2];
-        float factor[16][KV_MAX_PARTS + 1];
-    } lds;
+    __shared__ Operands ops[2];
     __shared__ int lds_last;
     const KvPlanView &v = p.v;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n = lane & 15, g = lane >> 4;
@@ -773,7 +775,7 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
             const int count = min(64, b1 - c0);
             bool ok, next_ok = false;
             start(recs.at(c0, __builtin_amdgcn_readlane(pages, 0), ok));
-            decode(lds.ops[0], c0);
+            decode(ops[0], c0);
             for (int i = 0; i < count; ++i) {
                 const int b = c0 + i;
                 const bool more = i + 1 < count;
@@ -781,7 +783,7 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
                 start(recs.at(more ? b + 1 : b, __builtin_amdgcn_readlane(pages, more ? i + 1 : i), next_ok));
                 // Record b is whole in LDS; nobody reads the other half any more.
                 lds_barrier();
-                const Operands &o = lds.ops[i & 1];
+                const Operands &o = ops[i & 1];
                 if (ok) {
                     const bool masked = !k.whole(b);
                     typename Wave::Scores s;
@@ -801,7 +803,7 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
                             w.add(x, h, u, __builtin_bit_cast(bf16x8_t, o.v[h][2 * u][lane]), __builtin_bit_cast(bf16x8_t, o.v[h][2 * u + 1][lane]), 2);
                 }
                 bad |= !ok;
-                if (more) decode(lds.ops[(i + 1) & 1], b + 1);
+                if (more) decode(ops[(i + 1) & 1], b + 1);
                 ok = next_ok;
             }
         }
@@ -809,15 +811,58 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
     }
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) w.l[nt] = sum4(w.l[nt]);
-    float *part_o = p.a.partial + (((int64_t)(t.pslot + t.part) * v.n_kv + k.h) * KV_TILE_ROWS) * (D + 2);
-    const bool alone = t.n_parts == 1;
+    if (t.n_parts > 1) {
+        // A part's results lie as the lanes have them: whole lines, and the join needs no order of rows.
+        const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
+        float *first_part = p.a.partial + ((int64_t)t.pslot * v.n_kv + k.h) * KV_TILE_ROWS * (D + 2);
+        const int ml_at = KV_TILE_ROWS * D + (wave * 32 + n) * 2, o_at = (wave * 4 * NJ * 64 + lane) * 2;
+        float *mine = first_part + t.part * part_step;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            if (g == 0) put_agent(mine + ml_at + nt * 32, w.m[nt], w.l[nt]);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) put_agent(mine + o_at + ((nt * NJ + j) * 2 + e) * 128, w.o[nt][j][2 * e], w.o[nt][j][2 * e + 1]);
+        }
+        if (!last_of(v, k, &lds_last)) return;
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+            w.m[nt] = NEG_INF;
+            w.l[nt] = 0.f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) w.o[nt][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
+        for (int u = 0; u < t.n_parts; ++u) {
+            const float *part = first_part + u * part_step;
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+                const float2 ml = get_agent(part + ml_at + nt * 32);
+                float2 x[NJ][2];
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) x[j][e] = get_agent(part + o_at + ((nt * NJ + j) * 2 + e) * 128);
+                const float top = fmaxf(w.m[nt], ml.x), base = top == NEG_INF ? 0.f : top * c;
+                const float f0 = __builtin_amdgcn_exp2f(fmaf(w.m[nt], c, -base)), f1 = __builtin_amdgcn_exp2f(fmaf(ml.x, c, -base));
+                w.m[nt] = top;
+                w.l[nt] = fmaf(ml.y, f1, w.l[nt] * f0);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        w.o[nt][j][2 * e] = fmaf(x[j][e].x, f1, w.o[nt][j][2 * e] * f0);
+                        w.o[nt][j][2 * e + 1] = fmaf(x[j][e].y, f1, w.o[nt][j][2 * e + 1] * f0);
+                    }
+            }
+        }
+    }
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt) {
-        const int local = wave * 32 + nt * 16 + n, r = t.row0 + local;
+        const int r = wrow0 + nt * 16 + n;
         if (r >= k.row_end) continue;
-        const float l = w.l[nt], inv = alone ? inverse(l) : 1.f;
+        const float inv = inverse(w.l[nt]);
         const int64_t y = y_row(t, r, v.group, v.n_kv, k.h);
-        float *o = part_o + local * (D + 2);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
 #pragma unroll
@@ -826,19 +871,11 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
                 float x[N];
 #pragma unroll
                 for (int j = 0; j < N; ++j) x[j] = w.o[nt][b * 8 + j][e] * inv;
-                const int ch = o_channel<D>(g * 4 + e) + b * 128;
-                if (alone) store_y(p.a, y, D, ch, x);
-                else
-#pragma unroll
-                    for (int j = 0; j < N; j += 2) put_agent(o + 2 + ch + j, x[j], x[j + 1]);
+                store_y(p.a, y, D, o_channel<D>(g * 4 + e) + b * 128, x);
             }
         }
-        if (g == 0) {
-            if (!alone) put_agent(o, w.m[nt], l);
-            else if (p.a.lse) p.a.lse[y] = log_sum(w.m[nt], l, c);
-        }
+        if (g == 0 && p.a.lse) p.a.lse[y] = log_sum(w.m[nt], w.l[nt], c);
     }
-    if (!alone) join_parts<D, KV_TILE_ROWS>(p, k, c, lds.factor, &lds_last);
 }
 
 template <int D, int NT, int CW, int KW, bool Y32>
