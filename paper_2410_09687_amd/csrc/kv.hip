@@ -159,10 +159,45 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
     // parts: so large that the launch has about its target of workgroups, over all kv heads
     const int few_goal = max(1, KV_FEW_TARGET / v.n_kv), tile_goal = max(1, KV_TILE_TARGET / v.n_kv);
     const int few_chunk = (int)max((long long)KV_FEW_MIN, (few_all + few_goal - 1) / few_goal);
-    // (of tiles no more than the target, each one's last part being a shorter one, lest a few begin when the others end: chunks of 400 - 500 tokens
-    // of four requests, 640 workgroups 161 us, 448 120; but at least half of it, for the sake of a long request among many short ones)
-    const int tile_room = max((tile_goal + 1) / 2, tile_goal - tiles_all);
-    const int tile_chunk = (int)max((long long)KV_TILE_MIN, (tile_all + tile_room - 1) / tile_room);
+    int tile_chunk = (int)max((long long)KV_TILE_MIN, (tile_all + tile_goal - 1) / tile_goal);
+    // Tiles of many rows run long, and a few that begin when the others end cost as much as all of those: chunks of 400 - 500 tokens of four
+    // requests 161 us in 640 workgroups, 127 in 448; 16 prefixes of 4000 113 us whole, 86 halved.  So a few sizes of parts, from the
+    // smallest on, are weighed by when the last part would end: beside the others if all have room, else when the work before it is done.
+    constexpr int SIZES = 8;
+    __shared__ int count[SIZES], longest[SIZES];
+    if (tiles_all > 0 && tiles_all < 4 * tile_goal) {
+        const int eighths[SIZES] = {8, 9, 10, 12, 14, 16, 20, 32};
+        int size[SIZES];
+#pragma unroll
+        for (int i = 0; i < SIZES; ++i)
+            size[i] = (int)min(0x3fffffffLL, max((long long)KV_TILE_MIN, (tile_all * eighths[i] / 8 + tile_goal - 1) / tile_goal));
+        if (tid < SIZES) count[tid] = longest[tid] = 0;
+        lds_barrier();
+        for (int s = tid; s < v.S; s += KV_PLAN_THREADS) {
+            const int4 q = v.req[s];   // (what this thread wrote in the first walk)
+            const int64_t rows = (int64_t)q.w * v.group;
+            if (rows <= KV_FEW_ROWS) continue;
+            const int tiles = (int)min((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS, (int64_t)KV_TILE_TARGET);
+            const int blocks = q.y >= 0 ? ceil_shift(q.x + q.w, 6) : 0;
+#pragma unroll
+            for (int i = 0; i < SIZES; ++i) {
+                const int parts = min(KV_MAX_PARTS, max(1, (blocks + size[i] - 1) / size[i]));
+                atomicAdd(&count[i], tiles * parts);
+                atomicMax(&longest[i], (blocks + parts - 1) / parts);
+            }
+        }
+        lds_barrier();
+        constexpr int COST = 4;   // of a workgroup's beginning and end, in records
+        long long best = 0x7fffffffffffffffLL;
+#pragma unroll
+        for (int i = 0; i < SIZES; ++i) {
+            const long long ends = (count[i] <= tile_goal ? 0 : (tile_all + (long long)COST * count[i]) / tile_goal) + longest[i] + COST;
+            if (ends < best) {
+                best = ends;
+                tile_chunk = size[i];
+            }
+        }
+    }
     // Tiles of few rows are listed by the length of their parts, longest first (in 64 steps; who is first in a step is left to chance and
     // shows in no result): the last workgroups to begin are then short ones.
     __shared__ int place[64];
