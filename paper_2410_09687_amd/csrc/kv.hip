@@ -5,7 +5,7 @@
 
 namespace moin {
 
-constexpr int KV_PLAN_THREADS = 1024, KV_PLAN_WAVES = KV_PLAN_THREADS / 64;
+constexpr int KV_RELEASE_THREADS = 1024;
 constexpr int KV_SLOT_CHUNK = 2048;   // tokens of a request per workgroup of the second launch
 
 // Inclusive scans over the workgroup, two quantities at once; `total` gets the workgroup's sums.
@@ -13,6 +13,7 @@ struct Scan2 {
     long long a;
     int b;
 };
+template <int PT>
 __device__ __forceinline__ Scan2 block_scan(Scan2 v, Scan2 *lds, Scan2 &total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -31,7 +32,7 @@ __device__ __forceinline__ Scan2 block_scan(Scan2 v, Scan2 *lds, Scan2 &total)
     Scan2 before{0, 0};
     total = Scan2{0, 0};
 #pragma unroll
-    for (int w = 0; w < KV_PLAN_WAVES; ++w) {
+    for (int w = 0; w < PT / 64; ++w) {
         const Scan2 x = lds[w];
         if (w < wave) {
             before.a += x.a;
@@ -66,18 +67,19 @@ __device__ __forceinline__ void kv_write_tile(KvTile *dst, int tok0, int n_tok, 
     d[1] = make_int4(row0, part, n_parts, pslot);
 }
 
-// One workgroup walks the requests, 1024 at a time, twice.  First: offsets (a sum over the new tokens), pages to deal (a sum over
+// One workgroup walks the requests, PT at a time, twice.  First: offsets (a sum over the new tokens), pages to deal (a sum over
 // the pages that each request lacks), which requests are served.  Then, with the keys of all requests known, the
 // size of the parts that fill the chip and everybody's place in the lists.  Up to KV_FEW_TOKENS new tokens a
 // request (decode), it writes slots and table entries itself; else a second launch does, a workgroup for 2048 tokens of a request.
 // Bound by latency: a chain of a dozen trips to memory and barriers.
-__global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, KvPlanArgs a, int log_page, int few_tokens)
+template <int PT>
+__global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a, int log_page, int few_tokens)
 {
-    __shared__ Scan2 lds[KV_PLAN_WAVES];
+    __shared__ Scan2 lds[PT / 64];
     __shared__ int lds_err;
     const int tid = threadIdx.x;
     if (tid == 0) lds_err = 0;
-    for (int i = tid; i < v.max_pslots * v.n_kv; i += KV_PLAN_THREADS) v.tickets[i] = 0;
+    for (int i = tid; i < v.max_pslots * v.n_kv; i += PT) v.tickets[i] = 0;
     int n_free = *a.n_free;
     int err = 0;
     if (n_free < 0 || n_free > a.free_cap) {
@@ -89,7 +91,7 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
     int page_base = 0, taken = 0;
     long long few_blocks = 0, tile_blocks = 0;   // records that the tiles of either kind walk, one kv head
     int tiles = 0;
-    for (int s0 = 0; s0 < v.S; s0 += KV_PLAN_THREADS) {
+    for (int s0 = 0; s0 < v.S; s0 += PT) {
         const int s = s0 + tid;
         const bool in = s < v.S;
         const int kv = in ? a.kv_lens[s] : 0, n0 = in ? a.new_lens[s] : 0;
@@ -97,7 +99,7 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
         const int have = ceil_shift(max(kv, 0), log_page);
         const int need = sane ? ceil_shift(kv + n0, log_page) - have : 0;
         Scan2 total;
-        const Scan2 up = block_scan(Scan2{max(n0, 0), need}, lds, total);
+        const Scan2 up = block_scan<PT>(Scan2{max(n0, 0), need}, lds, total);
         const long long end = tok_base + up.a, begin = end - max(n0, 0);
         const int dealt = page_base + up.b - need;
         const bool whole = end <= v.T;
@@ -139,9 +141,9 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
     }
     // sums over the workgroup (served requests are a prefix of those that want pages: the last one's end is what is taken)
     Scan2 sums, t2;
-    block_scan(Scan2{few_blocks, 0}, lds, sums);
+    block_scan<PT>(Scan2{few_blocks, 0}, lds, sums);
     const long long few_all = sums.a;
-    block_scan(Scan2{tile_blocks, tiles}, lds, sums);
+    block_scan<PT>(Scan2{tile_blocks, tiles}, lds, sums);
     const long long tile_all = sums.a;
     const int tiles_all = sums.b;
     lds_barrier();
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
             size[i] = (int)min(0x3fffffffLL, max((long long)KV_TILE_MIN, (tile_all * eighths[i] / 8 + tile_goal - 1) / tile_goal));
         if (tid < SIZES) count[tid] = longest[tid] = 0;
         lds_barrier();
-        for (int s = tid; s < v.S; s += KV_PLAN_THREADS) {
+        for (int s = tid; s < v.S; s += PT) {
             const int4 q = v.req[s];   // (what this thread wrote in the first walk)
             const int64_t rows = (int64_t)q.w * v.group;
             if (rows <= KV_FEW_ROWS) continue;
@@ -213,7 +215,7 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
     auto step_of = [&](int L, int parts) { return 63 - min(63, (ceil_shift(L, 6) + parts - 1) / parts * 63 / few_chunk); };
     auto is_few = [&](int n) { return n > 0 && (int64_t)n * v.group <= KV_FEW_ROWS; };
     if (v.has_few) {
-        for (int s = tid; s < v.S; s += KV_PLAN_THREADS) {
+        for (int s = tid; s < v.S; s += PT) {
             int tok0, n, L;
             work_of(s, tok0, n, L);
             if (!is_few(n)) continue;
@@ -237,7 +239,7 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
         v.head[0] = 0;
     }
     int tile_base = 0, ps_base = 0;
-    for (int s0 = 0; s0 < v.S; s0 += KV_PLAN_THREADS) {
+    for (int s0 = 0; s0 < v.S; s0 += PT) {
         const int s = s0 + tid;
         const bool in = s < v.S;
         int tok0 = 0, n = 0, L = 0;
@@ -247,7 +249,7 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_plan_kernel(KvPlanView v, 
         const int n_tiles = tiled ? (int)((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS) : few ? 1 : 0;
         const int parts = parts_of(L, tiled ? tile_chunk : few_chunk);
         const int recs = n_tiles * parts, ps = parts > 1 ? recs : 0;
-        const Scan2 up = block_scan(Scan2{tiled ? recs : 0, ps}, lds, t2);
+        const Scan2 up = block_scan<PT>(Scan2{tiled ? recs : 0, ps}, lds, t2);
         const int tile_at = tile_base + (int)up.a - (tiled ? recs : 0), ps_at = ps_base + up.b - ps;
         if (few) {
             const int at = atomicAdd(&place[step_of(L, parts)], parts);
@@ -305,7 +307,9 @@ static int log2_of(int v)
 hipError_t launch_kv_plan(const KvPlanView &v, const KvPlanArgs &a, hipStream_t stream)
 {
     const int few_tokens = v.max_new <= KV_FEW_TOKENS, log_page = log2_of(a.page_tokens);
-    hipLaunchKernelGGL(kv_plan_kernel, dim3(1), dim3(KV_PLAN_THREADS), 0, stream, v, a, log_page, few_tokens);
+    // (a barrier costs fewer waves less: 64 requests in 13.2 us with 1024 threads, 8.1 with 256; 1000 prompts in 22.3 with 1024, 17.2 with 512)
+    if (v.S <= 256) hipLaunchKernelGGL(kv_plan_kernel<256>, dim3(1), dim3(256), 0, stream, v, a, log_page, few_tokens);
+    else hipLaunchKernelGGL(kv_plan_kernel<512>, dim3(1), dim3(512), 0, stream, v, a, log_page, few_tokens);
     if (!few_tokens)
         hipLaunchKernelGGL(kv_slots_kernel, dim3((unsigned)v.S, (unsigned)((v.max_new + KV_SLOT_CHUNK - 1) / KV_SLOT_CHUNK)), dim3(256), 0,
                            stream, v, a, log_page);
@@ -313,29 +317,29 @@ hipError_t launch_kv_plan(const KvPlanView &v, const KvPlanArgs &a, hipStream_t 
 }
 
 // Pages of finished requests go back on the stack, in the requests' order; their rows of the table become -1, their lengths 0.
-__global__ __launch_bounds__(KV_PLAN_THREADS) void kv_release_kernel(const int *finished, int S, int *kv_lens, int *block_table, int max_pages,
+__global__ __launch_bounds__(KV_RELEASE_THREADS) void kv_release_kernel(const int *finished, int S, int *kv_lens, int *block_table, int max_pages,
                                                                      int log_page, int *free_pages, int *n_free, int free_cap, int n_pages,
                                                                      int *err_word)
 {
-    __shared__ Scan2 lds[KV_PLAN_WAVES];
-    __shared__ int2 range[KV_PLAN_THREADS];
+    __shared__ Scan2 lds[KV_RELEASE_THREADS / 64];
+    __shared__ int2 range[KV_RELEASE_THREADS];
     const int tid = threadIdx.x;
     int base = *n_free;
     const int before = base;
     bool bad = base < 0 || base > free_cap;
     base = max(0, min(base, free_cap));
-    for (int s0 = 0; s0 < S; s0 += KV_PLAN_THREADS) {
+    for (int s0 = 0; s0 < S; s0 += KV_RELEASE_THREADS) {
         const int s = s0 + tid;
         const bool done = s < S && finished[s] != 0;
         const int kv = done ? kv_lens[s] : 0;
         const int pages = done ? min(ceil_shift(max(kv, 0), log_page), max_pages) : 0;
         if (done && (kv < 0 || ceil_shift(max(kv, 0), log_page) > max_pages)) bad = true;
         Scan2 total;
-        const Scan2 up = block_scan(Scan2{0, pages}, lds, total);
+        const Scan2 up = block_scan<KV_RELEASE_THREADS>(Scan2{0, pages}, lds, total);
         range[tid] = make_int2(base + up.b - pages, pages);
         if (done) kv_lens[s] = 0;
         lds_barrier();
-        for (int w = tid >> 6; w < min(KV_PLAN_THREADS, S - s0); w += KV_PLAN_WAVES) {   // a wave per request
+        for (int w = tid >> 6; w < min(KV_RELEASE_THREADS, S - s0); w += KV_RELEASE_THREADS / 64) {   // a wave per request
             const int2 r = range[w];
             for (int j = tid & 63; j < r.y; j += 64) {
                 int *entry = block_table + (int64_t)(s0 + w) * max_pages + j;
@@ -355,7 +359,7 @@ __global__ __launch_bounds__(KV_PLAN_THREADS) void kv_release_kernel(const int *
 hipError_t launch_kv_release(const int *finished, int S, int *kv_lens, int *block_table, int max_pages, int page_tokens, int *free_pages,
                              int *n_free, int free_cap, int n_pages, int *err_word, hipStream_t stream)
 {
-    hipLaunchKernelGGL(kv_release_kernel, dim3(1), dim3(KV_PLAN_THREADS), 0, stream, finished, S, kv_lens, block_table, max_pages,
+    hipLaunchKernelGGL(kv_release_kernel, dim3(1), dim3(KV_RELEASE_THREADS), 0, stream, finished, S, kv_lens, block_table, max_pages,
                        log2_of(page_tokens), free_pages, n_free, free_cap, n_pages, err_word);
     return hipGetLastError();
 }
