@@ -755,8 +755,8 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
             for (int i = 0; i < 2; ++i)
                 vc[i] = *reinterpret_cast<const uint4 *>(rec + (at.v + (2 * half + i) * 8 * D + (D == 256 ? wave & 1 : 0) * 1024));
         };
-        auto decode = [&](Operands &o, int b) {
-            if (!k.whole(b)) w.mask_values(vs, 2, b * 64, lo, hi, t.kv_len, lane);
+        auto decode = [&](Operands &o, int b, bool ok) {   // ok: else it is some other record, of which nothing is used
+            if (ok && !k.whole(b)) w.mask_values(vs, 2, b * 64, lo, hi, t.kv_len, lane);
 #pragma unroll
             for (int j = 0; j < KD; ++j) o.k[wave][j][lane] = mx4_decode(kc[j], mx4_scale(ks[j / 4] >> (8 * wave), 0));
             uint4 scales = SB == 2 && (wave & 1) ? vs[SB - 1] : vs[0];
@@ -775,7 +775,7 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
             const int count = min(64, b1 - c0);
             bool ok, next_ok = false;
             start(recs.at(c0, __builtin_amdgcn_readlane(pages, 0), ok));
-            decode(ops[0], c0);
+            decode(ops[0], c0, ok);
             for (int i = 0; i < count; ++i) {
                 const int b = c0 + i;
                 const bool more = i + 1 < count;
@@ -803,7 +803,7 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
                             w.add(x, h, u, __builtin_bit_cast(bf16x8_t, o.v[h][2 * u][lane]), __builtin_bit_cast(bf16x8_t, o.v[h][2 * u + 1][lane]), 2);
                 }
                 bad |= !ok;
-                if (more) decode(ops[(i + 1) & 1], b + 1);
+                if (more) decode(ops[(i + 1) & 1], b + 1, next_ok);
                 ok = next_ok;
             }
         }
