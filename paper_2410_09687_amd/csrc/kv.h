@@ -26,12 +26,17 @@ struct KvPages {
 };
 
 // Query rows of a request (its tokens times the query heads of a kv head) are cut into tiles.  Requests of up to KV_FEW_ROWS
-// rows are one tile, whose workgroup's waves take the keys in turn; larger ones have tiles of KV_TILE_ROWS rows, KV_TILE_ROWS / 4 to
+// rows are one tile, whose workgroup's waves take the records in turn; larger ones have tiles of KV_TILE_ROWS rows, KV_TILE_ROWS / 4 to
 // a wave, and every wave walks all the keys.  A tile's keys are cut into parts where there are too few tiles to fill the
 // chip; the workgroup of a tile that ends last joins its parts.
+// (Rows 32: 64 requests of 2000 keys and 4 tokens, 32 heads on 4 of 64 channels, 19.5 us as one tile of few rows, 36 as tiles of 128; 32 heads on 8 of
+// 128, 8 tokens 41 and 76.)
 constexpr int KV_FEW_ROWS = 32, KV_TILE_ROWS = 128;
-constexpr int KV_FEW_TOKENS = 8;   // up to here (new tokens of a request) the plan is one launch
-// Workgroups aimed at per launch where the keys allow, and the fewest records of a part.
+// Up to here (new tokens of a request) the plan is one launch: 64 requests of 4 tokens 7.0 us, 9.4 in two; of 32 tokens 15.3 and 11.5.
+constexpr int KV_FEW_TOKENS = 8;
+// Workgroups aimed at per launch where the keys allow, two for every compute unit, and the fewest records of a part.  (Two requests of 100000 keys 65 us, with
+// 768 75, with 1024 80; 8 prompts of 128 behind 2000 keys 55, with 768 68.  One request of 4000 keys 8.5, with 16 records and more 10.5; a
+// prompt of 128 behind 3000 20.0, with 4 and more 28, with 16 23.7.)
 constexpr int KV_FEW_TARGET = 512, KV_FEW_MIN = 4;
 constexpr int KV_TILE_TARGET = 512, KV_TILE_MIN = 8;
 constexpr int KV_MAX_PARTS = 128;  // of a tile

@@ -165,40 +165,52 @@ __global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a,
     // Tiles of many rows run long, and a few that begin when the others end cost as much as all of those: chunks of 400 - 500 tokens of four
     // requests 161 us in 640 workgroups, 127 in 448; 16 prefixes of 4000 113 us whole, 86 halved.  So a few sizes of parts, from the
     // smallest on, are weighed by when the last part would end: beside the others if all have room, else when the work before it is done.
-    constexpr int SIZES = 8;
+    constexpr int SIZES = 8, COST = 4;   // COST: of a workgroup's beginning and end, in records
     __shared__ int count[SIZES], longest[SIZES];
+    __shared__ int2 work[PT];
     if (tiles_all > 0 && tiles_all < 4 * tile_goal) {
-        const int eighths[SIZES] = {8, 9, 10, 12, 14, 16, 20, 32};
-        int size[SIZES];
-#pragma unroll
-        for (int i = 0; i < SIZES; ++i)
-            size[i] = (int)min(0x3fffffffLL, max((long long)KV_TILE_MIN, (tile_all * eighths[i] / 8 + tile_goal - 1) / tile_goal));
+        // (a thread to a size and every PT / 8-th request; through LDS, and sums by shuffles: atomics of all requests on eight words took 36 us
+        // for 64 of them)
+        const int i = tid % SIZES;
+        const int eighths = (int)(0x2014100E0C0A0908uLL >> 8 * i & 255);   // of the smallest: 8, 9, 10, 12, 14, 16, 20, 32
+        const int size = (int)min(0x3fffffffLL, max((long long)KV_TILE_MIN, (tile_all * eighths / 8 + tile_goal - 1) / tile_goal));
+        int parts_all = 0, top = 0;
         if (tid < SIZES) count[tid] = longest[tid] = 0;
-        lds_barrier();
-        for (int s = tid; s < v.S; s += PT) {
-            const int4 q = v.req[s];   // (what this thread wrote in the first walk)
-            const int64_t rows = (int64_t)q.w * v.group;
-            if (rows <= KV_FEW_ROWS) continue;
-            const int tiles = (int)min((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS, (int64_t)KV_TILE_TARGET);
-            const int blocks = q.y >= 0 ? ceil_shift(q.x + q.w, 6) : 0;
-#pragma unroll
-            for (int i = 0; i < SIZES; ++i) {
-                const int parts = min(KV_MAX_PARTS, max(1, (blocks + size[i] - 1) / size[i]));
-                atomicAdd(&count[i], tiles * parts);
-                atomicMax(&longest[i], (blocks + parts - 1) / parts);
+        for (int s0 = 0; s0 < v.S; s0 += PT) {
+            const int s = s0 + tid;
+            int2 own = make_int2(0, 0);
+            if (s < v.S) {
+                const int4 q = v.req[s];   // (what this thread wrote in the first walk)
+                const int64_t rows = (int64_t)q.w * v.group;
+                if (rows > KV_FEW_ROWS)
+                    own = make_int2((int)min((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS, (int64_t)KV_TILE_TARGET), q.y >= 0 ? ceil_shift(q.x + q.w, 6) : 0);
             }
+            work[tid] = own;
+            lds_barrier();
+            for (int r = tid / SIZES; r < min(PT, v.S - s0); r += PT / SIZES) {
+                const int2 w = work[r];
+                if (w.x == 0) continue;
+                const int parts = min(KV_MAX_PARTS, max(1, (w.y + size - 1) / size));
+                parts_all += w.x * parts;
+                top = max(top, (w.y + parts - 1) / parts);
+            }
+            lds_barrier();
+        }
+#pragma unroll
+        for (int d = SIZES; d < 64; d <<= 1) {
+            parts_all += __shfl_xor(parts_all, d);
+            top = max(top, __shfl_xor(top, d));
+        }
+        if ((tid & 63) < SIZES) {
+            atomicAdd(&count[i], parts_all);
+            atomicMax(&longest[i], top);
         }
         lds_barrier();
-        constexpr int COST = 4;   // of a workgroup's beginning and end, in records
-        long long best = 0x7fffffffffffffffLL;
+        // (the eight in neighbouring lanes; of equals the smaller size)
+        long long best = ((count[i] <= tile_goal ? 0 : (tile_all + (long long)COST * count[i]) / tile_goal) + longest[i] + COST) * SIZES + i;
 #pragma unroll
-        for (int i = 0; i < SIZES; ++i) {
-            const long long ends = (count[i] <= tile_goal ? 0 : (tile_all + (long long)COST * count[i]) / tile_goal) + longest[i] + COST;
-            if (ends < best) {
-                best = ends;
-                tile_chunk = size[i];
-            }
-        }
+        for (int d = 1; d < SIZES; d <<= 1) best = min(best, (long long)__shfl_xor(best, d));
+        tile_chunk = __shfl(size, (int)(best % SIZES));
     }
     // Tiles of few rows are listed by the length of their parts, longest first (in 64 steps; who is first in a step is left to chance and
     // shows in no result): the last workgroups to begin are then short ones.
