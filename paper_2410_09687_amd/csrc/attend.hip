@@ -5,18 +5,26 @@
 //
 // Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T: the codes are the A operand and a row of queries is a
 // COLUMN of the accumulators.  A lane then holds 16 scores of one query row per record of 64 tokens, the softmax's
-// statistics are its own but for two exchanges between the four lanes that share the row, the scores turn into the second product's B operand
+// statistics are its own, the scores turn into the second product's B operand
 // where they are (the contraction order over the keys is free: the keys of a lane's accumulators are taken as its slots), and the
-// rescaling of O^T is a product with the lane's own factor.  Nothing goes through LDS before the end.
+// rescaling of O^T is a product with the lane's own factor.  Scores and weights never leave the registers.
 //   K: lane (m, g) (m = lane % 16, g = lane / 16) takes row m of a tile of 16 keys, channels [D/4 g, D/4 g + D/4);
 //   V: word m of each key (8 channels), for the 4 keys 4 g .. 4 g + 3 of a tile: one 16-byte load, whose eight channels are rows m
 //      of eight accumulators.  (D = 64: words m % 8, the nibbles of half m / 8.)
 // Codes become bf16 exactly, two a conversion, the block's scale in the same instruction; V's pairs of channels are then regrouped into pairs
 // of keys, one v_perm a pair.  Scores, statistics and sums are fp32; the weights exp(s - m) are rounded to bf16 for the second product, for
-// fp32 results as the sum of three bf16.
+// fp32 results as the sum of three bf16; their sum is taken before.
 //
-// Bound by memory where a request adds one token (68 D bytes a record and kv head against 4 D flops a row and key); by the vector
-// unit's softmax in prompts.
+// Up to 32 rows of queries to a request and kv head (a token or a few): the workgroup's waves take the records in turn, each decodes its own,
+// and the work is cut along the keys until the chip is full.  Bound by memory: 68 D bytes a record and kv head against 4 D flops a row and key.
+// 256 requests of up to 4096 keys, 32 heads on 4 of 64 channels, 36 us: 4.1 TB/s; two of 100000 and more, 64 heads on 8 of 128, 66 us: 4.0 TB/s;
+// a thousand keys 7.1 us: four trips to memory.  (An even cut over a grid that stays: 47 - 52 us for the first, a piece's beginning and
+// end cost 4 to 6.)
+// More rows (prompts, chunks of them): tiles of 128, every wave has 32 rows and walks all records, a quarter of which it decodes into
+// LDS for the others.  Bound by the vector unit (eight prompts of 2048, 32 heads on 4 of 64 channels, 197 us, 0.70 PFLOP/s: busy 67 % of the
+// time, the matrix cores 29 %): the softmax's 16 fma, exp and sum and 8 packs a row and record, and the decoding.  Long prompts 0.91 PFLOP/s (64
+// channels), 1.05 (128).  A record's keys multiplied ahead, beside the weights of the one before: 272 us, the registers then hold two waves of a
+// SIMD instead of three.
 #include "kv.h"
 #include "mxfp4.h"
 
@@ -428,13 +436,14 @@ constexpr int min_waves()
 // The end of a workgroup whose tile has several parts, its own left in `partial`: whether it is the last of the tile's to report, which then joins
 // the parts, in their order.  What the parts leave are device-scope stores: a workgroup waits for its own before it reports, and nobody's L2
 // has to be written back.
-__device__ __forceinline__ bool last_of(const KvPlanView &v, const Work &k, int *flag)
+// `place`: which of the tile's tickets (it has as many as parts); `expected`: how many report there.
+__device__ __forceinline__ bool last_of(const KvPlanView &v, const Work &k, int place, int expected, int *flag)
 {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    int *ticket = v.tickets + (int64_t)(k.t.pslot + k.sub) * v.n_kv + k.h;   // (two parts or more: as many places)
+    int *ticket = v.tickets + (int64_t)(k.t.pslot + place) * v.n_kv + k.h;
     if (threadIdx.x == 0) {
-        *flag = atomicAdd(ticket, 1) == k.t.n_parts - 1;
+        *flag = atomicAdd(ticket, 1) == expected - 1;
         if (*flag) *ticket = 0;   // clean for the next call
     }
     __syncthreads();
@@ -699,7 +708,7 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_few
             if (ch == 0) put_agent(o, m, l);
         }
     }
-    if (!alone && last_of(v, k, &lds_last)) join_rows<D, ROWS>(p, k, c, factor);
+    if (!alone && last_of(v, k, k.sub, t.n_parts, &lds_last)) join_rows<D, ROWS>(p, k, c, factor);
 }
 
 // Tiles of many rows: every one of the four waves has 32 rows and walks all of the records, a quarter of which it decodes into LDS for
@@ -816,45 +825,63 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
         const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
         float *first_part = p.a.partial + ((int64_t)t.pslot * v.n_kv + k.h) * KV_TILE_ROWS * (D + 2);
         const int ml_at = KV_TILE_ROWS * D + (wave * 32 + n) * 2, o_at = (wave * 4 * NJ * 64 + lane) * 2;
-        float *mine = first_part + t.part * part_step;
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-            if (g == 0) put_agent(mine + ml_at + nt * 32, w.m[nt], w.l[nt]);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) put_agent(mine + o_at + ((nt * NJ + j) * 2 + e) * 128, w.o[nt][j][2 * e], w.o[nt][j][2 * e + 1]);
-        }
-        if (!last_of(v, k, &lds_last)) return;
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-            w.m[nt] = NEG_INF;
-            w.l[nt] = 0.f;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) w.o[nt][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        }
-        for (int u = 0; u < t.n_parts; ++u) {
-            const float *part = first_part + u * part_step;
+        auto leave = [&](int part) {
+            float *mine = first_part + part * part_step;
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt) {
-                const float2 ml = get_agent(part + ml_at + nt * 32);
-                float2 x[NJ][2];
+                if (g == 0) put_agent(mine + ml_at + nt * 32, w.m[nt], w.l[nt]);
 #pragma unroll
                 for (int j = 0; j < NJ; ++j)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) x[j][e] = get_agent(part + o_at + ((nt * NJ + j) * 2 + e) * 128);
-                const float top = fmaxf(w.m[nt], ml.x), base = top == NEG_INF ? 0.f : top * c;
-                const float f0 = __builtin_amdgcn_exp2f(fmaf(w.m[nt], c, -base)), f1 = __builtin_amdgcn_exp2f(fmaf(ml.x, c, -base));
-                w.m[nt] = top;
-                w.l[nt] = fmaf(ml.y, f1, w.l[nt] * f0);
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        w.o[nt][j][2 * e] = fmaf(x[j][e].x, f1, w.o[nt][j][2 * e] * f0);
-                        w.o[nt][j][2 * e + 1] = fmaf(x[j][e].y, f1, w.o[nt][j][2 * e + 1] * f0);
-                    }
+                    for (int e = 0; e < 2; ++e)
+                        put_agent(mine + o_at + ((nt * NJ + j) * 2 + e) * 128, w.o[nt][j][2 * e], w.o[nt][j][2 * e + 1]);
             }
+        };
+        auto join = [&](int from, int to, int step) {
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+                w.m[nt] = NEG_INF;
+                w.l[nt] = 0.f;
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) w.o[nt][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+            for (int u = from; u < to; u += step) {
+                const float *part = first_part + u * part_step;
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    const float2 ml = get_agent(part + ml_at + nt * 32);
+                    float2 x[NJ][2];
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) x[j][e] = get_agent(part + o_at + ((nt * NJ + j) * 2 + e) * 128);
+                    const float top = fmaxf(w.m[nt], ml.x), base = top == NEG_INF ? 0.f : top * c;
+                    const float f0 = __builtin_amdgcn_exp2f(fmaf(w.m[nt], c, -base)), f1 = __builtin_amdgcn_exp2f(fmaf(ml.x, c, -base));
+                    w.m[nt] = top;
+                    w.l[nt] = fmaf(ml.y, f1, w.l[nt] * f0);
+#pragma unroll
+                    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            w.o[nt][j][2 * e] = fmaf(x[j][e].x, f1, w.o[nt][j][2 * e] * f0);
+                            w.o[nt][j][2 * e + 1] = fmaf(x[j][e].y, f1, w.o[nt][j][2 * e + 1] * f0);
+                        }
+                }
+            }
+        };
+        // One workgroup reads parts at 1.5 us each: beyond eight they are joined in groups first, whose last ones to report join the
+        // groups (a prompt of 64 behind 30000 keys, 32 parts, 62 us; one after the other 104).
+        int many = t.n_parts;
+        if (t.n_parts > 8)
+            for (many = 3; many * many < t.n_parts;) ++many;
+        const int group0 = t.part - t.part % many, group_end = min(group0 + many, t.n_parts);
+        leave(t.part);
+        if (!last_of(v, k, 1 + group0 / many, group_end - group0, &lds_last)) return;
+        join(group0, group_end, 1);
+        if (many < t.n_parts) {
+            leave(group0);
+            if (!last_of(v, k, 0, (t.n_parts + many - 1) / many, &lds_last)) return;
+            join(0, t.n_parts, many);
         }
     }
 #pragma unroll
