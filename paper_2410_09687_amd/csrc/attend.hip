@@ -149,11 +149,11 @@ struct AttendK {
 // A workgroup's work: rows [t.row0, row_end) of a request's tile, one kv head, records [b0, b1).
 struct Work {
     KvTile t;
-    int h, sub, row_end;
+    int h, row_end;
     int pos0, first, last;   // positions of the request's first new token, and of the rows' first and last
     int window, b0, b1;
 
-    // False: nothing to do.  (A tile of the plan may be several workgroups', of `height` rows each.)
+    // False: nothing to do.  `height`: rows of a tile.
     __device__ __forceinline__ bool find(const AttendK &p, int height)
     {
         const KvPlanView &v = p.v;
@@ -164,9 +164,6 @@ struct Work {
         if (rec_id >= v.head[p.list]) return false;
         t = KvTile{uniform(ta.x), uniform(ta.y), uniform(ta.z), uniform(ta.w), uniform(tb.x), uniform(tb.y), uniform(tb.z), uniform(tb.w)};
         const int rows = t.n_tok * v.group;
-        sub = blockIdx.y;
-        t.row0 += sub * height;
-        if (t.row0 >= rows) return false;
         row_end = min(rows, t.row0 + height);
         pos0 = t.kv_len - t.n_tok;
         first = pos0 + t.row0 / v.group;
@@ -450,130 +447,95 @@ __device__ __forceinline__ bool last_of(const KvPlanView &v, const Work &k, int 
     return *flag;
 }
 
-// The join of a tile of few rows, a part's rows one after the other, {m, l, channels} each; 256 threads.
+// The groups in which a tile's parts are joined: one workgroup reads them at a microsecond or more each, so beyond eight they are joined in
+// groups first, whose last ones to report join the groups.  (A prompt of 64 behind 30000 keys, 32 parts, 62 us; one after the other 104.)
+struct Groups {
+    int size, first, last;   // parts of a whole group; the first of this part's, and behind its last
+    __device__ __forceinline__ explicit Groups(const KvTile &t)
+    {
+        size = t.n_parts;
+        if (t.n_parts > 8)
+            for (size = 3; size * size < t.n_parts;) ++size;
+        first = t.part - t.part % size;
+        last = min(first + size, t.n_parts);
+    }
+};
+
+// Joins parts from, from + step ... below `to` of a tile of few rows, a part's rows one after the other, {m, l, channels} each: to part `from`, or to y.
+// 256 threads, 16 to a row, everything of four parts on its way at once and of two rows a thread: a trip to memory for 32 rows.
 template <int D, int ROWS>
-__device__ __forceinline__ void join_rows(const AttendK &p, const Work &k, float c, float (*factor)[KV_MAX_PARTS + 1])
+__device__ __forceinline__ void join_rows(const AttendK &p, const Work &k, float c, int from, int to, int step, bool final)
 {
+    constexpr int CH = D / 16, AHEAD = 4, G = ROWS > 16 ? 2 : 1;   // CH: channels of a row per thread
     const KvPlanView &v = p.v;
     const KvTile &t = k.t;
-    const int tid = threadIdx.x, group = v.group, h = k.h, sub = k.sub, row_end = k.row_end;
-    constexpr int CH = D / 16;   // channels of a row per thread
+    const int row = threadIdx.x >> 4, ch = (threadIdx.x & 15) * CH, n_rows = k.row_end - t.row0;
     const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
-    const float *first_part = p.a.partial + (((int64_t)t.pslot * v.n_kv + h) * KV_TILE_ROWS + sub * ROWS) * (D + 2);
-    const int row = tid >> 4, sl = tid & 15, n_rows = row_end - t.row0;
-    if (t.n_parts <= 8) {
-        // 16 threads a row, everything of four parts on its way at once and of two rows a thread: a trip to memory for 32 rows, where the
-        // form below takes six.
-        constexpr int AHEAD = 4, G = ROWS > 16 ? 2 : 1;
-        const int ch = sl * CH;
-        for (int r0 = 0; r0 < n_rows; r0 += 16 * G) {
-            float m[G], l[G], x[G][CH];
+    float *tile = p.a.partial + ((int64_t)t.pslot * v.n_kv + k.h) * KV_TILE_ROWS * (D + 2);
+    for (int r0 = 0; r0 < n_rows; r0 += 16 * G) {
+        float m[G], l[G], x[G][CH];
+#pragma unroll
+        for (int z = 0; z < G; ++z) {
+            m[z] = NEG_INF;
+            l[z] = 0.f;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[z][i] = 0.f;
+        }
+        for (int u0 = from; u0 < to; u0 += AHEAD * step) {
+            float2 ml[G][AHEAD], a[G][AHEAD][CH / 2];
 #pragma unroll
             for (int z = 0; z < G; ++z) {
-                m[z] = NEG_INF;
-                l[z] = 0.f;
+                const float *o = tile + min(r0 + 16 * z + row, n_rows - 1) * (D + 2);
 #pragma unroll
-                for (int i = 0; i < CH; ++i) x[z][i] = 0.f;
-            }
-            for (int u0 = 0; u0 < t.n_parts; u0 += AHEAD) {
-                float2 ml[G][AHEAD], a[G][AHEAD][CH / 2];
+                for (int u = 0; u < AHEAD; ++u) {
+                    const float *part = o + (u0 + u * step < to ? u0 + u * step : from) * part_step;
+                    ml[z][u] = get_agent(part);
 #pragma unroll
-                for (int z = 0; z < G; ++z) {
-                    const float *o = first_part + min(r0 + 16 * z + row, n_rows - 1) * (D + 2);
-#pragma unroll
-                    for (int u = 0; u < AHEAD; ++u) {
-                        const float *part = o + min(u0 + u, t.n_parts - 1) * part_step;
-                        ml[z][u] = get_agent(part);
-#pragma unroll
-                        for (int i = 0; i < CH / 2; ++i) a[z][u][i] = get_agent(part + 2 + ch + 2 * i);
-                    }
-                }
-#pragma unroll
-                for (int z = 0; z < G; ++z) {
-                    float top = m[z];
-#pragma unroll
-                    for (int u = 0; u < AHEAD; ++u) top = fmaxf(top, ml[z][u].x);   // (the last part more than once: no harm to a maximum)
-                    const float base = top == NEG_INF ? 0.f : top * c;
-                    const float shrink = __builtin_amdgcn_exp2f(fmaf(m[z], c, -base));
-                    m[z] = top;
-                    l[z] *= shrink;
-#pragma unroll
-                    for (int i = 0; i < CH; ++i) x[z][i] *= shrink;
-#pragma unroll
-                    for (int u = 0; u < AHEAD; ++u) {
-                        if (u0 + u >= t.n_parts) break;
-                        const float f = __builtin_amdgcn_exp2f(fmaf(ml[z][u].x, c, -base));
-                        l[z] = fmaf(ml[z][u].y, f, l[z]);
-#pragma unroll
-                        for (int i = 0; i < CH / 2; ++i) {
-                            x[z][2 * i] = fmaf(a[z][u][i].x, f, x[z][2 * i]);
-                            x[z][2 * i + 1] = fmaf(a[z][u][i].y, f, x[z][2 * i + 1]);
-                        }
-                    }
+                    for (int i = 0; i < CH / 2; ++i) a[z][u][i] = get_agent(part + 2 + ch + 2 * i);
                 }
             }
 #pragma unroll
             for (int z = 0; z < G; ++z) {
-                if (r0 + 16 * z + row >= n_rows) continue;
+                float top = m[z];
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) top = fmaxf(top, ml[z][u].x);   // (one part more than once: no harm to a maximum)
+                const float base = top == NEG_INF ? 0.f : top * c;
+                const float shrink = __builtin_amdgcn_exp2f(fmaf(m[z], c, -base));
+                m[z] = top;
+                l[z] *= shrink;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) x[z][i] *= shrink;
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    if (u0 + u * step >= to) break;
+                    const float f = __builtin_amdgcn_exp2f(fmaf(ml[z][u].x, c, -base));
+                    l[z] = fmaf(ml[z][u].y, f, l[z]);
+#pragma unroll
+                    for (int i = 0; i < CH / 2; ++i) {
+                        x[z][2 * i] = fmaf(a[z][u][i].x, f, x[z][2 * i]);
+                        x[z][2 * i + 1] = fmaf(a[z][u][i].y, f, x[z][2 * i + 1]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int z = 0; z < G; ++z) {
+            const int local = r0 + 16 * z + row;
+            if (local >= n_rows) continue;
+            if (final) {
                 const float inv = inverse(l[z]);
 #pragma unroll
                 for (int i = 0; i < CH; ++i) x[z][i] *= inv;
-                const int64_t at = y_row(t, t.row0 + r0 + 16 * z + row, group, v.n_kv, h);
+                const int64_t at = y_row(t, t.row0 + local, v.group, v.n_kv, k.h);
                 store_y(p.a, at, D, ch, x[z]);
                 if (p.a.lse && ch == 0) p.a.lse[at] = log_sum(m[z], l[z], c);
+            } else {
+                float *o = tile + from * part_step + local * (D + 2);   // (nobody but the row's own threads reads it here, all of them before)
+#pragma unroll
+                for (int i = 0; i < CH; i += 2) put_agent(o + 2 + ch + i, x[z][i], x[z][i + 1]);
+                if (ch == 0) put_agent(o, m[z], l[z]);
             }
         }
-        return;
-    }
-    // More parts, 16 rows at a time: the factors of their parts into LDS (16 threads a row, each several parts), then the rows, several
-    // parts' loads at a time.
-    for (int r0 = 0; r0 < n_rows; r0 += 16) {
-        const int local = r0 + row, ch = sl * CH;
-        const bool real = local < n_rows;
-        const float *o = first_part + (real ? local : 0) * (D + 2);
-        float m = NEG_INF, l = 0.f, x[CH];
-        for (int u = sl; u < t.n_parts; u += 16) m = fmaxf(m, get_agent(o + u * part_step).x);
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-        const float base = m == NEG_INF ? 0.f : m * c;
-        if (r0) lds_barrier();
-        for (int u = sl; u < t.n_parts; u += 16) {
-            const float2 ml = get_agent(o + u * part_step);
-            const float f = __builtin_amdgcn_exp2f(fmaf(ml.x, c, -base));
-            factor[row][u] = f;
-            l = fmaf(ml.y, f, l);
-        }
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) l += __shfl_xor(l, d);
-        lds_barrier();
-        if (!real) continue;
-#pragma unroll
-        for (int i = 0; i < CH; ++i) x[i] = 0.f;
-        o += 2 + ch;
-        constexpr int AHEAD = 64 / CH;   // parts whose loads are on their way together
-        for (int u0 = 0; u0 < t.n_parts; u0 += AHEAD) {
-            float2 ahead[AHEAD][CH / 2];
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u)
-#pragma unroll
-                for (int i = 0; i < CH / 2; ++i) ahead[u][i] = get_agent(o + min(u0 + u, t.n_parts - 1) * part_step + 2 * i);
-#pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                if (u0 + u >= t.n_parts) break;
-                const float f = factor[row][u0 + u];
-#pragma unroll
-                for (int i = 0; i < CH / 2; ++i) {
-                    x[2 * i] = fmaf(ahead[u][i].x, f, x[2 * i]);
-                    x[2 * i + 1] = fmaf(ahead[u][i].y, f, x[2 * i + 1]);
-                }
-            }
-        }
-        const float inv = inverse(l);
-#pragma unroll
-        for (int i = 0; i < CH; ++i) x[i] *= inv;
-        const int64_t at = y_row(t, t.row0 + local, group, v.n_kv, h);
-        store_y(p.a, at, D, ch, x);
-        if (p.a.lse && ch == 0) p.a.lse[at] = log_sum(m, l, c);
     }
 }
 
@@ -608,7 +570,6 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_few
     static_assert(CW * KW == 4, "the join's threads: 16 rows of 16");
     __shared__ float lds_o[KW][16][LDO];
     __shared__ float lds_ml[KW][16][2];
-    __shared__ float factor[16][KV_MAX_PARTS + 1];
     __shared__ int lds_last;
     const KvPlanView &v = p.v;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), kw = wave % KW, cw = wave / KW, n = lane & 15, g = lane >> 4;
@@ -659,7 +620,7 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_few
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) w.l[nt] = sum4(w.l[nt]);
 
-    float *part_o = p.a.partial + (((int64_t)(t.pslot + t.part) * v.n_kv + k.h) * KV_TILE_ROWS + k.sub * ROWS) * (D + 2);
+    float *part_o = p.a.partial + (((int64_t)(t.pslot + t.part) * v.n_kv + k.h) * KV_TILE_ROWS) * (D + 2);
     const bool alone = t.n_parts == 1;
     const int row = tid >> 4, ch = (tid & 15) * CH;
     for (int ct = 0; ct < CW * NT; ++ct) {
@@ -708,7 +669,12 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_few
             if (ch == 0) put_agent(o, m, l);
         }
     }
-    if (!alone && last_of(v, k, k.sub, t.n_parts, &lds_last)) join_rows<D, ROWS>(p, k, c, factor);
+    if (alone) return;
+    const Groups of(t);
+    if (!last_of(v, k, 1 + of.first / of.size, of.last - of.first, &lds_last)) return;
+    join_rows<D, ROWS>(p, k, c, of.first, of.last, 1, of.size == t.n_parts);
+    if (of.size < t.n_parts && last_of(v, k, 0, (t.n_parts + of.size - 1) / of.size, &lds_last))
+        join_rows<D, ROWS>(p, k, c, 0, t.n_parts, of.size, true);
 }
 
 // Tiles of many rows: every one of the four waves has 32 rows and walks all of the records, a quarter of which it decodes into LDS for
@@ -869,19 +835,14 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
                 }
             }
         };
-        // One workgroup reads parts at 1.5 us each: beyond eight they are joined in groups first, whose last ones to report join the
-        // groups (a prompt of 64 behind 30000 keys, 32 parts, 62 us; one after the other 104).
-        int many = t.n_parts;
-        if (t.n_parts > 8)
-            for (many = 3; many * many < t.n_parts;) ++many;
-        const int group0 = t.part - t.part % many, group_end = min(group0 + many, t.n_parts);
+        const Groups of(t);
         leave(t.part);
-        if (!last_of(v, k, 1 + group0 / many, group_end - group0, &lds_last)) return;
-        join(group0, group_end, 1);
-        if (many < t.n_parts) {
-            leave(group0);
-            if (!last_of(v, k, 0, (t.n_parts + many - 1) / many, &lds_last)) return;
-            join(0, t.n_parts, many);
+        if (!last_of(v, k, 1 + of.first / of.size, of.last - of.first, &lds_last)) return;
+        join(of.first, of.last, 1);
+        if (of.size < t.n_parts) {
+            leave(of.first);
+            if (!last_of(v, k, 0, (t.n_parts + of.size - 1) / of.size, &lds_last)) return;
+            join(0, t.n_parts, of.size);
         }
     }
 #pragma unroll
@@ -906,10 +867,9 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
 }
 
 template <int D, int NT, int CW, int KW, bool Y32>
-void launch_few(const AttendK &p, int rows, hipStream_t stream)
+void launch_few(const AttendK &p, hipStream_t stream)
 {
-    constexpr int ROWS = 16 * NT * CW;
-    hipLaunchKernelGGL((attend_few_kernel<D, NT, CW, KW, Y32>), dim3((unsigned)p.v.max_few * p.v.n_kv, (unsigned)(rows / ROWS)), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((attend_few_kernel<D, NT, CW, KW, Y32>), dim3((unsigned)p.v.max_few * p.v.n_kv), dim3(256), 0, stream, p);
 }
 
 template <int D, bool Y32>
@@ -918,8 +878,8 @@ hipError_t launch_d(const KvPlanView &v, const AttendArgs &a, hipStream_t stream
     constexpr bool WIDE = D == 256;   // two columns of accumulators would leave no registers for the rest
     AttendK p{v, a, 0};
     if (v.has_few) {
-        if (std::min(v.max_new * (int64_t)v.group, (int64_t)KV_FEW_ROWS) <= 16) launch_few<D, 1, 1, 4, Y32>(p, 16, stream);
-        else launch_few<D, WIDE ? 1 : 2, WIDE ? 2 : 1, WIDE ? 2 : 4, Y32>(p, KV_FEW_ROWS, stream);
+        if (std::min(v.max_new * (int64_t)v.group, (int64_t)KV_FEW_ROWS) <= 16) launch_few<D, 1, 1, 4, Y32>(p, stream);
+        else launch_few<D, WIDE ? 1 : 2, WIDE ? 2 : 1, WIDE ? 2 : 4, Y32>(p, stream);
     }
     if (v.has_tile) {
         p.list = 1;

@@ -37,7 +37,7 @@ constexpr int KV_FEW_TOKENS = 8;
 // Workgroups aimed at per launch where the keys allow, two for every compute unit, and the fewest records of a part.  (Two requests of 100000 keys 65 us, with
 // 768 75, with 1024 80; 8 prompts of 128 behind 2000 keys 55, with 768 68.  One request of 4000 keys 8.5, with 16 records and more 10.5; a
 // prompt of 128 behind 3000 20.0, with 4 and more 28, with 16 23.7.)
-constexpr int KV_FEW_TARGET = 512, KV_FEW_MIN = 4;
+constexpr int KV_FEW_TARGET = 512, KV_FEW_MIN = 8;
 constexpr int KV_TILE_TARGET = 512, KV_TILE_MIN = 8;
 constexpr int KV_MAX_PARTS = 128;  // of a tile
 
