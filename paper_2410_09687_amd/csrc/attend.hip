@@ -17,8 +17,8 @@
 //
 // Up to 32 rows of queries to a request and kv head (a token or a few): the workgroup's waves take the records in turn, each decodes its own,
 // and the work is cut along the keys until the chip is full.  Bound by memory: 68 D bytes a record and kv head against 4 D flops a row and key.
-// 256 requests of up to 4096 keys, 32 heads on 4 of 64 channels, 36 us: 4.1 TB/s; two of 100000 and more, 64 heads on 8 of 128, 66 us: 4.0 TB/s;
-// a thousand keys 7.1 us: four trips to memory.  (An even cut over a grid that stays: 47 - 52 us for the first, a piece's beginning and
+// 256 requests of up to 4096 keys, 32 heads on 4 of 64 channels, 35 us: 4.3 TB/s; two of 100000 and more, 64 heads on 8 of 128, 61 us: 4.3 TB/s;
+// a thousand keys 7.6 us: half a dozen trips to memory.  (An even cut over a grid that stays: 47 - 52 us for the first, a piece's beginning and
 // end cost 4 to 6.)
 // More rows (prompts, chunks of them): tiles of 128, every wave has 32 rows and walks all records, a quarter of which it decodes into
 // LDS for the others.  Bound by the vector unit (eight prompts of 2048, 32 heads on 4 of 64 channels, 197 us, 0.70 PFLOP/s: busy 67 % of the

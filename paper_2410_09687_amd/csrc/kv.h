@@ -32,13 +32,15 @@ struct KvPages {
 // (Rows 32: 64 requests of 2000 keys and 4 tokens, 32 heads on 4 of 64 channels, 19.5 us as one tile of few rows, 36 as tiles of 128; 32 heads on 8 of
 // 128, 8 tokens 41 and 76.)
 constexpr int KV_FEW_ROWS = 32, KV_TILE_ROWS = 128;
-// Up to here (new tokens of a request) the plan is one launch: 64 requests of 4 tokens 7.0 us, 9.4 in two; of 32 tokens 15.3 and 11.5.
+// Up to here (new tokens of a request) the plan is one launch: 64 requests of 4 tokens 7.0 us, 9.4 in two; of 32 tokens 16.0 and 11.5.
 constexpr int KV_FEW_TOKENS = 8;
-// Workgroups aimed at per launch where the keys allow, two for every compute unit, and the fewest records of a part.  (Two requests of 100000 keys 65 us, with
-// 768 75, with 1024 80; 8 prompts of 128 behind 2000 keys 55, with 768 68.  One request of 4000 keys 8.5, with 16 records and more 10.5; a
-// prompt of 128 behind 3000 20.0, with 4 and more 28, with 16 23.7.)
-constexpr int KV_FEW_TARGET = 512, KV_FEW_MIN = 8;
-constexpr int KV_TILE_TARGET = 512, KV_TILE_MIN = 8;
+// Workgroups aimed at per launch where the keys allow, two for every compute unit.  Us with 384 / 512 / 768 / 1024: two requests of 100000 keys and
+// more 67 / 61 / 71 / 70, 256 of up to 4096 34.7 / 34.8 / 37 / 39, 64 of 2000 13.7 / 13.8 / 14.8 / 18.5.  Tiles of 128 with 512 / 768: 8 prompts of 128
+// behind 2000 keys 55 / 68.
+constexpr int KV_FEW_TARGET = 512, KV_TILE_TARGET = 512;
+// The fewest records of a part.  Us with 4 / 8 / 16: one request of 1000 keys 7.0 / 7.6 / 7.3, of 4000 9.1 / 8.6 / 9.3, four of 8000 and 4 tokens 19.5 / 13.8 /
+// 14.7, 16 of 2000 and 3 tokens 14.0 / 11.2 / 13.4; a prompt of 128 behind 3000 28 / 20 / 24, of 64 behind 500 12.5 / 14.2 / 15.8.
+constexpr int KV_FEW_MIN = 8, KV_TILE_MIN = 8;
 constexpr int KV_MAX_PARTS = 128;  // of a tile
 
 struct KvTile {            // one workgroup's work, per kv head
