@@ -593,6 +593,8 @@ int64_t moin_kv_page_bytes(int32_t page_tokens, int32_t n_kv, int32_t head_dim);
  *   seq_offsets [S+1] int32 out: the requests' tokens in the batch (as moin_plan_build takes)
  *   slots [T]     int32 out: page * page_tokens + place in the page of every new token
  *   n_heads, n_kv        query heads (a multiple of n_kv) and kv heads of the attention
+ * Without requests (S = 0, T = 0) n_free_out and seq_offsets are written all the same; the arrays of
+ * no elements may be NULL.
  * A request that needs more pages than are left, as the requests before it take theirs, or than
  * its row holds gets none: its length stays, its slots are -1, its attention rows are zeros, and the
  * sticky data fault is raised.  So it is for lengths that are negative or above max_new, and for

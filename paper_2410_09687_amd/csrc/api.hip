@@ -1692,7 +1692,13 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
     v.max_pages = max_pages;
     v.page_tokens = page_tokens;
     if (S == 0) {
-        if (T != 0) return MOIN_EINVAL;
+        if (T != 0 || !n_free || !n_free_out || !seq_offsets) return MOIN_EINVAL;
+        DeviceGuard guard(ctx->device);
+        if (!guard.ok) return MOIN_EHIP;
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        if (timed(ctx, MOIN_K_KV_PLAN, st, [&] { return launch_kv_plan_empty(n_free, free_cap, n_free_out, seq_offsets, ctx->err_word, st); }) !=
+            hipSuccess)
+            return MOIN_EHIP;
         plan->built = 1;
         return MOIN_OK;
     }

@@ -74,6 +74,7 @@ struct KvPlanArgs {
     int *err_word;
 };
 hipError_t launch_kv_plan(const KvPlanView &v, const KvPlanArgs &a, hipStream_t stream);
+hipError_t launch_kv_plan_empty(const int *n_free, int free_cap, int *n_free_out, int *seq_offsets, int *err_word, hipStream_t stream);
 hipError_t launch_kv_release(const int *finished, int S, int *kv_lens, int *block_table, int max_pages, int page_tokens, int *free_pages,
                              int *n_free, int free_cap, int n_pages, int *err_word, hipStream_t stream);
 // k / v: [T, n_kv, D] bf16, rows of tokens k_stride / v_stride elements apart

@@ -67,6 +67,23 @@ __device__ __forceinline__ void kv_write_tile(KvTile *dst, int tok0, int n_tok, 
     d[1] = make_int4(row0, part, n_parts, pslot);
 }
 
+// Height of the stack of free pages, of at most its room.
+__device__ __forceinline__ int free_pages_there(int n_free, int free_cap, int &err)
+{
+    if (n_free < 0 || n_free > free_cap) err |= ERR_NO_PAGES;
+    return max(0, min(n_free, free_cap));
+}
+
+// A step without requests.
+__global__ __launch_bounds__(64) void kv_plan_empty_kernel(const int *n_free, int free_cap, int *n_free_out, int *seq_offsets, int *err_word)
+{
+    if (threadIdx.x) return;
+    int err = 0;
+    *n_free_out = free_pages_there(*n_free, free_cap, err);
+    *seq_offsets = 0;
+    if (err) atomicOr(err_word, err);
+}
+
 // One workgroup walks the requests, PT at a time, twice.  First: offsets (a sum over the new tokens), pages to deal (a sum over
 // the pages that each request lacks), which requests are served.  Then, with the keys of all requests known, the
 // size of the parts that fill the chip and everybody's place in the lists.  Up to KV_FEW_TOKENS new tokens a
@@ -80,12 +97,8 @@ __global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a,
     const int tid = threadIdx.x;
     if (tid == 0) lds_err = 0;
     for (int i = tid; i < v.max_pslots * v.n_kv; i += PT) v.tickets[i] = 0;
-    int n_free = *a.n_free;
     int err = 0;
-    if (n_free < 0 || n_free > a.free_cap) {
-        err |= ERR_NO_PAGES;
-        n_free = max(0, min(n_free, a.free_cap));
-    }
+    const int n_free = free_pages_there(*a.n_free, a.free_cap, err);
     const long long row_max = (long long)a.max_pages << log_page;
     long long tok_base = 0;
     int page_base = 0, taken = 0;
@@ -314,6 +327,12 @@ static int log2_of(int v)
     int s = 0;
     while ((1 << s) < v) ++s;
     return s;
+}
+
+hipError_t launch_kv_plan_empty(const int *n_free, int free_cap, int *n_free_out, int *seq_offsets, int *err_word, hipStream_t stream)
+{
+    hipLaunchKernelGGL(kv_plan_empty_kernel, dim3(1), dim3(64), 0, stream, n_free, free_cap, n_free_out, seq_offsets, err_word);
+    return hipGetLastError();
 }
 
 hipError_t launch_kv_plan(const KvPlanView &v, const KvPlanArgs &a, hipStream_t stream)
