@@ -1712,9 +1712,10 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
     hipStream_t st = static_cast<hipStream_t>(stream);
     v.max_new = (int)std::min<int64_t>(max_new, T);
     v.has_tile = (int64_t)v.max_new * group > KV_FEW_ROWS;
-    // (tokens that every request has at least, as none has more than max_new)
+    // Without faults in the lengths every request has at least this many tokens, as none has more than max_new: beyond the rows of a tile of
+    // few there is no launch for those, and what faults leave of short requests is listed with the others.
     const int64_t least = T - (int64_t)(S - 1) * v.max_new;
-    v.has_few = least * group <= KV_FEW_ROWS && group <= KV_FEW_ROWS;
+    v.has_few = group <= KV_FEW_ROWS && (least * group <= KV_FEW_ROWS || !v.has_tile);
     // parts of at least 1 / goal of a list's records each: no more than the goal beside the tiles themselves, and
     // tiles of several parts have at most twice that many
     const int few_goal = std::max(1, KV_FEW_TARGET / n_kv), tile_goal = std::max(1, KV_TILE_TARGET / n_kv);

@@ -67,6 +67,9 @@ __device__ __forceinline__ void kv_write_tile(KvTile *dst, int tok0, int n_tok, 
     d[1] = make_int4(row0, part, n_parts, pslot);
 }
 
+// Whether a request's rows are tiles of many: also few rows where the launch for those is left out.
+__device__ __forceinline__ bool kv_tiled(const KvPlanView &v, int64_t rows) { return rows > (v.has_few ? KV_FEW_ROWS : 0); }
+
 // Height of the stack of free pages, of at most its room.
 __device__ __forceinline__ int free_pages_there(int n_free, int free_cap, int &err)
 {
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a,
             // (a request that is not served has no keys: its rows come out as zeros)
             const int64_t rows = (int64_t)n * v.group;
             const int blocks = served ? ceil_shift(kv + n0, 6) : 0;
-            if (rows > KV_FEW_ROWS) {
+            if (kv_tiled(v, rows)) {
                 const int own = (int)min((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS, (int64_t)KV_TILE_TARGET);   // (as many fill the chip alone)
                 tiles += own;
                 tile_blocks += (long long)own * blocks;
@@ -195,7 +198,7 @@ __global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a,
             if (s < v.S) {
                 const int4 q = v.req[s];   // (what this thread wrote in the first walk)
                 const int64_t rows = (int64_t)q.w * v.group;
-                if (rows > KV_FEW_ROWS)
+                if (kv_tiled(v, rows))
                     own = make_int2((int)min((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS, (int64_t)KV_TILE_TARGET), q.y >= 0 ? ceil_shift(q.x + q.w, 6) : 0);
             }
             work[tid] = own;
@@ -238,7 +241,7 @@ __global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a,
     };
     auto parts_of = [&](int L, int size) { return min(KV_MAX_PARTS, max(1, (ceil_shift(L, 6) + size - 1) / size)); };
     auto step_of = [&](int L, int parts) { return 63 - min(63, (ceil_shift(L, 6) + parts - 1) / parts * 63 / few_chunk); };
-    auto is_few = [&](int n) { return n > 0 && (int64_t)n * v.group <= KV_FEW_ROWS; };
+    auto is_few = [&](int n) { return n > 0 && !kv_tiled(v, (int64_t)n * v.group); };
     if (v.has_few) {
         for (int s = tid; s < v.S; s += PT) {
             int tok0, n, L;
@@ -270,7 +273,7 @@ __global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a,
         int tok0 = 0, n = 0, L = 0;
         if (in) work_of(s, tok0, n, L);
         const int64_t rows = (int64_t)n * v.group;
-        const bool few = is_few(n) && v.has_few, tiled = rows > KV_FEW_ROWS && v.has_tile;
+        const bool few = is_few(n) && v.has_few, tiled = kv_tiled(v, rows) && v.has_tile;
         const int n_tiles = tiled ? (int)((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS) : few ? 1 : 0;
         const int parts = parts_of(L, tiled ? tile_chunk : few_chunk);
         const int recs = n_tiles * parts, ps = parts > 1 ? recs : 0;
