@@ -1725,14 +1725,18 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
     v.max_few = (int)few;
     v.max_tile = (int)tiles;
     v.max_pslots = (v.has_few ? 2 * few_goal : 0) + (v.has_tile ? 2 * tile_goal : 0);
+    // The buffer is that of any step of up to these requests and tokens: a smaller one may have the list that this one lacks.
+    const bool few_any = group <= KV_FEW_ROWS;
+    const int64_t few_room = few_any ? (int64_t)S + few_goal : 0;
+    const int64_t ticket_room = (few_any ? 2 * few_goal : 0) + (v.has_tile ? 2 * tile_goal : 0);
     size_t off = 0;
     auto take = [&](size_t bytes) {
         const size_t at = off;
         off = align_up(off + bytes, 256);
         return at;
     };
-    const size_t o_head = take(16), o_req = take((size_t)S * 16), o_rt = take((size_t)S * 8), o_few = take((size_t)few * sizeof(KvTile)),
-                 o_tile = take((size_t)tiles * sizeof(KvTile)), o_tick = take((size_t)v.max_pslots * n_kv * 4);
+    const size_t o_head = take(16), o_req = take((size_t)S * 16), o_rt = take((size_t)S * 8), o_few = take((size_t)few_room * sizeof(KvTile)),
+                 o_tile = take((size_t)tiles * sizeof(KvTile)), o_tick = take((size_t)ticket_room * n_kv * 4);
     const int rc = plan_grow(plan, off, st);
     if (rc != MOIN_OK) return rc;
     char *b = static_cast<char *>(plan->buf);
