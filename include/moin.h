@@ -643,7 +643,8 @@ int moin_kv_gather(moin_ctx *ctx, const moin_kv_pages *pages, const int32_t *slo
  * product as bf16, for fp32 results as the sum of three bf16.  A call repeated gives the same bits.
  * `plan` is of moin_kv_plan_build with the same n_heads and n_kv and the block_table it filled;
  * pages that the cache does not have raise the sticky data fault and count as unseen.
- * Workspace: partial results of keys that are walked in parts.  Errors: MOIN_EINVAL (null, a plan that
+ * Workspace: partial results of keys that are walked in parts; an eager call sizes it for any step of at
+ * most its plan's requests, tokens and max_new.  Errors: MOIN_EINVAL (null, a plan that
  * is not built, head counts that differ, sizes, alignment), MOIN_ENOMEM, MOIN_ECAPTURE. */
 int moin_kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pages *pages, const void *q, int64_t q_stride,
                       int32_t n_heads, const int32_t *block_table, int32_t max_pages, float scale, int32_t window, void *y,

@@ -1728,7 +1728,7 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
     // The buffer is that of any step of up to these requests and tokens: a smaller one may have the list that this one lacks.
     const bool few_any = group <= KV_FEW_ROWS;
     const int64_t few_room = few_any ? (int64_t)S + few_goal : 0;
-    const int64_t ticket_room = (few_any ? 2 * few_goal : 0) + (v.has_tile ? 2 * tile_goal : 0);
+    v.room_pslots = (few_any ? 2 * few_goal : 0) + (v.has_tile ? 2 * tile_goal : 0);
     size_t off = 0;
     auto take = [&](size_t bytes) {
         const size_t at = off;
@@ -1736,7 +1736,7 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
         return at;
     };
     const size_t o_head = take(16), o_req = take((size_t)S * 16), o_rt = take((size_t)S * 8), o_few = take((size_t)few_room * sizeof(KvTile)),
-                 o_tile = take((size_t)tiles * sizeof(KvTile)), o_tick = take((size_t)ticket_room * n_kv * 4);
+                 o_tile = take((size_t)tiles * sizeof(KvTile)), o_tick = take((size_t)v.room_pslots * n_kv * 4);
     const int rc = plan_grow(plan, off, st);
     if (rc != MOIN_OK) return rc;
     char *b = static_cast<char *>(plan->buf);
@@ -1827,7 +1827,8 @@ int moin_kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pag
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return MOIN_EHIP;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int rc = ensure_ws(ctx, (size_t)attend_partial_floats(v, a.pages.D) * 4, st);
+    const int rc = ensure_ws(ctx, (size_t)attend_partial_floats(v, v.max_pslots, a.pages.D) * 4, st, false,
+                             (size_t)attend_partial_floats(v, v.room_pslots, a.pages.D) * 4);
     if (rc != MOIN_OK) return rc;
     if (capturing(st)) plan->pinned = 1;
     a.q = q;

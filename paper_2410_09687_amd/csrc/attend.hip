@@ -890,9 +890,9 @@ hipError_t launch_d(const KvPlanView &v, const AttendArgs &a, hipStream_t stream
 
 }  // namespace
 
-int64_t attend_partial_floats(const KvPlanView &v, int D)
+int64_t attend_partial_floats(const KvPlanView &v, int pslots, int D)
 {
-    return (int64_t)v.max_pslots * v.n_kv * KV_TILE_ROWS * (D + 2);
+    return (int64_t)pslots * v.n_kv * KV_TILE_ROWS * (D + 2);
 }
 
 hipError_t launch_attend(const KvPlanView &v, const AttendArgs &a, hipStream_t stream)

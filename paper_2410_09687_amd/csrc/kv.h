@@ -61,6 +61,7 @@ struct KvPlanView {
     int S, n_kv, group, max_new, max_pages, page_tokens;
     int64_t T;
     int max_few, max_tile, max_pslots;
+    int room_pslots;       // the most of any step of up to these requests and tokens
     bool has_few, has_tile;
 };
 
@@ -95,8 +96,8 @@ struct AttendArgs {
     float *partial;        // attend_partial_floats()
     int *err_word;
 };
-// fp32 words of partial results that a plan's calls need.
-int64_t attend_partial_floats(const KvPlanView &v, int D);
+// fp32 words of that many partial results.
+int64_t attend_partial_floats(const KvPlanView &v, int pslots, int D);
 hipError_t launch_attend(const KvPlanView &v, const AttendArgs &a, hipStream_t stream);
 
 constexpr int ERR_BAD_LENGTHS = 16;   // lengths that are negative, beyond the table's rows, or do not add up to the tokens

@@ -89,3 +89,8 @@ def captured(first, then, max_new, heads, H, D, whole):
 @pytest.mark.parametrize("first,then,max_new,heads,H,D", CASES)
 def test_a_plan_captured_after_the_largest_eager_one(first, then, max_new, heads, H, D):
     captured(first, then, max_new, heads, H, D, False)
+
+
+@pytest.mark.parametrize("first,then,max_new,heads,H,D", CASES)
+def test_attention_captured_after_the_largest_eager_step(first, then, max_new, heads, H, D):
+    captured(first, then, max_new, heads, H, D, True)
