@@ -370,6 +370,25 @@ size_t linear_ws_most(const PlanView &pv, int n, int d_in, const int32_t *d_out,
     return std::max({tiled, small, large});
 }
 
+// The same for a call on an MXFP4 base: gathered batches, multiplied with the codes, keep one plane, row tiles the weight in bf16.  Of the
+// batches of up to the plan's sequences and tokens, one sequence of all of them takes row tiles if any does.
+size_t mx4_ws_most(const PlanView &pv, int d_in, int d_out, int r)
+{
+    LinearArgs a;
+    a.d_in = d_in;
+    a.r = r;
+    const int64_t T = pv.T;
+    const auto planes = [&](int ldu) { return 2 * align_up((size_t)T * (size_t)ldu * 2, 256); };
+    const size_t gathered = pv.decode ? planes(r) + align_up((size_t)T * (size_t)d_out * 4, 256) : 0;
+    const PlanLayout L = plan_layout(1, T, pv.E);
+    PlanView one = pv;
+    one.S = 1;
+    one.decode = L.decode;
+    one.tiles = L.tiles;
+    if (gathered_pays(one, d_in, r)) return gathered;
+    return std::max(gathered, align_up((size_t)d_out * (size_t)d_in * 2, 256) + planes(prefill_ldu(a)));
+}
+
 // The plan's buffer, at least `bytes` large; same rules under stream capture as ensure_ws.
 template <class Plan>
 int plan_grow(Plan *plan, size_t bytes, hipStream_t st)
@@ -506,7 +525,7 @@ int linear_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, con
     const bool direct = mx4 && (gathered || a.r == 0);
     const size_t w_bytes = mx4 && !direct ? align_up((size_t)d_out * (size_t)d_in * 2, 256) : 0;
     const auto reserve = [&](size_t bytes) -> int {
-        const int rc = ensure_ws(ctx, w_bytes + bytes, stream, false, w_bytes + linear_ws_most(pv, 1, d_in, &d_out, r));
+        const int rc = ensure_ws(ctx, w_bytes + bytes, stream, false, mx4 ? mx4_ws_most(pv, d_in, d_out, r) : linear_ws_most(pv, 1, d_in, &d_out, r));
         if (rc != MOIN_OK || !w_bytes) return rc;
         const hipError_t e = timed(ctx, MOIN_K_MX4_LINEAR, stream, [&] { return launch_mx4_dequantize(W, d_out, d_in, ctx->ws, stream); });
         a.W = ctx->ws;
