@@ -615,7 +615,8 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
 
 /* Requests with finished[s] != 0 (int32) give their pages back: pushed on the stack in the
  * requests' order, their table entries become -1 and their lengths 0, n_free counts them.
- * Pages that do not exist or do not fit the stack raise the sticky data fault. */
+ * Pages that do not exist or do not fit the stack raise the sticky data fault and are left out.
+ * Entries of free_pages from n_free on may be anything afterwards. */
 int moin_kv_release(moin_ctx *ctx, const int32_t *finished, int32_t S, int32_t *kv_lens, int32_t page_tokens,
                     int32_t n_pages, int32_t *block_table, int32_t max_pages, int32_t *free_pages, int32_t free_cap,
                     int32_t *n_free, void *stream);
