@@ -1701,7 +1701,7 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
     if (S < 0 || T < 0 || max_new < 0 || free_cap < 0 || n_kv < 1 || n_kv > (1 << 16) || n_heads < n_kv || n_heads % n_kv) return MOIN_EINVAL;
     if (!page_tokens_ok(page_tokens) || n_pages < 1 || (int64_t)n_pages * page_tokens > 0x7fffffffLL) return MOIN_EINVAL;
     const int group = n_heads / n_kv;
-    if (group > 0xffff || T * group > 0x7fffffffLL - KV_TILE_ROWS) return MOIN_EINVAL;
+    if (group > 0xffff || T > 0x7fffffffLL || T * group > 0x7fffffffLL - KV_TILE_ROWS) return MOIN_EINVAL;
     KvPlanView &v = plan->v;
     v = KvPlanView{};
     v.S = S;
@@ -1721,7 +1721,7 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
         plan->built = 1;
         return MOIN_OK;
     }
-    if (max_pages < 1 || (int64_t)S * max_pages * (page_tokens / KV_BLOCK) > 0x7fffffffLL || (int64_t)max_pages * page_tokens > 0x7fffffffLL)
+    if (max_pages < 1 || (int64_t)max_pages * page_tokens > 0x7fffffffLL || (int64_t)S * max_pages * (page_tokens / KV_BLOCK) > 0x7fffffffLL)
         return MOIN_EINVAL;
     if (!kv_lens || !new_lens || !block_table || (!free_pages && free_cap > 0) || !n_free || !n_free_out || !kv_lens_out || !seq_offsets ||
         (!slots && T > 0))
