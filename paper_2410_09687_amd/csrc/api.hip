@@ -1743,11 +1743,11 @@ int moin_kv_plan_build(moin_ctx *ctx, moin_kv_plan *plan, const int32_t *kv_lens
     if ((few + tiles) * n_kv > 0x7fffffffLL) return MOIN_EINVAL;
     v.max_few = (int)few;
     v.max_tile = (int)tiles;
-    v.max_pslots = (v.has_few ? 2 * few_goal : 0) + (v.has_tile ? 2 * tile_goal : 0);
+    v.max_pslots = (v.has_few ? 2 * few_goal : 0) + (v.has_tile ? 2 * tile_goal * KV_TILE_PLACES : 0);
     // The buffer is that of any step of up to these requests and tokens: a smaller one may have the list that this one lacks.
     const bool few_any = group <= KV_FEW_ROWS;
     const int64_t few_room = few_any ? (int64_t)S + few_goal : 0;
-    v.room_pslots = (few_any ? 2 * few_goal : 0) + (v.has_tile ? 2 * tile_goal : 0);
+    v.room_pslots = (few_any ? 2 * few_goal : 0) + (v.has_tile ? 2 * tile_goal * KV_TILE_PLACES : 0);
     size_t off = 0;
     auto take = [&](size_t bytes) {
         const size_t at = off;

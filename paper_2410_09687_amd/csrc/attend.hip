@@ -470,8 +470,8 @@ __device__ __forceinline__ void join_rows(const AttendK &p, const Work &k, float
     const KvPlanView &v = p.v;
     const KvTile &t = k.t;
     const int row = threadIdx.x >> 4, ch = (threadIdx.x & 15) * CH, n_rows = k.row_end - t.row0;
-    const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
-    float *tile = p.a.partial + ((int64_t)t.pslot * v.n_kv + k.h) * KV_TILE_ROWS * (D + 2);
+    const int64_t part_step = (int64_t)v.n_kv * KV_FEW_ROWS * (D + 2);
+    float *tile = p.a.partial + ((int64_t)t.pslot * v.n_kv + k.h) * KV_FEW_ROWS * (D + 2);
     for (int r0 = 0; r0 < n_rows; r0 += 16 * G) {
         float m[G], l[G], x[G][CH];
 #pragma unroll
@@ -620,7 +620,7 @@ __global__ __launch_bounds__(64 * CW * KW, (min_waves<D, NT>())) void attend_few
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) w.l[nt] = sum4(w.l[nt]);
 
-    float *part_o = p.a.partial + (((int64_t)(t.pslot + t.part) * v.n_kv + k.h) * KV_TILE_ROWS) * (D + 2);
+    float *part_o = p.a.partial + (((int64_t)(t.pslot + t.part) * v.n_kv + k.h) * KV_FEW_ROWS) * (D + 2);
     const bool alone = t.n_parts == 1;
     const int row = tid >> 4, ch = (tid & 15) * CH;
     for (int ct = 0; ct < CW * NT; ++ct) {
@@ -789,7 +789,7 @@ __global__ __launch_bounds__(256, (D == 256 ? 1 : 2)) void attend_tile_kernel(At
     if (t.n_parts > 1) {
         // A part's results lie as the lanes have them: whole lines, and the join needs no order of rows.
         const int64_t part_step = (int64_t)v.n_kv * KV_TILE_ROWS * (D + 2);
-        float *first_part = p.a.partial + ((int64_t)t.pslot * v.n_kv + k.h) * KV_TILE_ROWS * (D + 2);
+        float *first_part = p.a.partial + ((int64_t)t.pslot * v.n_kv * KV_FEW_ROWS + k.h * KV_TILE_ROWS) * (D + 2);
         const int ml_at = KV_TILE_ROWS * D + (wave * 32 + n) * 2, o_at = (wave * 4 * NJ * 64 + lane) * 2;
         auto leave = [&](int part) {
             float *mine = first_part + part * part_step;
@@ -892,7 +892,7 @@ hipError_t launch_d(const KvPlanView &v, const AttendArgs &a, hipStream_t stream
 
 int64_t attend_partial_floats(const KvPlanView &v, int pslots, int D)
 {
-    return (int64_t)pslots * v.n_kv * KV_TILE_ROWS * (D + 2);
+    return (int64_t)pslots * v.n_kv * KV_FEW_ROWS * (D + 2);
 }
 
 hipError_t launch_attend(const KvPlanView &v, const AttendArgs &a, hipStream_t stream)

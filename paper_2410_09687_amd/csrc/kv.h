@@ -32,6 +32,8 @@ struct KvPages {
 // (Rows 32: 64 requests of 2000 keys and 4 tokens, 32 heads on 4 of 64 channels, 19.5 us as one tile of few rows, 36 as tiles of 128; 32 heads on 8 of
 // 128, 8 tokens 41 and 76.)
 constexpr int KV_FEW_ROWS = 32, KV_TILE_ROWS = 128;
+// Partial results are counted in places of KV_FEW_ROWS rows: a part of a tile of few rows takes one, of the others as many as here.
+constexpr int KV_TILE_PLACES = KV_TILE_ROWS / KV_FEW_ROWS;
 // Up to here (new tokens of a request) the plan is one launch: 64 requests of 4 tokens 7.0 us, 9.4 in two; of 32 tokens 16.0 and 11.5.
 constexpr int KV_FEW_TOKENS = 8;
 // Workgroups aimed at per launch where the keys allow, two for every compute unit.  Us with 384 / 512 / 768 / 1024: two requests of 100000 keys and
@@ -55,7 +57,7 @@ struct KvTile {            // one workgroup's work, per kv head
 struct KvPlanView {
     int *head;             // [4]: records of either list; free pages before the step
     int4 *req;             // [S] {keys before, first of its pages among those the step deals or -1, pages dealt, first record in `tile`}
-    int2 *req_tiles;       // [S] {parts of each of its tiles, first partial slot}
+    int2 *req_tiles;       // [S] {parts of each of its tiles, first place of their partial results}
     KvTile *few, *tile;
     int *tickets;          // [max_pslots * n_kv], zero between calls
     int S, n_kv, group, max_new, max_pages, page_tokens;
@@ -96,7 +98,7 @@ struct AttendArgs {
     float *partial;        // attend_partial_floats()
     int *err_word;
 };
-// fp32 words of that many partial results.
+// fp32 words of that many places of partial results.
 int64_t attend_partial_floats(const KvPlanView &v, int pslots, int D);
 hipError_t launch_attend(const KvPlanView &v, const AttendArgs &a, hipStream_t stream);
 

@@ -276,7 +276,7 @@ __global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a,
         const bool few = is_few(n) && v.has_few, tiled = kv_tiled(v, rows) && v.has_tile;
         const int n_tiles = tiled ? (int)((rows + KV_TILE_ROWS - 1) / KV_TILE_ROWS) : few ? 1 : 0;
         const int parts = parts_of(L, tiled ? tile_chunk : few_chunk);
-        const int recs = n_tiles * parts, ps = parts > 1 ? recs : 0;
+        const int recs = n_tiles * parts, ps = parts > 1 ? recs * (tiled ? KV_TILE_PLACES : 1) : 0;
         const Scan2 up = block_scan<PT>(Scan2{tiled ? recs : 0, ps}, lds, t2);
         const int tile_at = tile_base + (int)up.a - (tiled ? recs : 0), ps_at = ps_base + up.b - ps;
         if (few) {
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a,
             for (int t = 0; t < n_tiles; ++t)   // the last rows see the most keys: their tiles first
                 for (int p = 0; p < parts; ++p)
                     kv_write_tile(v.tile + tile_at + t * parts + p, tok0, n, L, s, (n_tiles - 1 - t) * KV_TILE_ROWS, p, parts,
-                                  ps_at + (parts > 1 ? t * parts : 0));
+                                  ps_at + (parts > 1 ? t * parts * KV_TILE_PLACES : 0));
         tile_base += (int)t2.a;
         ps_base += t2.b;
     }
@@ -318,10 +318,10 @@ __global__ __launch_bounds__(256) void kv_slots_kernel(KvPlanView v, KvPlanArgs 
     const int L = served ? kv + n : 0;
     const int2 t2 = v.req_tiles[s];
     const int parts = t2.x, n_tiles = (int)(((int64_t)n * v.group + KV_TILE_ROWS - 1) / KV_TILE_ROWS), recs = n_tiles * parts;
-    if (q.w + recs > v.max_tile || (parts > 1 && t2.y + recs > v.max_pslots)) return;
+    if (q.w + recs > v.max_tile || (parts > 1 && t2.y + recs * KV_TILE_PLACES > v.max_pslots)) return;
     for (int r = c * 256 + tid; r < recs; r += nc * 256) {
         const int t = r / parts, p = r - t * parts;
-        kv_write_tile(v.tile + q.w + r, tok0, n, L, s, (n_tiles - 1 - t) * KV_TILE_ROWS, p, parts, t2.y + (parts > 1 ? t * parts : 0));
+        kv_write_tile(v.tile + q.w + r, tok0, n, L, s, (n_tiles - 1 - t) * KV_TILE_ROWS, p, parts, t2.y + (parts > 1 ? t * parts * KV_TILE_PLACES : 0));
     }
 }
 
