@@ -13,17 +13,22 @@
 //      of eight accumulators.  (D = 64: words m % 8, the nibbles of half m / 8.)
 // Codes become bf16 exactly, two a conversion, the block's scale in the same instruction; V's pairs of channels are then regrouped into pairs
 // of keys, one v_perm a pair.  Scores, statistics and sums are fp32; the weights exp(s - m) are rounded to bf16 for the second product, for
-// fp32 results as the sum of three bf16; their sum is taken before.
+// fp32 results as the sum of three bf16; their sum is taken before.  For bf16 results one it is: beside the result's own rounding it shows
+// little, and two cost more than they give (error against 64 bits and us, one / two: 256 requests 1.644e-3 and 35.0 / 1.609e-3 and 36.6, 8 tokens at
+// 128 channels 1.756e-3 and 40.9 / 1.732e-3 and 46.2, prompts 1.729e-3 and 196 / 1.626e-3 and 258).
 //
 // Up to 32 rows of queries to a request and kv head (a token or a few): the workgroup's waves take the records in turn, each decodes its own,
 // and the work is cut along the keys until the chip is full.  Bound by memory: 68 D bytes a record and kv head against 4 D flops a row and key.
 // 256 requests of up to 4096 keys, 32 heads on 4 of 64 channels, 35 us: 4.3 TB/s; two of 100000 and more, 64 heads on 8 of 128, 61 us: 4.3 TB/s;
 // a thousand keys 7.6 us: half a dozen trips to memory.  (An even cut over a grid that stays: 47 - 52 us for the first, a piece's beginning and
-// end cost 4 to 6.)
+// end cost 4 to 6.)  A few tokens a request: 64 requests of 2000 keys and 4 tokens, 32 heads on 4 of 64, 18.2 us (floor 7.4), 8 tokens, 32 on 8 of 128,
+// 40.8 (29.5), where a wave's two columns leave a SIMD one wave.
 // More rows (prompts, chunks of them): tiles of 128, every wave has 32 rows and walks all records, a quarter of which it decodes into
-// LDS for the others.  Bound by the vector unit (eight prompts of 2048, 32 heads on 4 of 64 channels, 197 us, 0.70 PFLOP/s: busy 67 % of the
-// time, the matrix cores 29 %): the softmax's 16 fma, exp and sum and 8 packs a row and record, and the decoding.  Long prompts 0.91 PFLOP/s (64
-// channels), 1.05 (128).  A record's keys multiplied ahead, beside the weights of the one before: 272 us, the registers then hold two waves of a
+// LDS for the others.  Bound by the vector unit (eight prompts of 2048, 32 heads on 4 of 64 channels, 196 us, 0.70 PFLOP/s: busy 76 % of the
+// cycles in which a compute unit has work, the matrix cores 32 %).  265 vector instructions a wave and record by the counters: 32 of the matrix cores, 181 of the
+// others where every row sees the record and the reference stays (the softmax's fma, exp and sum of 32 scores a lane 104, packs 18, decoding 49), and some 50
+// for the rest: a tile's first record, whose weights are computed twice, its last one's masks, its beginning and end with
+// their divisions.  Long prompts 0.91 PFLOP/s (64 channels), 1.05 (128); fp32 results 339 us; heads of 256 channels 241 for the same products.  A record's keys multiplied ahead, beside the weights of the one before: 272 us, the registers then hold two waves of a
 // SIMD instead of three.
 #include "kv.h"
 #include "mxfp4.h"

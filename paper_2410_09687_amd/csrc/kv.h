@@ -40,7 +40,8 @@ constexpr int KV_FEW_TOKENS = 8;
 // more 67 / 61 / 71 / 70, 256 of up to 4096 34.7 / 34.8 / 37 / 39, 64 of 2000 13.7 / 13.8 / 14.8 / 18.5.  Tiles of 128 with 512 / 768: 8 prompts of 128
 // behind 2000 keys 55 / 68.
 constexpr int KV_FEW_TARGET = 512, KV_TILE_TARGET = 512;
-// The fewest records of a part.  Us with 4 / 8 / 16: one request of 1000 keys 7.0 / 7.6 / 7.3, of 4000 9.1 / 8.6 / 9.3, four of 8000 and 4 tokens 19.5 / 13.8 /
+// The fewest records of a part, of all the keys that a request has: a window is the attention's own, which divides what it leaves among the same
+// parts, so that short windows of long requests have parts of fewer records or of none.  Us with 4 / 8 / 16: one request of 1000 keys 7.0 / 7.6 / 7.3, of 4000 9.1 / 8.6 / 9.3, four of 8000 and 4 tokens 19.5 / 13.8 /
 // 14.7, 16 of 2000 and 3 tokens 14.0 / 11.2 / 13.4; a prompt of 128 behind 3000 28 / 20 / 24, of 64 behind 500 12.5 / 14.2 / 15.8.
 constexpr int KV_FEW_MIN = 8, KV_TILE_MIN = 8;
 constexpr int KV_MAX_PARTS = 128;  // of a tile

@@ -344,6 +344,7 @@ constexpr int MX4_VECTOR_MAX_T = 4;
 //  17 to 32: 2048 -> 2048 4.3 / 4.7 / 7.9, 2048 -> 5632 8.3 / 5.0 / 8.4, 8192 -> 8192 22.4 / 15.5 / 28.6, 8192 -> 28672 81 / 60 / 35
 //  64: 2048 -> 2048 6.9 / 11.0 / 17, 5632 -> 2048 16.2 / 27 / 47, 8192 -> 28672 69 / 43.6 / 73
 //  256: 2048 -> 2048 7.9 / 11.5 / 17, 2048 -> 5632 21 / 13.3 / 20, 8192 -> 8192 65 / 45 / 69, 8192 -> 28672 - / 150 / 108 (1.1 PFLOP/s)
+//  (8192 -> 28672 at 17 to 32 tokens is 224 workgroups, one a compute unit: 32 units have none, and the codes come at 3.6 TB/s)
 //  1024: 2048 -> 2048 22 / 14.6 / 20.5, 2048 -> 5632 - / 38 / 32, 8192 -> 8192 - / 160 / 108, 8192 -> 28672 - / - / 390 (1.23 PFLOP/s)
 hipError_t launch_mx4_linear(const void *x, const void *W, void *y, int y_f32, int64_t T, int d_in, int d_out, hipStream_t stream)
 {
