@@ -81,7 +81,9 @@ typedef enum {
     MOIN_K_KV_APPEND = 16,    /* tokens into the paged cache, and back             */
     MOIN_K_KV_ATTEND = 17,    /* attention over the paged cache                    */
     MOIN_K_MX4_LINEAR = 18,   /* MXFP4 base: y = x Wq^T from the codes, or Wq to bf16 */
-    MOIN_K_COUNT = 19
+    MOIN_K_QK_ROTATE = 19,    /* norms and rotation of queries and keys            */
+    MOIN_K_I8_LINEAR = 20,    /* integer base: y = s_t s_o xq Wq^T                 */
+    MOIN_K_COUNT = 21
 } moin_kernel_id;
 
 /* ---- context ----------------------------------------------------------- */
@@ -650,6 +652,80 @@ int moin_kv_gather(moin_ctx *ctx, const moin_kv_pages *pages, const int32_t *slo
 int moin_kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pages *pages, const void *q, int64_t q_stride,
                       int32_t n_heads, const int32_t *block_table, int32_t max_pages, float scale, int32_t window, void *y,
                       moin_dtype y_dt, float *lse, void *stream);
+
+/* ==== serving in eight bits ========================================================
+ * The same step where four bits lose too much: the base weight in 8-bit integers, the cache in E4M3. */
+
+/* ---- norms and rotation of queries and keys --------------------------------------
+ * Between the projections and the cache: for token t and each head of q and of k,
+ *     x' = gain * x / sqrt(mean_c x_c^2 + eps)                        with MOIN_QK_NORM, else x' = x
+ *     (a, b) -> (a cos w - b sin w, b cos w + a sin w),  w = positions[t] * freqs[i]
+ * for pair i < rot_dim / 2 of its first rot_dim channels: channels (i, i + rot_dim / 2), with
+ * MOIN_QK_NEIGHBOURS (2 i, 2 i + 1); the others pass.  rot_dim = 0: no rotation.
+ *   q [T, n_heads, head_dim], k [T, n_kv, head_dim]  x_dt; q_out, k_out the same shapes, bf16; rows of
+ *             tokens `stride` elements apart (multiples of 8, of 4 for fp32 inputs), so that they may be columns of one
+ *             projection's output.  n_heads or n_kv may be 0 (q or k alone).  The outputs may be the inputs
+ *             themselves, with their strides, else they must not overlap them
+ *   positions [T] int32 (any), freqs [rot_dim / 2] double: radians a position.  NULL without rotation
+ *   q_gain, k_gain [head_dim] bf16 or NULL (ones; without MOIN_QK_NORM they must be)
+ * head_dim 64, 128 or 256; rot_dim a multiple of 16; pointers 16-byte aligned.  Angles are reduced in 64 bits;
+ * sums, norms and the rotation are fp32, the result is rounded once.  No workspace.
+ * Errors: MOIN_EINVAL. */
+#define MOIN_QK_NORM 1
+#define MOIN_QK_NEIGHBOURS 2
+int moin_qk_norm_rope(moin_ctx *ctx, const void *q, const void *k, moin_dtype x_dt, int64_t q_stride, int64_t k_stride, int64_t T,
+                      int32_t n_heads, int32_t n_kv, int32_t head_dim, const int32_t *positions, const double *freqs, int32_t rot_dim,
+                      int32_t flags, const void *q_gain, const void *k_gain, float eps, void *q_out, void *k_out, int64_t q_out_stride,
+                      int64_t k_out_stride, void *stream);
+
+/* ---- paged cache in E4M3 -----------------------------------------------------------
+ * As the MXFP4 cache above -- the same pages, plans, block tables, slots and releases -- in 8-bit values that share a power of
+ * two 2^(E-127) (byte E) for each 64 tokens x head, one for the keys and one for the values.  E4M3: bias 7, largest value
+ * 448, no infinities.  A page (moin_kv8_page_bytes) holds [n_kv][page_tokens / 64] records of 64 tokens, 128 D bytes each: channel 64 l + c of the
+ * keys of token 16 i + m at [i][l][m][c] (i < 4, m < 16, c < 64), channel 16 j + m of the values of token 16 w + 4 g + e (w, g, e < 4)
+ * at [j][m][g][w][e] from byte 64 D on; behind the records the bytes E, [n_kv][page_tokens / 64][2].
+ * E is the smallest, 10 to 246, in whose unit the largest magnitude of what was appended to the block is below 464; elements
+ * are rounded to nearest, ties to even (2.98e38 and more becomes 448 units).  Where later tokens ask
+ * for a larger E, what the block holds is rounded again.  A block that was given a NaN or an infinity has E = 255
+ * and stands for NaNs: 64 tokens of the head's keys or of its values.  E never falls before the block begins anew: with a
+ * token at its place 0.  Every other value is exact in bf16. */
+int64_t moin_kv8_page_bytes(int32_t page_tokens, int32_t n_kv, int32_t head_dim);
+
+/* moin_kv8_append: as moin_kv_append; seq_offsets [S+1] and slots [T] are a plan's (moin_kv_plan_build): the tokens of
+ * request s, from seq_offsets[s] on, follow one another in its pages.  A request whose first slot is -1 is skipped.  Offsets that run
+ * backwards, a first slot that the cache does not have, a later block whose slots do not follow each other or whose page does not
+ * exist raise the sticky data fault; such a request or block is left as it was.  No two requests may append to one block.
+ * moin_kv8_gather: as moin_kv_gather, any slots. */
+int moin_kv8_append(moin_ctx *ctx, const moin_kv_pages *pages, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
+                    int64_t T, const int32_t *seq_offsets, int32_t S, const int32_t *slots, void *stream);
+int moin_kv8_gather(moin_ctx *ctx, const moin_kv_pages *pages, const int32_t *slots, int64_t T, void *k, void *v, void *stream);
+
+/* moin_kv_attention over such a cache: the same arguments, results and errors.  A block of NaNs makes the rows that see a key of
+ * it NaN (its keys: lse, too), and no others. */
+int moin_kv8_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pages *pages, const void *q, int64_t q_stride,
+                       int32_t n_heads, const int32_t *block_table, int32_t max_pages, float scale, int32_t window, void *y,
+                       moin_dtype y_dt, float *lse, void *stream);
+
+/* ---- base weight in 8-bit integers ---------------------------------------------------
+ * Rows of a matrix have a scale each: s = max(amax / 127, 2^-126), rounded to fp32; code = x / s to the nearest, ties to
+ * even.  A row that holds a NaN or an infinity has s = NaN and codes of 0, and stands for NaNs.
+ *   moin_i8_pitch        bytes of a row of codes: cols padded with zeros to a multiple of 128, 256 at least (0: sizes that
+ *                        are not supported)
+ *   moin_i8_quantize     src [rows, cols] bf16 -> codes [rows, pitch] int8, scales [rows] fp32
+ *   moin_i8_linear       y [T, d_out] = s_t s_o sum_c xq wq, any T: x [T, d_in] bf16 is quantised by the call, a scale
+ *                        for each token; Wq [d_out, pitch], ws [d_out] from moin_i8_quantize, a scale for each channel.
+ *                        Sums are exact (int32) and rounded to fp32 once.
+ *   moin_lora_linear_i8_planned
+ *                        moin_lora_linear_planned on such a base: the adapters' products are those of the bf16 x.
+ * cols / d_in a multiple of 8 up to 131072, d_out of 8, r of 64; pointers 16-byte aligned (src, codes, ws too).  Stacks,
+ * y, workspace (the tokens' codes, 2 T r bf16, planes of partial sums) and errors as in moin_lora_linear_mx_planned. */
+int64_t moin_i8_pitch(int64_t cols);
+int moin_i8_quantize(moin_ctx *ctx, const void *src, int64_t rows, int64_t cols, void *codes, float *scales, void *stream);
+int moin_i8_linear(moin_ctx *ctx, const void *x, int64_t T, const void *Wq, const float *ws, int32_t d_in, int32_t d_out, void *y,
+                   moin_dtype y_dt, void *stream);
+int moin_lora_linear_i8_planned(moin_ctx *ctx, const moin_plan *plan, const void *x, const void *Wq, const float *ws, const void *A_stack,
+                                const void *B_stack, int32_t d_in, int32_t d_out, int32_t r, float scale, void *y, moin_dtype y_dt,
+                                void *stream);
 
 /* ==== measurement aids (not part of the method's path) =========================== */
 

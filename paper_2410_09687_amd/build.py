@@ -16,13 +16,13 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libmoin.so")
 BINDING = os.path.join(HERE, "_moin_binding.so")
 SOURCES = ["api.hip", "plan.hip", "linear.hip", "linear_stream.hip", "linear_mid.hip", "decode.hip", "route.hip", "route_exact.hip", "kmeans.hip", "cache.hip", "mx.hip", "probe.hip", "merge.hip",
-           "kv.hip", "attend.hip", "mx4.hip"]
+           "kv.hip", "attend.hip", "mx4.hip", "kv8.hip", "attend8.hip", "rotate.hip", "i8.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-# attend.hip: accumulators that the vector unit rescales and reads all the time stay in vector registers (a tenth of the
+# attend.hip, attend8.hip: accumulators that the vector unit rescales and reads all the time stay in vector registers (a tenth of the
 # instructions were moves to and from the accumulation registers)
-FILE_FLAGS = {"attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+FILE_FLAGS = {name: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for name in ("attend.hip", "attend8.hip")}
 
 
 def _start_binding():

@@ -12,6 +12,7 @@
 
 #include "kernels.h"
 #include "kv.h"
+#include "kv8.h"
 
 namespace moin {
 hipError_t prepare_linear_kernels();
@@ -707,6 +708,75 @@ int linear_mx_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, 
             return launch_linear_mx_stream(pv, m, compute_units(), stream);
         }) != hipSuccess)
         return MOIN_EHIP;
+    return MOIN_OK;
+}
+
+// Base in 8-bit integers: the tokens' codes into the workspace, then as on the MXFP8 base.
+int linear_i8_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, const void *Wq, const float *ws, const void *A_stack,
+                           const void *B_stack, int32_t d_in, int32_t d_out, int32_t r, float scale, void *y, moin_dtype y_dt,
+                           hipStream_t stream)
+{
+    const PlanView &pv = plan->pv;
+    if (capturing(stream)) plan->pinned = 1;
+    const bool adapters = pv.E > 0 && r > 0;
+    MxLinearArgs m;
+    LinearArgs &a = m.lin;
+    a.x = x; a.W = nullptr; a.A_stack = A_stack; a.B_stack = B_stack;
+    a.y = y; a.y_f32 = (y_dt == MOIN_F32);
+    a.d_in = d_in; a.d_out = d_out; a.r = adapters ? r : 0; a.scale = scale; a.act = ctx->act;
+    a.u_hi = a.u_lo = nullptr;
+    a.ldu = a.r;                          // (a multiple of 64 here)
+    m.Wq = Wq;
+    m.Ws = ws;
+    m.plain_splits = 0;
+    m.plain_kb_per_split = 0;
+    const int pitch = i8_pitch(d_in);
+    const size_t u_bytes = align_up((size_t)pv.T * (size_t)a.r * 2, 256), xq_bytes = align_up((size_t)pv.T * (size_t)pitch, 256),
+                 xs_bytes = align_up((size_t)pv.T * 4, 256);
+    const bool gathered = gathered_pays_mx(pv, d_in, d_out, a.r), decode = gathered && a.r > 0;
+    const bool few = gathered && pv.T <= I8_FEW_TOKENS, quantised = !(few && i8_few_quantises(pv.T, d_in));
+    size_t yb_bytes = 0;
+    if (decode) {
+        if (few) m.plain_splits = 1;
+        else mx_plain_shape(pv.T, pitch, d_out, &m.plain_splits, &m.plain_kb_per_split);
+        yb_bytes = align_up((size_t)m.plain_splits * (size_t)pv.T * (size_t)d_out * 4, 256);
+    } else if (gathered) {
+        m.plain_splits = 1;            // no adapters anywhere: the plain product writes y itself
+        m.plain_kb_per_split = pitch / 128;
+    }
+    const size_t head_bytes = 2 * u_bytes + xq_bytes + xs_bytes;
+    const size_t yb_most = pv.decode && a.r > 0 ? align_up((size_t)mx_plain_rows(pv.T, pitch, d_out) * (size_t)d_out * 4, 256) : 0;
+    const int rc = ensure_ws(ctx, head_bytes + yb_bytes, stream, false, head_bytes + yb_most);
+    if (rc != MOIN_OK) return rc;
+    char *w = static_cast<char *>(ctx->ws);
+    a.u_hi = w;
+    a.u_lo = w + u_bytes;
+    char *xq = w + 2 * u_bytes;
+    float *xs = reinterpret_cast<float *>(xq + xq_bytes);
+    m.xq = xq;
+    m.xs = xs;
+    if (quantised && timed(ctx, MOIN_K_MX_QUANT, stream, [&] { return launch_i8_quantize(x, pv.T, d_in, xq, xs, stream); }) != hipSuccess)
+        return MOIN_EHIP;
+    auto base = [&](void *out, int f32) {
+        if (few) return launch_i8_few(x, xq, xs, Wq, ws, (int)pv.T, d_in, d_out, out, f32, stream);
+        m.lin.y = out;
+        m.lin.y_f32 = f32;
+        return launch_linear_i8_stream(pv, m, compute_units(), stream);
+    };
+    if (decode) {
+        DecodeArgs d;
+        d.lin = a;
+        d.ug_hi = a.u_hi;
+        d.ug_lo = a.u_lo;
+        d.ybase = reinterpret_cast<float *>(w + head_bytes);
+        d.k_splits = m.plain_splits;
+        if (timed(ctx, MOIN_K_I8_LINEAR, stream, [&] { return base(d.ybase, 1); }) != hipSuccess) return MOIN_EHIP;
+        if (timed(ctx, MOIN_K_DECODE_SHRINK, stream, [&] { return launch_decode_shrink(pv, d, stream); }) != hipSuccess) return MOIN_EHIP;
+        if (timed(ctx, MOIN_K_DECODE_EXPAND, stream, [&] { return launch_decode_expand(pv, d, stream); }) != hipSuccess) return MOIN_EHIP;
+        return MOIN_OK;
+    }
+    if (a.r > 0 && timed(ctx, MOIN_K_SHRINK, stream, [&] { return launch_prefill_shrink(pv, a, stream); }) != hipSuccess) return MOIN_EHIP;
+    if (timed(ctx, MOIN_K_I8_LINEAR, stream, [&] { return base(y, y_dt == MOIN_F32); }) != hipSuccess) return MOIN_EHIP;
     return MOIN_OK;
 }
 
@@ -1828,9 +1898,9 @@ int moin_kv_gather(moin_ctx *ctx, const moin_kv_pages *pages, const int32_t *slo
     return timed(ctx, MOIN_K_KV_APPEND, st, [&] { return launch_kv_gather(p, k, v, T, slots, ctx->err_word, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
 }
 
-int moin_kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pages *pages, const void *q, int64_t q_stride, int32_t n_heads,
-                      const int32_t *block_table, int32_t max_pages, float scale, int32_t window, void *y, moin_dtype y_dt, float *lse,
-                      void *stream)
+static int kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pages *pages, const void *q, int64_t q_stride, int32_t n_heads,
+                        const int32_t *block_table, int32_t max_pages, float scale, int32_t window, void *y, moin_dtype y_dt, float *lse,
+                        void *stream, hipError_t (*launch)(const KvPlanView &, const AttendArgs &, hipStream_t))
 {
     if (!ctx || !plan || plan->device != ctx->device || !plan->built) return MOIN_EINVAL;
     AttendArgs a;
@@ -1861,7 +1931,171 @@ int moin_kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pag
     a.lse = lse;
     a.partial = static_cast<float *>(ctx->ws);
     a.err_word = ctx->err_word;
-    return timed(ctx, MOIN_K_KV_ATTEND, st, [&] { return launch_attend(v, a, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+    return timed(ctx, MOIN_K_KV_ATTEND, st, [&] { return launch(v, a, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+}
+
+int moin_kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pages *pages, const void *q, int64_t q_stride, int32_t n_heads,
+                      const int32_t *block_table, int32_t max_pages, float scale, int32_t window, void *y, moin_dtype y_dt, float *lse,
+                      void *stream)
+{
+    return kv_attention(ctx, plan, pages, q, q_stride, n_heads, block_table, max_pages, scale, window, y, y_dt, lse, stream, launch_attend);
+}
+
+// ---- serving in eight bits ------------------------------------------------------
+
+int64_t moin_kv8_page_bytes(int32_t page_tokens, int32_t n_kv, int32_t head_dim)
+{
+    if (moin_kv_page_bytes(page_tokens, n_kv, head_dim) == 0) return 0;
+    return kv8_page_bytes(KvPages{nullptr, 0, n_kv, head_dim, log2_exact(page_tokens / KV_BLOCK)});
+}
+
+int moin_kv8_append(moin_ctx *ctx, const moin_kv_pages *pages, const void *k, const void *v, int64_t k_stride, int64_t v_stride, int64_t T,
+                    const int32_t *seq_offsets, int32_t S, const int32_t *slots, void *stream)
+{
+    KvPages p;
+    if (!ctx || S < 0) return MOIN_EINVAL;
+    const int rc = validate_kv_rows(pages, &p, k, v, T, slots);
+    if (rc != MOIN_OK) return rc;
+    if (T == 0 || S == 0) return T == 0 ? MOIN_OK : MOIN_EINVAL;
+    if (!seq_offsets) return MOIN_EINVAL;
+    const int64_t row = (int64_t)p.n_kv * p.D;
+    if (k_stride % 8 || v_stride % 8 || k_stride < row || v_stride < row || k_stride > ((int64_t)1 << 31) || v_stride > ((int64_t)1 << 31)) return MOIN_EINVAL;
+    if ((T / 64 + 2 * (int64_t)S) * 2 * p.n_kv > 0x7fffffffLL) return MOIN_EINVAL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return timed(ctx, MOIN_K_KV_APPEND, st, [&] {
+               return launch_kv8_append(p, k, v, k_stride, v_stride, T, seq_offsets, S, slots, ctx->err_word, st);
+           }) == hipSuccess
+               ? MOIN_OK
+               : MOIN_EHIP;
+}
+
+int moin_kv8_gather(moin_ctx *ctx, const moin_kv_pages *pages, const int32_t *slots, int64_t T, void *k, void *v, void *stream)
+{
+    KvPages p;
+    if (!ctx) return MOIN_EINVAL;
+    const int rc = validate_kv_rows(pages, &p, k, v, T, slots);
+    if (rc != MOIN_OK || T == 0) return rc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return timed(ctx, MOIN_K_KV_APPEND, st, [&] { return launch_kv8_gather(p, k, v, T, slots, ctx->err_word, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+}
+
+int moin_kv8_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pages *pages, const void *q, int64_t q_stride, int32_t n_heads,
+                       const int32_t *block_table, int32_t max_pages, float scale, int32_t window, void *y, moin_dtype y_dt, float *lse,
+                       void *stream)
+{
+    return kv_attention(ctx, plan, pages, q, q_stride, n_heads, block_table, max_pages, scale, window, y, y_dt, lse, stream, launch_attend8);
+}
+
+int moin_qk_norm_rope(moin_ctx *ctx, const void *q, const void *k, moin_dtype x_dt, int64_t q_stride, int64_t k_stride, int64_t T, int32_t n_heads,
+                      int32_t n_kv, int32_t head_dim, const int32_t *positions, const double *freqs, int32_t rot_dim, int32_t flags,
+                      const void *q_gain, const void *k_gain, float eps, void *q_out, void *k_out, int64_t q_out_stride, int64_t k_out_stride,
+                      void *stream)
+{
+    if (!ctx || T < 0 || n_heads < 0 || n_kv < 0 || n_heads + (int64_t)n_kv < 1 || n_heads + (int64_t)n_kv > (1 << 16) || !kv_head_dim_ok(head_dim))
+        return MOIN_EINVAL;
+    if ((x_dt != MOIN_BF16 && x_dt != MOIN_F32) || (flags & ~(MOIN_QK_NORM | MOIN_QK_NEIGHBOURS)) || rot_dim < 0 || rot_dim > head_dim || rot_dim % 16)
+        return MOIN_EINVAL;
+    const bool norm = flags & MOIN_QK_NORM;
+    if (norm && (!(eps > 0.f) || eps > 3.0e38f)) return MOIN_EINVAL;
+    if (!norm && (q_gain || k_gain)) return MOIN_EINVAL;
+    if (T > 0x7fffffffLL || T * (n_heads + (int64_t)n_kv) > (int64_t)1 << 33) return MOIN_EINVAL;
+    if (T == 0) return MOIN_OK;
+    const int64_t mult = x_dt == MOIN_BF16 ? 8 : 4, far = (int64_t)1 << 31;
+    auto rows_ok = [&](const void *in, const void *out, int64_t stride, int64_t out_stride, int32_t heads) {
+        if (heads == 0) return true;
+        const int64_t row = (int64_t)heads * head_dim;
+        return in && out && !misaligned(in, 16) && !misaligned(out, 16) && stride % mult == 0 && out_stride % 8 == 0 && stride >= row &&
+               out_stride >= row && stride <= far && out_stride <= far;
+    };
+    if (!rows_ok(q, q_out, q_stride, q_out_stride, n_heads) || !rows_ok(k, k_out, k_stride, k_out_stride, n_kv)) return MOIN_EINVAL;
+    if (rot_dim > 0 && (!positions || !freqs || misaligned(freqs, 8))) return MOIN_EINVAL;
+    if (misaligned(q_gain, 16) || misaligned(k_gain, 16)) return MOIN_EINVAL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const RotateArgs a{q, k, q_stride, k_stride, T, x_dt == MOIN_F32, n_heads, n_kv, head_dim, positions, freqs, rot_dim, (flags & MOIN_QK_NEIGHBOURS) != 0,
+                       norm, q_gain, k_gain, eps, q_out, k_out, q_out_stride, k_out_stride};
+    return timed(ctx, MOIN_K_QK_ROTATE, st, [&] { return launch_qk_norm_rope(a, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+}
+
+static bool i8_sizes_ok(int64_t rows, int64_t cols) { return rows >= 0 && rows <= 0x7fffffffLL && cols > 0 && cols % 8 == 0 && cols <= I8_MAX_COLS; }
+
+int64_t moin_i8_pitch(int64_t cols) { return i8_sizes_ok(0, cols) ? i8_pitch((int)cols) : 0; }
+
+int moin_i8_quantize(moin_ctx *ctx, const void *src, int64_t rows, int64_t cols, void *codes, float *scales, void *stream)
+{
+    if (!ctx || !i8_sizes_ok(rows, cols)) return MOIN_EINVAL;
+    if (rows == 0) return MOIN_OK;
+    if (!src || !codes || !scales || misaligned(src, 16) || misaligned(codes, 16) || misaligned(scales, 4)) return MOIN_EINVAL;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return timed(ctx, MOIN_K_MX_QUANT, st, [&] { return launch_i8_quantize(src, rows, (int)cols, codes, scales, st); }) == hipSuccess ? MOIN_OK : MOIN_EHIP;
+}
+
+static int validate_i8(const void *x, const void *Wq, const float *ws, const void *A_stack, const void *B_stack, int32_t E, int32_t d_in, int32_t d_out,
+                       int32_t r, float scale, const void *y, moin_dtype y_dt)
+{
+    const int rc = validate_linear(x, Wq, A_stack, B_stack, E, d_in, d_out, r, scale, y, y_dt);
+    if (rc != MOIN_OK) return rc;
+    return !ws || misaligned(ws, 16) || d_in > I8_MAX_COLS || (E > 0 && r % 64) ? MOIN_EINVAL : MOIN_OK;
+}
+
+int moin_i8_linear(moin_ctx *ctx, const void *x, int64_t T, const void *Wq, const float *ws, int32_t d_in, int32_t d_out, void *y, moin_dtype y_dt,
+                   void *stream)
+{
+    if (!ctx || T < 0 || T > 0x7fffffffLL - TILE_M) return MOIN_EINVAL;
+    if (T == 0) return MOIN_OK;
+    const int vrc = validate_i8(x, Wq, ws, nullptr, nullptr, 0, d_in, d_out, 0, 1.f, y, y_dt);
+    if (vrc != MOIN_OK) return vrc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int pitch = i8_pitch(d_in);
+    const size_t xq_bytes = align_up((size_t)T * (size_t)pitch, 256);
+    const int rc = ensure_ws(ctx, xq_bytes + align_up((size_t)T * 4, 256), st);
+    if (rc != MOIN_OK) return rc;
+    char *xq = static_cast<char *>(ctx->ws);
+    float *xs = reinterpret_cast<float *>(xq + xq_bytes);
+    const bool few = T <= I8_FEW_TOKENS;
+    if (!(few && i8_few_quantises(T, d_in)) &&
+        timed(ctx, MOIN_K_MX_QUANT, st, [&] { return launch_i8_quantize(x, T, d_in, xq, xs, st); }) != hipSuccess)
+        return MOIN_EHIP;
+    return timed(ctx, MOIN_K_I8_LINEAR, st, [&] {
+               if (few) return launch_i8_few(x, xq, xs, Wq, ws, (int)T, d_in, d_out, y, y_dt == MOIN_F32, st);
+               MxLinearArgs m{};
+               m.lin.y = y;
+               m.lin.y_f32 = y_dt == MOIN_F32;
+               m.lin.d_in = d_in;
+               m.lin.d_out = d_out;
+               m.xq = xq;
+               m.xs = xs;
+               m.Wq = Wq;
+               m.Ws = ws;
+               m.plain_splits = 1;
+               m.plain_kb_per_split = pitch / 128;
+               PlanView pv{};
+               pv.T = T;
+               return launch_linear_i8_stream(pv, m, compute_units(), st);
+           }) == hipSuccess
+               ? MOIN_OK
+               : MOIN_EHIP;
+}
+
+int moin_lora_linear_i8_planned(moin_ctx *ctx, const moin_plan *plan, const void *x, const void *Wq, const float *ws, const void *A_stack,
+                                const void *B_stack, int32_t d_in, int32_t d_out, int32_t r, float scale, void *y, moin_dtype y_dt, void *stream)
+{
+    if (!ctx || !plan || plan->device != ctx->device || !plan->built) return MOIN_EINVAL;
+    if (plan->pv.S == 0 || plan->pv.T == 0) return MOIN_OK;
+    const int vrc = validate_i8(x, Wq, ws, A_stack, B_stack, plan->pv.E, d_in, d_out, r, scale, y, y_dt);
+    if (vrc != MOIN_OK) return vrc;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return MOIN_EHIP;
+    return linear_i8_planned_impl(ctx, plan, x, Wq, ws, A_stack, B_stack, d_in, d_out, r, scale, y, y_dt, static_cast<hipStream_t>(stream));
 }
 
 int64_t moin_probe_out_len(moin_ctx *ctx)

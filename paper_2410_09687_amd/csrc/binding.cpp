@@ -566,15 +566,15 @@ struct Strided {
     void *p;
     int64_t stride;
 };
-// [T, heads, D] bf16 whose heads lie side by side; the rows of tokens may be strided.
-Strided token_rows(const at::Tensor &t, const char *name)
+// [T, heads, D] bf16 (or `other`) whose heads lie side by side; the rows of tokens may be strided.
+Strided token_rows(const at::Tensor &t, const char *name, at::ScalarType other = at::kBFloat16)
 {
     if (!t.is_cuda()) {
         PyErr_Format(PyExc_ValueError, "%s must live on the GPU", name);
         throw Raised{};
     }
-    if (t.scalar_type() != at::kBFloat16) {
-        PyErr_Format(PyExc_TypeError, "%s: bfloat16 expected", name);
+    if (t.scalar_type() != at::kBFloat16 && t.scalar_type() != other) {
+        PyErr_Format(PyExc_TypeError, other == at::kBFloat16 ? "%s: bfloat16 expected" : "%s: bfloat16 or float32 expected", name);
         throw Raised{};
     }
     if ((t.size(2) > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != t.size(2))) {
@@ -650,7 +650,8 @@ PyObject *kv_append(PyObject *const *a)
     Py_RETURN_NONE;
 }
 
-// kv_gather(ctx, data, n_pages, page_tokens, n_kv, head_dim, slots, stream) -> (k, v)
+// kv_gather, kv8_gather(ctx, data, n_pages, page_tokens, n_kv, head_dim, slots, stream) -> (k, v)
+template <bool EIGHT>
 PyObject *kv_gather(PyObject *const *a)
 {
     const at::Tensor &slots = tensor(a[6], "slots");
@@ -661,12 +662,32 @@ PyObject *kv_gather(PyObject *const *a)
     moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
     const int32_t *ps = T ? int_ptr(slots, "slots") : nullptr;
     void *pk = T ? dev_ptr(r[0].t, "k") : nullptr, *pv = T ? dev_ptr(r[1].t, "v") : nullptr, *st = handle(a[7]);
-    call("moin_kv_gather", [&] { return moin_kv_gather(ctx, &p, ps, T, pk, pv, st); });
+    call(EIGHT ? "moin_kv8_gather" : "moin_kv_gather", [&] { return (EIGHT ? moin_kv8_gather : moin_kv_gather)(ctx, &p, ps, T, pk, pv, st); });
     return tuple(r, 2);
 }
 
-// kv_attention(ctx, plan, plan.T, plan.S, data, n_pages, page_tokens, n_kv, head_dim, q, block_table, scale, window, y_dtype, out, want_lse, stream)
+// kv8_append(ctx, data, n_pages, page_tokens, n_kv, head_dim, k, v, seq_offsets, slots, stream)
+PyObject *kv8_append(PyObject *const *a)
+{
+    const at::Tensor &k = tensor(a[6], "k"), &v = tensor(a[7], "v"), &off = tensor(a[8], "seq_offsets"), &slots = tensor(a[9], "slots");
+    const moin_kv_pages p = kv_pages(a[1], a[2], a[3], a[4], a[5]);
+    const int64_t T = slots.numel();
+    if (off.numel() < 1) fail(PyExc_ValueError, "seq_offsets [S+1] expected");
+    for (const at::Tensor *t : {&k, &v})
+        if (t->dim() != 3 || t->size(0) != T || t->size(1) != p.n_kv || t->size(2) != p.head_dim)
+            fail(PyExc_ValueError, "k, v [T,n_kv,head_dim] and slots [T] expected");
+    const Strided sk = token_rows(k, "k"), sv = token_rows(v, "v");
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    const int32_t *po = int_ptr(off, "seq_offsets"), *ps = T ? int_ptr(slots, "slots") : nullptr;
+    const int32_t S = size32(off.numel() - 1);
+    void *st = handle(a[10]);
+    call("moin_kv8_append", [&] { return moin_kv8_append(ctx, &p, sk.p, sv.p, sk.stride, sv.stride, T, po, S, ps, st); });
+    Py_RETURN_NONE;
+}
+
+// kv_attention, kv8_attention(ctx, plan, plan.T, plan.S, data, n_pages, page_tokens, n_kv, head_dim, q, block_table, scale, window, y_dtype, out, want_lse, stream)
 //   -> (y, lse or None)
+template <bool EIGHT>
 PyObject *kv_attention(PyObject *const *a)
 {
     const at::Tensor &q = tensor(a[9], "q"), &table = tensor(a[10], "block_table");
@@ -691,8 +712,8 @@ PyObject *kv_attention(PyObject *const *a)
     const int32_t *pt = table.numel() ? int_ptr(table, "block_table") : nullptr;
     void *py = T ? dev_ptr(r[0].t, "out") : nullptr, *st = handle(a[16]);
     float *pl = T && r[1].defined() ? static_cast<float *>(dev_ptr(r[1].t, "lse")) : nullptr;
-    call("moin_kv_attention", [&] {
-        return moin_kv_attention(ctx, plan, &p, sq.p, sq.stride, heads, pt, mp, scale, window, py, y_enum(yt), pl, st);
+    call(EIGHT ? "moin_kv8_attention" : "moin_kv_attention", [&] {
+        return (EIGHT ? moin_kv8_attention : moin_kv_attention)(ctx, plan, &p, sq.p, sq.stride, heads, pt, mp, scale, window, py, y_enum(yt), pl, st);
     });
     return tuple(r, 2);
 }
@@ -725,32 +746,159 @@ PyObject *mx4_linear(PyObject *const *a)
     return y.object();
 }
 
+struct Stacks {
+    const void *A, *B;
+    int32_t r;
+};
+// The adapters of a planned call (or None), for the plan's number of experts.
+Stacks stacks(PyObject *a, PyObject *b, int32_t d_in, int32_t d_out, PyObject *plan_E)
+{
+    Stacks s{nullptr, nullptr, 0};
+    int32_t E = 0;
+    if (a != Py_None && b != Py_None) {
+        const at::Tensor &A = tensor(a, "A_stack"), &B = tensor(b, "B_stack");
+        if (A.dim() != 3 || B.dim() != 3 || A.size(2) != d_in || B.size(0) != A.size(0) || B.size(1) != d_out || B.size(2) != A.size(1))
+            fail(PyExc_ValueError, "A_stack [E,r,d_in] / B_stack [E,d_out,r] shape mismatch");
+        E = size32(A.size(0));
+        s.r = size32(A.size(1));
+    }
+    if (E && E != integer(plan_E)) fail(PyExc_ValueError, "stack holds a different number of experts than the plan was built for");
+    s.A = dev_ptr_or_null(a, "A_stack", at::kBFloat16);
+    s.B = dev_ptr_or_null(b, "B_stack", at::kBFloat16);
+    return s;
+}
+
 // lora_linear_mx4_planned(ctx, plan, plan.T, plan.E, x, W4, d_out, d_in, A, B, scale, y_dtype, out, stream)
 PyObject *lora_linear_mx4_planned(PyObject *const *a)
 {
     const at::Tensor &x = tensor(a[4], "x");
     const Packed w = packed(a[5], a[6], a[7]);
     if (x.dim() != 2 || x.size(1) != w.d_in || x.size(0) != integer(a[2])) fail(PyExc_ValueError, "x [T,d_in] (T as planned) expected");
-    int32_t E = 0, r = 0;
-    if (a[8] != Py_None && a[9] != Py_None) {
-        const at::Tensor &A = tensor(a[8], "A_stack"), &B = tensor(a[9], "B_stack");
-        if (A.dim() != 3 || B.dim() != 3 || A.size(2) != w.d_in || B.size(0) != A.size(0) || B.size(1) != w.d_out || B.size(2) != A.size(1))
-            fail(PyExc_ValueError, "A_stack [E,r,d_in] / B_stack [E,d_out,r] shape mismatch");
-        E = size32(A.size(0));
-        r = size32(A.size(1));
-    }
-    if (E && E != integer(a[3])) fail(PyExc_ValueError, "stack holds a different number of experts than the plan was built for");
+    const Stacks ab = stacks(a[8], a[9], w.d_in, w.d_out, a[3]);
     const at::ScalarType yt = y_type(a[11]);
     const int64_t T = x.size(0);
     Out y = y_out(x, w.d_out, yt, a[12]);
     moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
     const moin_plan *plan = static_cast<moin_plan *>(handle(a[1]));
     const void *px = T ? dev_ptr(x, "x", at::kBFloat16) : nullptr;
-    const void *pA = dev_ptr_or_null(a[8], "A_stack", at::kBFloat16), *pB = dev_ptr_or_null(a[9], "B_stack", at::kBFloat16);
     const float scale = real(a[10]);
     void *py = T ? dev_ptr(y.t, "y") : nullptr, *st = handle(a[13]);
     call("moin_lora_linear_mx4_planned", [&] {
-        return moin_lora_linear_mx4_planned(ctx, plan, px, w.p, pA, pB, w.d_in, w.d_out, r, scale, py, y_enum(yt), st);
+        return moin_lora_linear_mx4_planned(ctx, plan, px, w.p, ab.A, ab.B, w.d_in, w.d_out, ab.r, scale, py, y_enum(yt), st);
+    });
+    return y.object();
+}
+
+// qk_norm_rope(ctx, q, k, positions, freqs, q_gain, k_gain, flags, eps, out, stream) -> (q_out, k_out); k may be None
+PyObject *qk_norm_rope(PyObject *const *a)
+{
+    const bool has_k = a[2] != Py_None;
+    const at::Tensor &q = tensor(a[1], "q");
+    if (q.dim() != 3) fail(PyExc_ValueError, "q [T,n_heads,head_dim] expected");
+    const int64_t T = q.size(0), D = q.size(2);
+    Strided in[2] = {token_rows(q, "q", at::kFloat), {nullptr, 0}}, out[2] = {{nullptr, 0}, {nullptr, 0}};
+    int32_t heads[2] = {size32(q.size(1)), 0};
+    if (has_k) {
+        const at::Tensor &k = tensor(a[2], "k");
+        if (k.dim() != 3 || k.size(0) != T || k.size(2) != D) fail(PyExc_ValueError, "k [T,n_kv,head_dim] with q's T and head_dim expected");
+        in[1] = token_rows(k, "k", at::kFloat);
+        if (k.scalar_type() != q.scalar_type()) fail(PyExc_TypeError, "q and k must be of one type");
+        heads[1] = size32(k.size(1));
+    }
+    Out r[2];
+    if (a[9] == Py_None) {
+        for (int i = 0; i < 1 + has_k; ++i) {
+            r[i].t = empty({T, heads[i], D}, at::kBFloat16, q);
+        }
+    } else {
+        PyObject *seq = PySequence_Fast(a[9], "out: (q_out, k_out) expected");
+        if (!seq) throw Raised{};
+        const bool two = PySequence_Fast_GET_SIZE(seq) == 2;
+        if (two)
+            for (int i = 0; i < 1 + has_k; ++i) r[i].is(PySequence_Fast_GET_ITEM(seq, i));
+        Py_DECREF(seq);
+        if (!two) fail(PyExc_ValueError, "out: (q_out, k_out) expected");
+        for (int i = 0; i < 1 + has_k; ++i) {
+            r[i].t = tensor(r[i].own, "out");
+            if (r[i].t.dim() != 3 || r[i].t.size(0) != T || r[i].t.size(1) != heads[i] || r[i].t.size(2) != D)
+                fail(PyExc_ValueError, "out has the wrong shape");
+        }
+    }
+    for (int i = 0; i < 1 + has_k; ++i) out[i] = token_rows(r[i].t, "out");
+    const int32_t *pos = nullptr;
+    const double *freqs = nullptr;
+    int32_t rot = 0;
+    if (a[3] != Py_None) {
+        const at::Tensor &p = tensor(a[3], "positions"), &f = tensor(a[4], "freqs");
+        if (p.numel() != T) fail(PyExc_ValueError, "positions [T] expected");
+        pos = T ? int_ptr(p, "positions") : nullptr;
+        freqs = static_cast<const double *>(dev_ptr(f, "freqs", at::kDouble));
+        rot = size32(2 * f.numel());
+    }
+    const void *gain[2];
+    for (int i = 0; i < 2; ++i) {
+        gain[i] = dev_ptr_or_null(a[5 + i], i ? "k_gain" : "q_gain", at::kBFloat16);
+        if (gain[i] && tensor(a[5 + i], "gain").numel() != D) fail(PyExc_ValueError, "q_gain, k_gain [head_dim] expected");
+    }
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    const int32_t flags = integer32(a[7]);
+    const float eps = real(a[8]);
+    void *st = handle(a[10]);
+    const moin_dtype dt = q.scalar_type() == at::kFloat ? MOIN_F32 : MOIN_BF16;
+    call("moin_qk_norm_rope", [&] {
+        return moin_qk_norm_rope(ctx, in[0].p, in[1].p, dt, in[0].stride, in[1].stride, T, heads[0], heads[1], size32(D), pos, freqs, rot, flags, gain[0],
+                                 gain[1], eps, out[0].p, out[1].p, out[0].stride, out[1].stride, st);
+    });
+    return tuple(r, 2);
+}
+
+struct Integers {
+    const void *p;
+    const float *s;
+    int32_t d_out, d_in;
+};
+Integers integers(PyObject *codes, PyObject *scales, PyObject *d_in)
+{
+    const at::Tensor &t = tensor(codes, "W8"), &s = tensor(scales, "scales");
+    const int32_t n = integer32(d_in);
+    if (t.dim() != 2 || t.size(0) == 0 || t.size(1) != moin_i8_pitch(n) || s.numel() != t.size(0))
+        fail(PyExc_ValueError, "W8: the codes [d_out,pitch] and scales [d_out] of a [d_out,d_in] weight expected");
+    return Integers{dev_ptr(t, "W8", at::kChar), static_cast<const float *>(dev_ptr(s, "scales", at::kFloat)), size32(t.size(0)), n};
+}
+
+// i8_linear(ctx, x, codes, scales, d_in, y_dtype, out, stream)
+PyObject *i8_linear(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[1], "x");
+    const Integers w = integers(a[2], a[3], a[4]);
+    if (x.dim() != 2 || x.size(1) != w.d_in) fail(PyExc_ValueError, "x [T,d_in] expected");
+    const at::ScalarType yt = y_type(a[5]);
+    const int64_t T = x.size(0);
+    Out y = y_out(x, w.d_out, yt, a[6]);
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    const void *px = T ? dev_ptr(x, "x", at::kBFloat16) : nullptr;
+    void *py = T ? dev_ptr(y.t, "y") : nullptr, *st = handle(a[7]);
+    call("moin_i8_linear", [&] { return moin_i8_linear(ctx, px, T, w.p, w.s, w.d_in, w.d_out, py, y_enum(yt), st); });
+    return y.object();
+}
+
+// lora_linear_i8_planned(ctx, plan, plan.T, plan.E, x, codes, scales, d_in, A, B, scale, y_dtype, out, stream)
+PyObject *lora_linear_i8_planned(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[4], "x");
+    const Integers w = integers(a[5], a[6], a[7]);
+    if (x.dim() != 2 || x.size(1) != w.d_in || x.size(0) != integer(a[2])) fail(PyExc_ValueError, "x [T,d_in] (T as planned) expected");
+    const Stacks ab = stacks(a[8], a[9], w.d_in, w.d_out, a[3]);
+    const at::ScalarType yt = y_type(a[11]);
+    const int64_t T = x.size(0);
+    Out y = y_out(x, w.d_out, yt, a[12]);
+    moin_ctx *ctx = static_cast<moin_ctx *>(handle(a[0]));
+    const moin_plan *plan = static_cast<moin_plan *>(handle(a[1]));
+    const void *px = T ? dev_ptr(x, "x", at::kBFloat16) : nullptr;
+    const float scale = real(a[10]);
+    void *py = T ? dev_ptr(y.t, "y") : nullptr, *st = handle(a[13]);
+    call("moin_lora_linear_i8_planned", [&] {
+        return moin_lora_linear_i8_planned(ctx, plan, px, w.p, w.s, ab.A, ab.B, w.d_in, w.d_out, ab.r, scale, py, y_enum(yt), st);
     });
     return y.object();
 }
@@ -780,12 +928,15 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
     }
     END_HANDLE_TH_ERRORS
 }
-#define MOIN_ENTRY(f, n) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<f, n>)), METH_FASTCALL, nullptr}
+#define MOIN_ENTRY_AS(name, f, n) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<f, n>)), METH_FASTCALL, nullptr}
+#define MOIN_ENTRY(f, n) MOIN_ENTRY_AS(#f, f, n)
 PyMethodDef methods[] = {
     MOIN_ENTRY(route, 10), MOIN_ENTRY(route_topk, 7), MOIN_ENTRY(route_plan, 14), MOIN_ENTRY(plan_build, 8),
     MOIN_ENTRY(lora_linear, 12), MOIN_ENTRY(lora_linear_planned, 12), MOIN_ENTRY(lora_linear_mx_planned, 16),
     MOIN_ENTRY(lora_linear_planned_shared, 12), MOIN_ENTRY(merge_adapters, 8), MOIN_ENTRY(set_error, 1),
-    MOIN_ENTRY(kv_plan_build, 15), MOIN_ENTRY(kv_append, 10), MOIN_ENTRY(kv_gather, 8), MOIN_ENTRY(kv_attention, 17),
+    MOIN_ENTRY(kv_plan_build, 15), MOIN_ENTRY(kv_append, 10), MOIN_ENTRY_AS("kv_gather", kv_gather<false>, 8),
+    MOIN_ENTRY_AS("kv_attention", kv_attention<false>, 17), MOIN_ENTRY(kv8_append, 11), MOIN_ENTRY_AS("kv8_gather", kv_gather<true>, 8),
+    MOIN_ENTRY_AS("kv8_attention", kv_attention<true>, 17), MOIN_ENTRY(qk_norm_rope, 11), MOIN_ENTRY(i8_linear, 8), MOIN_ENTRY(lora_linear_i8_planned, 14),
     MOIN_ENTRY(mx4_linear, 8), MOIN_ENTRY(lora_linear_mx4_planned, 14),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_moin_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

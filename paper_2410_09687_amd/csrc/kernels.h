@@ -271,6 +271,32 @@ bool mx_stream_kernel_fits(int d_in, int r);
 hipError_t launch_linear_mx_stream(const PlanView &pv, const MxLinearArgs &a, int n_cus, hipStream_t stream);
 int compute_units();   // of the current device
 
+// Base in 8-bit integers (i8.hip, mx.hip): rows of codes padded with zeros to this many bytes, a scale of fp32 for each row.
+constexpr int i8_pitch(int cols) { return cols <= 256 ? 256 : (cols + 127) / 128 * 128; }
+constexpr int I8_MAX_COLS = 131072;   // sums of as many products of 127 x 127 fit 31 bits
+constexpr int I8_FEW_TOKENS = 64;     // up to here launch_i8_few
+hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *codes, float *scales, hipStream_t stream);
+// y [T, d_out] of up to I8_FEW_TOKENS tokens, whose codes and scales are given -- or, where launch_i8_few_quantises, x itself.
+bool i8_few_quantises(int64_t T, int d_in);
+hipError_t launch_i8_few(const void *x, const void *xq, const float *xs, const void *Wq, const float *ws, int T, int d_in, int d_out, void *y,
+                         int y_f32, hipStream_t stream);
+hipError_t launch_linear_i8_stream(const PlanView &pv, const MxLinearArgs &a, int n_cus, hipStream_t stream);   // (xs, Ws: fp32)
+
+// Norms and rotation of queries and keys (rotate.hip); strides in elements between the rows of tokens.
+struct RotateArgs {
+    const void *q, *k;
+    int64_t q_stride, k_stride, T;
+    int x_f32, n_heads, n_kv, D;
+    const int *positions;
+    const double *freqs;       // [rot / 2]
+    int rot, neighbours, norm;
+    const void *q_gain, *k_gain;   // [D] bf16, or null
+    float eps;
+    void *q_out, *k_out;
+    int64_t q_out_stride, k_out_stride;
+};
+hipError_t launch_qk_norm_rope(const RotateArgs &a, hipStream_t stream);
+
 hipError_t prepare_kernels();  // one-time attribute set-up (large dynamic LDS)
 
 // merged adapter (merge.hip): see moin_merge_adapters

@@ -4,6 +4,9 @@
 // blocks of 32 contraction steps share a power-of-two scale (one E8M0 byte) and
 // hold FP8 E4M3 elements.
 //
+// The same stream runs on 8-bit integers (a scale for each token and output channel, i8.hip), whose two 16-byte pieces are the operands of two
+// v_mfma_i32_32x32x32_i8.
+//
 //   mx_quantize_kernel      bf16 -> codes + scales (the weight once, the
 //                           activations per call);
 //   linear_mx_stream_kernel y tile = xq Wq^T (block-scaled FP8 MFMA)
@@ -117,6 +120,9 @@ hipError_t launch_mx_quantize(const void *src, int64_t rows, int64_t cols, void 
 
 namespace mxs {
 
+// What the base product's operands are.
+constexpr int BASE_BF16 = 0, BASE_MX = 1, BASE_I8 = 2;
+
 constexpr int BT = 256;              // tile edge, both ways
 constexpr int ROWB = 128;            // bytes of one operand row per block
 constexpr int KB16 = 64;             // contraction steps of an adapter block (bf16)
@@ -134,8 +140,8 @@ constexpr int LOADS = 8;             // DMA instructions per wave per operand pe
 constexpr int NSC = FP + FQ;         // scale words a lane needs per block
 
 struct Params {
-    const char *xq, *Wq;             // FP8 codes [T, d_in], [d_out, d_in]
-    const char *xs, *Ws;             // scale words [d_in / 128, T], [d_in / 128, d_out] (four bytes each)
+    const char *xq, *Wq;             // codes [T, d_in], [d_out, d_in]
+    const char *xs, *Ws;             // FP8: scale words [d_in / 128, T], [d_in / 128, d_out] (four bytes each); integers: fp32 [T], [d_out]
     int64_t T;
     const char *B_stack, *u_hi, *u_lo;
     char *y;
@@ -166,10 +172,10 @@ struct Tile {
 };
 
 // E: the tile's edge; a plan tile is TILE_M / E of them along the tokens (the last may be empty: q_rows <= 0).
-template <bool MX, int E = BT>
+template <int BASE, int E = BT>
 __device__ __forceinline__ Tile load_tile(const Params &p, int id, int n_work)
 {
-    constexpr int EB = MX ? 1 : 2;   // bytes per base operand element
+    constexpr int EB = BASE == BASE_BF16 ? 2 : 1;   // bytes per base operand element
     constexpr int SUB = TILE_M / E;
     Tile t;
     t.valid = id < n_work;
@@ -218,6 +224,50 @@ typedef int i32x4_t __attribute__((ext_vector_type(4)));
 // One MFMA operand of a lane: 16 + 16 bytes of a row (see the head of the file).
 typedef i32x8_t Frag;
 
+typedef int i32x16_t __attribute__((ext_vector_type(16)));
+// Two integer MFMAs on an accumulator whose bits are int32 sums: the two 16-byte pieces are 32 steps each.
+__device__ __forceinline__ f32x16_t i8_products(const Frag &a, const Frag &b, f32x16_t c)
+{
+    i32x16_t v = __builtin_bit_cast(i32x16_t, c);
+    v = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_shufflevector(a, a, 0, 1, 2, 3), __builtin_shufflevector(b, b, 0, 1, 2, 3), v, 0, 0, 0);
+    v = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_shufflevector(a, a, 4, 5, 6, 7), __builtin_shufflevector(b, b, 4, 5, 6, 7), v, 0, 0, 0);
+    return __builtin_bit_cast(f32x16_t, v);
+}
+// The base product's sums to fp32 with their scales, in front of the adapter's blocks or the epilogue; the wave's outputs begin at n, its tokens at t.
+template <bool AGPR, int FP, int FQ>
+__device__ __forceinline__ void i8_scale(f32x16_t (&acc)[FP][FQ], const Params &p, int n, int t, int lane)
+{
+    const float *ws = reinterpret_cast<const float *>(p.Ws), *xs = reinterpret_cast<const float *>(p.xs);
+    float st[FQ];
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) st[j] = xs[min((int64_t)t + j * 32 + (lane & 31), p.T - 1)];
+#pragma unroll
+    for (int i = 0; i < FP; ++i) {
+        f32x4_t so[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g)   // (d_out is a multiple of 8: four outputs are all there or none is)
+            so[g] = *reinterpret_cast<const f32x4_t *>(ws + min(n + i * 32 + 8 * g + 4 * (lane >> 5), p.d_out - 4));
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                if constexpr (AGPR) {
+                    // (in place, register by register: as a whole the accumulator would be copied, and others spilled for it)
+                    int v;
+                    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[i][j][e]));
+                    const float f = (float)v * (st[j] * so[e >> 2][e & 3]);
+                    float x;
+                    asm volatile("v_accvgpr_write_b32 %0, %1" : "=a"(x) : "v"(f));
+                    acc[i][j][e] = x;
+                } else {
+                    acc[i][j][e] = (float)(int)f32_bits(acc[i][j][e]) * (st[j] * so[e >> 2][e & 3]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+}
+
 }  // namespace mxs
 
 // Shape of the kernel: one persistent workgroup of four waves per compute unit
@@ -229,15 +279,17 @@ typedef i32x8_t Frag;
 // memory, so the only wait on the memory counter is the one in front of the
 // per-block barrier.
 //
-// MX = false runs the same stream on a bf16 base (xq / Wq then hold x and W, there
+// BASE_BF16 runs the same stream on a bf16 base (xq / Wq then hold x and W, there
 // are no scales, and every block takes the bf16 MFMAs); it is not instantiated:
 // measured against the eight-wave bf16 kernel on the 2048 -> 2048 prefill shape it
 // took 262 us against 252 us on the same device.
-template <bool MX, bool Y_F32>
+// On integers the accumulators hold int32 sums through the base's blocks and become fp32 in front of the adapter's.
+template <int BASE, bool Y_F32>
 __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
 {
     using namespace mxs;
-    constexpr int EB = MX ? 1 : 2;
+    constexpr bool MX = BASE == BASE_MX, I8 = BASE == BASE_I8;
+    constexpr int EB = BASE == BASE_BF16 ? 2 : 1;
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63;
     const int wave = uniform(threadIdx.x >> 6);
@@ -366,10 +418,12 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
     // (ZERO: the tile's first MFMA on this accumulator takes a constant zero as its addend, so the
     // accumulators are never cleared: 256 register writes per tile, 5.6 cycles each at one wave per SIMD)
     auto mfma_one = [&](auto base_tag, auto ks_tag, auto i_tag, auto j_tag, auto zero_tag) __attribute__((always_inline)) {
-        constexpr bool BASE = decltype(base_tag)::value, ZERO = decltype(zero_tag)::value;
+        constexpr bool ON_BASE = decltype(base_tag)::value, ZERO = decltype(zero_tag)::value;
         constexpr int KS = decltype(ks_tag)::value, I = decltype(i_tag)::value, J = decltype(j_tag)::value;
         const f32x16_t c0 = ZERO ? f32x16_t{} : acc[I][J];
-        if constexpr (BASE) {
+        if constexpr (ON_BASE && I8) {
+            acc[I][J] = i8_products(fp[KS][I], fq[KS][J], c0);
+        } else if constexpr (ON_BASE) {
             acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
                 fp[KS][I], fq[KS][J], c0, 0, 0, (I & 1) * 2 + KS, (int)sc[I / 2], (J & 1) * 2 + KS,
                 (int)sc[FP / 2 + J / 2]);
@@ -380,9 +434,9 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
     };
     static_assert(FP == 4 && FQ == 4 && LOADS == 8, "the steps below are written out for 4 x 4 accumulators");
 
-    Tile cur = load_tile<MX>(p, id, band_end);
+    Tile cur = load_tile<BASE>(p, id, band_end);
     id += nslot;
-    Tile nxt = load_tile<MX>(p, id, band_end);
+    Tile nxt = load_tile<BASE>(p, id, band_end);
 
     // fetch cursor: tile and block index of the next block to request
     Tile pft = cur;
@@ -399,7 +453,7 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
     // fragment (two LDS reads), a request with its three address instructions (about 40 cycles together),
     // a scale word -- and the source order IS the instruction order (a scheduling barrier after every
     // step).  With the steps left to the scheduler's group barriers a block of 32 MFMAs took 3500 cycles.
-    // BASE: kind of this block.  At the stream's end the requests and reads are repeated requests and
+    // base_tag: kind of this block.  At the stream's end the requests and reads are repeated requests and
     // stale bytes of LDS that nothing uses: no branch after the barrier.
     // (An MFMA has no side effects, so only data flow keeps it in its place: its accumulator and the
     // output-rows fragment of the NEXT step's MFMA pass through an empty assembly statement that also
@@ -479,10 +533,16 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
         if constexpr (MX) regroup();
         const int total = cur.total;
         const int nb = min(nkb0, total);   // a part of a plain tile has fewer blocks than the full range; >= 1
-        body(s, std::integral_constant<bool, MX>{}, std::true_type{});
+        body(s, std::integral_constant<bool, MX || I8>{}, std::true_type{});
         ++s;
         int b = 1;
-        for (; b < nb; ++b, ++s) body(s, std::integral_constant<bool, MX>{}, std::false_type{});
+        for (; b < nb; ++b, ++s) body(s, std::integral_constant<bool, MX || I8>{}, std::false_type{});
+        if constexpr (I8) {
+            int lane_s = lane;
+            asm volatile("; lane id, rematerialised\n\ts_nop 15\n\ts_nop 15" : "+v"(lane_s) : : "memory");
+            i8_scale<true, FP, FQ>(acc, p, cur.n0 + wp * (FP * 32), cur.row0 + wq * (FQ * 32), lane_s);
+            asm volatile("s_nop 15" ::: "memory");   // the assembly's writes before the adapter's MFMAs read them
+        }
         for (; b < total; ++b, ++s) body(s, std::false_type{}, std::false_type{});
 
         asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");   // the last MFMAs' results before the epilogue's assembly reads them
@@ -498,7 +558,7 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
         if (!nxt.valid) break;
         cur = nxt;
         id += nslot;
-        nxt = load_tile<MX>(p, id, band_end);
+        nxt = load_tile<BASE>(p, id, band_end);
     }
     // the last blocks' repeated requests must have landed before the LDS is released
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -520,16 +580,17 @@ using mxs::SCR_BYTES;
 using mxs::Tile;
 constexpr int BT = 128, FP = 2, FQ = 2;
 constexpr int OP_BYTES = BT * ROWB;
-constexpr int LOADS = 4;                  // requests of a wave per operand per block, 8 rows each, and one of scale words
-constexpr int REQ = 2 * LOADS + 1;
+constexpr int LOADS = 4;                  // requests of a wave per operand per block, 8 rows each, and on FP8 one of scale words
 constexpr int SC_BYTES = 2 * BT * 4;      // scale words of a block: 128 output rows, then 128 tokens
 constexpr int NS = 2, STAGE_BYTES = 2 * OP_BYTES + SC_BYTES;   // 33 KB a stage
 }  // namespace mxm
 
-template <bool Y_F32>
+template <int BASE, bool Y_F32>
 __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p)
 {
     using namespace mxm;
+    constexpr bool MX = BASE == mxs::BASE_MX;
+    constexpr int REQ = 2 * LOADS + (MX ? 1 : 0);   // requests of a wave per block
     using mxs::i32x4_t;
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63;
@@ -548,7 +609,7 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
         const int j = id / p.n_tiles_n;
         id += (halves.find(j) - j) * p.n_tiles_n;
     }
-    const Tile t = mxs::load_tile<true, BT>(p, id, id + 1);
+    const Tile t = mxs::load_tile<BASE, BT>(p, id, id + 1);
     const int q_rows = t.q_rows, p_rows = t.p_rows, row0 = t.row0, n0 = t.n0, kb0 = t.kb0, nkb1 = t.nkb1, total = t.total;
     const char *const q0 = t.q0, *const p0 = t.p0, *const uh = t.uh, *const ul = t.ul, *const be = t.be;
     char *const y = p.y + t.y_off;
@@ -580,7 +641,7 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
         const int kb = base ? b : (hi ? jb : jb - nkb1);
         f.pq = (base ? q0 : (hi ? uh : ul)) + kb * ROWB;
         f.pp = (base ? p0 : be) + kb * ROWB;
-        f.ps = sc0 + (base ? b : 0) * sc_pitch;   // (an adapter block repeats the first one's: no branch)
+        f.ps = MX ? sc0 + (base ? b : 0) * sc_pitch : nullptr;   // (an adapter block repeats the first one's: no branch)
         f.ld = base ? ldq : ldu;
         return f;
     };
@@ -633,7 +694,12 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
     };
     auto products = [&](auto base_tag, auto ks_tag) __attribute__((always_inline)) {
         constexpr int KS = decltype(ks_tag)::value;
-        if constexpr (decltype(base_tag)::value) {
+        if constexpr (decltype(base_tag)::value && !MX) {
+#pragma unroll
+            for (int i = 0; i < FP; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) acc[i][j] = mxs::i8_products(fr[KS][i], fr[KS][FP + j], acc[i][j]);
+        } else if constexpr (decltype(base_tag)::value) {
 #define MOIN_MXM(I, J)                                                                                                \
     acc[I][J] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fr[KS][I], fr[KS][FP + J], acc[I][J], 0, 0,             \
                                                                 I * 2 + KS, (int)sc[0], J * 2 + KS, (int)sc[1])
@@ -675,12 +741,14 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
         // (after the last block: stale bytes that nothing uses)
 #pragma unroll
         for (int n = 0; n < FP + FQ; ++n) read_frag(nxt, 0, n);
+        if constexpr (MX) {
 #pragma unroll
-        for (int n = 0; n < FP + FQ; ++n) read_scale(nxt, n);
+            for (int n = 0; n < FP + FQ; ++n) read_scale(nxt, n);
+        }
         __builtin_amdgcn_sched_barrier(0);
         products(base_tag, K1{});
         __builtin_amdgcn_sched_barrier(0);
-        regroup();
+        if constexpr (MX) regroup();
     };
 
 #pragma unroll
@@ -692,11 +760,14 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
     wait_vm_then_barrier<(NS - 1) * REQ>();
 #pragma unroll
     for (int n = 0; n < FP + FQ; ++n) read_frag(0, 0, n);
+    if constexpr (MX) {
 #pragma unroll
-    for (int n = 0; n < FP + FQ; ++n) read_scale(0, n);
-    regroup();
+        for (int n = 0; n < FP + FQ; ++n) read_scale(0, n);
+        regroup();
+    }
     int b = 0;
     for (; b < nb; ++b) body(b, std::true_type{});
+    if constexpr (!MX) mxs::i8_scale<false, FP, FQ>(acc, p, n0 + wp * (FP * 32), row0 + wq * (FQ * 32), lane);
     for (; b < total; ++b) body(b, std::false_type{});
     // the stages become the waves' scratch: no request (waited for in the last blocks) and no stale read is under way
     asm volatile("s_nop 15\n\ts_nop 15\n\ts_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -704,22 +775,22 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
                                       wq, lane);
 }
 
-template <bool Y_F32>
-static hipError_t allow_mid_lds()
+template <int BASE, bool Y_F32>
+static hipError_t allow_lds()
 {
-    return hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_mx_mid_kernel<Y_F32>),
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_stream4_kernel<BASE, Y_F32>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, mxs::SMEM_BYTES);
+    if (e != hipSuccess) return e;
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_mx_mid_kernel<BASE, Y_F32>),
                                hipFuncAttributeMaxDynamicSharedMemorySize, mxm::NS * mxm::STAGE_BYTES);
 }
 
 hipError_t prepare_mx_kernels()
 {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_stream4_kernel<true, false>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, mxs::SMEM_BYTES);
-    if (e != hipSuccess) return e;
-    e = hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_stream4_kernel<true, true>),
-                            hipFuncAttributeMaxDynamicSharedMemorySize, mxs::SMEM_BYTES);
-    if (e == hipSuccess) e = allow_mid_lds<false>();
-    if (e == hipSuccess) e = allow_mid_lds<true>();
+    hipError_t e = allow_lds<mxs::BASE_MX, false>();
+    if (e == hipSuccess) e = allow_lds<mxs::BASE_MX, true>();
+    if (e == hipSuccess) e = allow_lds<mxs::BASE_I8, false>();
+    if (e == hipSuccess) e = allow_lds<mxs::BASE_I8, true>();
     return e;
 }
 
@@ -769,7 +840,8 @@ int64_t mx_plain_rows(int64_t T, int d_in, int d_out)
     return most;
 }
 
-hipError_t launch_linear_mx_stream(const PlanView &pv, const MxLinearArgs &a, int n_cus, hipStream_t stream_)
+template <int BASE>
+static hipError_t launch_stream(const PlanView &pv, const MxLinearArgs &a, int n_cus, hipStream_t stream_)
 {
     mxs::Params p;
     p.xq = (const char *)a.xq; p.Wq = (const char *)a.Wq; p.xs = (const char *)a.xs; p.Ws = (const char *)a.Ws;
@@ -781,7 +853,7 @@ hipError_t launch_linear_mx_stream(const PlanView &pv, const MxLinearArgs &a, in
     p.tile_rank = pv.tile_rank;
     p.n_tiles = pv.n_tiles;
     p.max_tiles = pv.max_tiles;
-    p.d_in = a.lin.d_in; p.d_out = a.lin.d_out; p.r = a.lin.r;
+    p.d_in = BASE == mxs::BASE_I8 ? i8_pitch(a.lin.d_in) : a.lin.d_in; p.d_out = a.lin.d_out; p.r = a.lin.r;
     p.n_tiles_n = (a.lin.d_out + mxs::BT - 1) / mxs::BT;
     p.y_f32 = a.lin.y_f32;
     p.plain = a.plain_splits > 0;
@@ -798,9 +870,9 @@ hipError_t launch_linear_mx_stream(const PlanView &pv, const MxLinearArgs &a, in
         if (work > 0x7ffffff0LL) return hipErrorInvalidValue;
         const dim3 grid((unsigned)((work + 7) / 8 * 8));
         if (p.y_f32)
-            hipLaunchKernelGGL((linear_mx_mid_kernel<true>), grid, dim3(mxm::NT), mxm::NS * mxm::STAGE_BYTES, stream_, p);
+            hipLaunchKernelGGL((linear_mx_mid_kernel<BASE, true>), grid, dim3(mxm::NT), mxm::NS * mxm::STAGE_BYTES, stream_, p);
         else
-            hipLaunchKernelGGL((linear_mx_mid_kernel<false>), grid, dim3(mxm::NT), mxm::NS * mxm::STAGE_BYTES, stream_, p);
+            hipLaunchKernelGGL((linear_mx_mid_kernel<BASE, false>), grid, dim3(mxm::NT), mxm::NS * mxm::STAGE_BYTES, stream_, p);
         return hipGetLastError();
     }
     // one workgroup per compute unit (the LDS footprint allows no more), fewer
@@ -813,12 +885,21 @@ hipError_t launch_linear_mx_stream(const PlanView &pv, const MxLinearArgs &a, in
     // (one instantiation per output type: with both epilogues in one kernel the
     // compiler moved accumulators through scratch memory at every tile's end)
     if (a.lin.y_f32)
-        hipLaunchKernelGGL((linear_stream4_kernel<true, true>), dim3((unsigned)grid), dim3(mxs::NT), mxs::SMEM_BYTES,
+        hipLaunchKernelGGL((linear_stream4_kernel<BASE, true>), dim3((unsigned)grid), dim3(mxs::NT), mxs::SMEM_BYTES,
                            stream_, p);
     else
-        hipLaunchKernelGGL((linear_stream4_kernel<true, false>), dim3((unsigned)grid), dim3(mxs::NT), mxs::SMEM_BYTES,
+        hipLaunchKernelGGL((linear_stream4_kernel<BASE, false>), dim3((unsigned)grid), dim3(mxs::NT), mxs::SMEM_BYTES,
                            stream_, p);
     return hipGetLastError();
+}
+
+hipError_t launch_linear_mx_stream(const PlanView &pv, const MxLinearArgs &a, int n_cus, hipStream_t stream)
+{
+    return launch_stream<mxs::BASE_MX>(pv, a, n_cus, stream);
+}
+hipError_t launch_linear_i8_stream(const PlanView &pv, const MxLinearArgs &a, int n_cus, hipStream_t stream)
+{
+    return launch_stream<mxs::BASE_I8>(pv, a, n_cus, stream);
 }
 
 }  // namespace moin

@@ -23,11 +23,13 @@ MOIN_F32, MOIN_BF16 = 0, 1
 MOIN_MX_X_INTERNAL, MOIN_MX_X_EMIT, MOIN_MX_X_GIVEN = 0, 1, 2
 MOIN_ROUTE_RETAINED_ONLY = 1
 MOIN_ROUTE_SAME_CENTROIDS = 2
+MOIN_QK_NORM, MOIN_QK_NEIGHBOURS = 1, 2
 (K_PLAN, K_SHRINK, K_LINEAR, K_ROUTE, K_ROUTE_AUX, K_DECODE_SHRINK, K_DECODE_EXPAND, K_DECODE_BASE,
  K_KMEANS_SORT, K_KMEANS_SUM, K_KMEANS_FINAL) = range(11)
 KERNEL_NAMES = ["plan", "shrink", "linear", "route", "route_aux", "decode_shrink", "decode_expand",
                 "decode_base", "kmeans_sort", "kmeans_sum", "kmeans_final", "mx_quant", "mx_linear",
-                "probe_mfma", "probe_read", "kv_plan", "kv_append", "kv_attend", "mx4_linear"]
+                "probe_mfma", "probe_read", "kv_plan", "kv_append", "kv_attend", "mx4_linear",
+                "qk_rotate", "i8_linear"]
 
 EXPORTS = [
     "moin_create", "moin_destroy", "moin_strerror", "moin_check", "moin_route", "moin_histogram",
@@ -44,6 +46,8 @@ EXPORTS = [
     "moin_mx4_bytes", "moin_mx4_quantize", "moin_mx4_dequantize", "moin_mx4_linear", "moin_lora_linear_mx4_planned",
     "moin_kv_page_bytes", "moin_kv_plan_create", "moin_kv_plan_destroy", "moin_kv_plan_build", "moin_kv_release", "moin_kv_append",
     "moin_kv_gather", "moin_kv_attention",
+    "moin_qk_norm_rope", "moin_kv8_page_bytes", "moin_kv8_append", "moin_kv8_gather", "moin_kv8_attention",
+    "moin_i8_pitch", "moin_i8_quantize", "moin_i8_linear", "moin_lora_linear_i8_planned",
 ]
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
 CACHE_STATS = ["batches", "seq_hits", "seq_misses", "loads", "evictions", "overflows", "bytes"]
@@ -147,7 +151,16 @@ def load() -> ctypes.CDLL:
     lib.moin_kv_append.argtypes = [vp, kvp, vp, vp, i64, i64, i64, vp, vp]
     lib.moin_kv_gather.argtypes = [vp, kvp, vp, i64, vp, vp, vp]
     lib.moin_kv_attention.argtypes = [vp, vp, kvp, vp, i64, i32, vp, i32, c.c_float, i32, vp, c.c_int, vp, vp]
-    sizes = ("moin_probe_out_len", "moin_workspace_bytes", "moin_mx4_bytes", "moin_kv_page_bytes")
+    lib.moin_qk_norm_rope.argtypes = [vp, vp, vp, c.c_int, i64, i64, i64, i32, i32, i32, vp, vp, i32, i32, vp, vp, c.c_float, vp, vp, i64, i64, vp]
+    lib.moin_kv8_page_bytes.argtypes = lib.moin_kv_page_bytes.argtypes
+    lib.moin_kv8_append.argtypes = [vp, kvp, vp, vp, i64, i64, i64, vp, i32, vp, vp]
+    lib.moin_kv8_gather.argtypes = lib.moin_kv_gather.argtypes
+    lib.moin_kv8_attention.argtypes = lib.moin_kv_attention.argtypes
+    lib.moin_i8_pitch.argtypes = [i64]
+    lib.moin_i8_quantize.argtypes = [vp, vp, i64, i64, vp, vp, vp]
+    lib.moin_i8_linear.argtypes = [vp, vp, i64, vp, vp, i32, i32, vp, c.c_int, vp]
+    lib.moin_lora_linear_i8_planned.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, c.c_float, vp, c.c_int, vp]
+    sizes = ("moin_probe_out_len", "moin_workspace_bytes", "moin_mx4_bytes", "moin_kv_page_bytes", "moin_kv8_page_bytes", "moin_i8_pitch")
     for name in EXPORTS:
         if name not in ("moin_destroy", "moin_plan_destroy", "moin_strerror", "moin_cache_destroy", "moin_kv_plan_destroy", *sizes):
             getattr(lib, name).restype = c.c_int
@@ -679,12 +692,16 @@ class KVPages:
         self.data, self.n_kv, self.head_dim, self.page_tokens = data, int(n_kv), int(head_dim), int(page_tokens)
         self.n_pages = data.numel() // nbytes
 
-    @staticmethod
-    def page_bytes(n_kv: int, head_dim: int, page_tokens: int = 64) -> int:
-        nbytes = int(load().moin_kv_page_bytes(int(page_tokens), int(n_kv), int(head_dim)))
+    @classmethod
+    def page_bytes(cls, n_kv: int, head_dim: int, page_tokens: int = 64) -> int:
+        nbytes = cls._page_bytes(int(page_tokens), int(n_kv), int(head_dim))
         if nbytes == 0:
             raise ValueError("page_tokens and head_dim: 64, 128 or 256, at least one kv head expected")
         return nbytes
+
+    @staticmethod
+    def _page_bytes(page_tokens: int, n_kv: int, head_dim: int) -> int:
+        return int(load().moin_kv_page_bytes(page_tokens, n_kv, head_dim))
 
     @classmethod
     def empty(cls, n_pages: int, n_kv: int, head_dim: int, page_tokens: int = 64, device="cuda"):
@@ -741,19 +758,24 @@ def moin_kv_release(ctx: Context, finished: torch.Tensor, kv_lens: torch.Tensor,
                                _dev_ptr(n_free, "n_free", i32), _stream_ptr(stream)), "moin_kv_release")
 
 
+def _kv4(pages):
+    if isinstance(pages, KV8Pages):
+        raise TypeError("pages: KVPages expected, not KV8Pages")
+    return pages.data, pages.n_pages, pages.page_tokens, pages.n_kv, pages.head_dim
+
+
 def moin_kv_append(ctx: Context, pages: KVPages, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
     """Quantises ``k``, ``v`` [T, n_kv, head_dim] (bf16; rows of tokens may be strided, as columns of one projection's output are)
     into ``slots`` [T]; -1 is skipped."""
     load()
-    _native.kv_append(ctx._h.value, pages.data, pages.n_pages, pages.page_tokens, pages.n_kv, pages.head_dim, k, v, slots,
+    _native.kv_append(ctx._h.value, *_kv4(pages), k, v, slots,
                       _stream_ptr(stream))
 
 
 def moin_kv_gather(ctx: Context, pages: KVPages, slots: torch.Tensor, stream=None):
     """The keys and values that ``slots`` [T] hold: ``(k, v)``, bf16 [T, n_kv, head_dim]; zeros for -1."""
     load()
-    return _native.kv_gather(ctx._h.value, pages.data, pages.n_pages, pages.page_tokens, pages.n_kv, pages.head_dim, slots,
-                             _stream_ptr(stream))
+    return _native.kv_gather(ctx._h.value, *_kv4(pages), slots, _stream_ptr(stream))
 
 
 def moin_kv_attention(ctx: Context, plan: KVPlan, pages: KVPages, q: torch.Tensor, block_table: torch.Tensor,
@@ -762,6 +784,101 @@ def moin_kv_attention(ctx: Context, plan: KVPlan, pages: KVPages, q: torch.Tenso
     """Causal attention of the step's tokens ``q`` [T, n_heads, head_dim] (bf16) over the cache, their own keys appended before:
     ``(y, lse or None)``.  ``scale``: 1 / sqrt(head_dim) by default.  ``window`` > 0: the last so many keys alone."""
     load()
-    return _native.kv_attention(ctx._h.value, plan._h.value, plan.T, plan.S, pages.data, pages.n_pages, pages.page_tokens, pages.n_kv,
-                                pages.head_dim, q, block_table, float(pages.head_dim ** -0.5 if scale is None else scale), int(window),
+    return _native.kv_attention(ctx._h.value, plan._h.value, plan.T, plan.S, *_kv4(pages), q, block_table, float(pages.head_dim ** -0.5 if scale is None else scale), int(window),
                                 y_dtype, out, bool(want_lse), _stream_ptr(stream))
+
+
+# ---- serving in eight bits -------------------------------------------------------------------------------
+
+def rope_frequencies(rot_dim: int, theta: float = 10000.0, device="cuda") -> torch.Tensor:
+    """``theta ** (-2 i / rot_dim)`` for the ``rot_dim / 2`` pairs of channels, float64: the radians a position of the plain rotation."""
+    return (float(theta) ** (torch.arange(int(rot_dim) // 2, dtype=torch.float64) * (-2.0 / int(rot_dim)))).to(device)
+
+
+def moin_qk_norm_rope(ctx: Context, q: torch.Tensor, k: Optional[torch.Tensor], *, positions: Optional[torch.Tensor] = None,
+                      freqs: Optional[torch.Tensor] = None, q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
+                      norm: bool = True, eps: float = 1e-6, neighbours: bool = False, out=None, stream=None):
+    """Norms of queries ``q`` [T, n_heads, head_dim] and keys ``k`` [T, n_kv, head_dim] (bf16 or fp32; rows of tokens may be strided; ``k`` may be
+    None) for each head, and the rotation of their first ``2 * freqs.numel()`` channels by ``positions`` [T] (int32) times ``freqs`` (float64,
+    ``rope_frequencies``): ``(q_out, k_out)``, bf16.  Without ``positions`` no rotation, without ``norm`` no norm (and no gains).  Pairs are channels
+    (i, i + half), with ``neighbours`` (2 i, 2 i + 1).  ``out``: the pair preallocated; the inputs themselves for a call in place."""
+    if (positions is None) != (freqs is None):
+        raise ValueError("positions and freqs come together")
+    load()
+    return _native.qk_norm_rope(ctx._h.value, q, k, positions, freqs, q_gain, k_gain,
+                                (MOIN_QK_NORM if norm else 0) | (MOIN_QK_NEIGHBOURS if neighbours else 0), float(eps), out, _stream_ptr(stream))
+
+
+class KV8Pages(KVPages):
+    """A paged cache of keys and values in E4M3 with a power of two for each 64 tokens and head; otherwise as ``KVPages``."""
+
+    @staticmethod
+    def _page_bytes(page_tokens: int, n_kv: int, head_dim: int) -> int:
+        return int(load().moin_kv8_page_bytes(page_tokens, n_kv, head_dim))
+
+
+def _kv8(pages):
+    if not isinstance(pages, KV8Pages):
+        raise TypeError("pages: KV8Pages expected")
+    return pages.data, pages.n_pages, pages.page_tokens, pages.n_kv, pages.head_dim
+
+
+def moin_kv8_append(ctx: Context, pages: KV8Pages, k: torch.Tensor, v: torch.Tensor, seq_offsets: torch.Tensor, slots: torch.Tensor,
+                    stream=None) -> None:
+    """``moin_kv_append`` for a cache in E4M3; ``seq_offsets`` [S+1] and ``slots`` [T] as ``KVPlan.build`` gives them."""
+    load()
+    _native.kv8_append(ctx._h.value, *_kv8(pages), k, v, seq_offsets, slots, _stream_ptr(stream))
+
+
+def moin_kv8_gather(ctx: Context, pages: KV8Pages, slots: torch.Tensor, stream=None):
+    """``moin_kv_gather`` for a cache in E4M3."""
+    load()
+    return _native.kv8_gather(ctx._h.value, *_kv8(pages), slots, _stream_ptr(stream))
+
+
+def moin_kv8_attention(ctx: Context, plan: KVPlan, pages: KV8Pages, q: torch.Tensor, block_table: torch.Tensor,
+                       scale: Optional[float] = None, window: int = 0, y_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None,
+                       want_lse: bool = False, stream=None):
+    """``moin_kv_attention`` over a cache in E4M3."""
+    load()
+    return _native.kv8_attention(ctx._h.value, plan._h.value, plan.T, plan.S, *_kv8(pages), q, block_table,
+                                 float(pages.head_dim ** -0.5 if scale is None else scale), int(window), y_dtype, out, bool(want_lse),
+                                 _stream_ptr(stream))
+
+
+class I8Weight:
+    """A weight ``[d_out, d_in]`` in 8-bit integers: ``codes`` (int8 [d_out, pitch], zeros beyond ``d_in``) and ``scales`` (float32 [d_out]) of
+    ``moin_i8_quantize``."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, d_in: int):
+        if codes.dtype != torch.int8 or codes.dim() != 2 or codes.shape[0] == 0 or codes.shape[1] != load().moin_i8_pitch(int(d_in)) or \
+                scales.dtype != torch.float32 or scales.numel() != codes.shape[0]:
+            raise ValueError("codes [d_out,pitch] int8 and scales [d_out] float32 of a [d_out,d_in] weight expected")
+        self.codes, self.scales, self.d_out, self.d_in = codes, scales, codes.shape[0], int(d_in)
+
+
+def moin_i8_quantize(ctx: Context, W: torch.Tensor, stream=None) -> I8Weight:
+    """A bf16 matrix ``[rows, cols]`` (``cols`` a multiple of 8) in 8-bit integers with a scale for each row."""
+    if W.dim() != 2 or W.shape[0] == 0 or load().moin_i8_pitch(W.shape[1]) == 0:
+        raise ValueError("W [rows,cols] with cols a positive multiple of 8, at most 131072, expected")
+    rows, cols = W.shape
+    codes = torch.empty((rows, int(load().moin_i8_pitch(cols))), dtype=torch.int8, device=W.device)
+    scales = torch.empty(rows, dtype=torch.float32, device=W.device)
+    _ck(load().moin_i8_quantize(ctx._h, _dev_ptr(W, "W", torch.bfloat16), rows, cols, _dev_ptr(codes, "codes"), _dev_ptr(scales, "scales"),
+                                _stream_ptr(stream)), "moin_i8_quantize")
+    return I8Weight(codes, scales, cols)
+
+
+def moin_i8_linear(ctx: Context, x: torch.Tensor, W8: I8Weight, y_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """``y = q(x) W8^T`` with a scale for each token and channel, without adapters."""
+    load()
+    return _native.i8_linear(ctx._h.value, x, W8.codes, W8.scales, W8.d_in, y_dtype, out, _stream_ptr(stream))
+
+
+def moin_lora_linear_i8_planned(ctx: Context, plan: Plan, x: torch.Tensor, W8: I8Weight, A_stack: Optional[torch.Tensor],
+                                B_stack: Optional[torch.Tensor], scale: float, y_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None,
+                                stream=None) -> torch.Tensor:
+    """``moin_lora_linear_planned`` on a base in 8-bit integers (rank a multiple of 64)."""
+    load()
+    return _native.lora_linear_i8_planned(ctx._h.value, plan._h.value, plan.T, plan.E, x, W8.codes, W8.scales, W8.d_in, A_stack, B_stack,
+                                          float(scale), y_dtype, out, _stream_ptr(stream))
