@@ -15,6 +15,17 @@ namespace {
 
 __device__ __forceinline__ uint32_t word(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
+// The bf16 side of a copy passes through once: past L2, which holds the lines of the cache until they are whole.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_once(const char *p)
+{
+    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p)));
+}
+__device__ __forceinline__ void store_once(char *p, const uint4 &v)
+{
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v), reinterpret_cast<u32x4_t *>(p));
+}
+
 constexpr uint32_t KV8_MIN_E = 10, KV8_MAX_E = 246, KV8_NAN = 255;
 
 // E of values whose largest magnitude has these fp32 bits.  At least 10: the smallest code, 2^-9 units, is then a normal number of bf16.  At
@@ -49,14 +60,15 @@ __device__ __forceinline__ uint32_t recode(uint32_t w, float shrink)
     return encode4(lo[0] * shrink, lo[1] * shrink, hi[0] * shrink, hi[1] * shrink);
 }
 
-// Which request a workgroup serves: request s owns the places R(s) to R(s + 1), R(s) = seq_offsets[s] / 64 + 2 s, which are at least as many as
-// the blocks that its tokens can touch.  All lanes of the wave search, 64 ways at a time.
+// Which of a request's blocks a workgroup serves.  Places 0 to S - 1 are the first blocks of the requests, without a search: all there is of a
+// step of single tokens.  Behind them request s owns the places R(s) to R(s + 1), R(s) = seq_offsets[s] / 64 + s, at least as many
+// as the further blocks that its tokens can touch; all lanes of the wave look for theirs, 64 ways at a time.
 __device__ __forceinline__ int request_at(const int *seq_offsets, int S, int id)
 {
     int lo = 0, hi = S;
     while (hi - lo > 1) {
         const int step = (hi - lo + 63) >> 6, s = lo + (int)(threadIdx.x & 63) * step;
-        const bool before = s < hi && (seq_offsets[min(s, S)] >> 6) + 2 * s <= id;
+        const bool before = s < hi && (seq_offsets[min(s, S)] >> 6) + s <= id;
         const int count = max(1, (int)__popcll(__ballot(before)));   // (1: offsets that run backwards)
         lo += (count - 1) * step;
         hi = min(hi, lo + step);
@@ -75,13 +87,13 @@ __global__ __launch_bounds__(NT) void kv8_append_kernel(KvPages p, const char *_
     const int tid = threadIdx.x, lane = tid & 63;
     const bool is_v = blockIdx.x & 1;
     const int h = (int)((blockIdx.x >> 1) % (unsigned)p.n_kv), id = (int)((blockIdx.x >> 1) / (unsigned)p.n_kv);
-    const int s = uniform(request_at(seq_offsets, S, id));
-    const int tok0 = uniform(seq_offsets[s]), n_all = uniform(seq_offsets[s + 1]) - tok0, r = id - ((tok0 >> 6) + 2 * s);
+    const int s = id < S ? id : uniform(request_at(seq_offsets, S, id - S));
+    const int tok0 = uniform(seq_offsets[s]), n_all = uniform(seq_offsets[s + 1]) - tok0, r = id < S ? 0 : id - S - ((tok0 >> 6) + s) + 1;
     if (tok0 < 0 || n_all < 0 || n_all > T - tok0) {
         if (tid == 0) atomicOr(err_word, ERR_BAD_LENGTHS);
         return;
     }
-    if (n_all == 0 || r < 0) return;
+    if (n_all == 0 || r < 0 || (id >= S && r == 0)) return;
     const int slot0 = uniform(slots[tok0]), log_page = p.log_blocks + 6;
     if (slot0 < 0 || (slot0 >> log_page) >= p.n_pages) {   // a request that got no pages, or one that is given others' than there are
         if (slot0 != -1 && tid == 0) atomicOr(err_word, ERR_BAD_PAGE);
@@ -105,16 +117,19 @@ __global__ __launch_bounds__(NT) void kv8_append_kernel(KvPages p, const char *_
     const int64_t stride = (is_v ? v_stride : k_stride) * 2;
 
     constexpr int KC = 64 * D / 8 / NT, VC = (16 * D / 8 + NT - 1) / NT;   // chunks of a thread: a token's 8 channels; 4 tokens' 8 channels
+    // chunks of values: a wave's lanes are 8 quads of tokens x 8 groups of channels, 128 bytes of a row and half a channel's run
+    auto quad_of = [](int chunk) { return (chunk & 7) + (chunk >> 6 & 1) * 8; };
+    auto group_of = [](int chunk) { return (chunk >> 3 & 7) + (chunk >> 7) * 8; };
     uint4 x[KC > 4 * VC ? KC : 4 * VC];
     uint32_t amax = 0;
     if (is_v) {
 #pragma unroll
         for (int u = 0; u < VC; ++u) {
-            const int chunk = u * NT + tid, t4 = (chunk & 15) * 4, c = (chunk >> 4) * 8;
+            const int chunk = u * NT + tid, t4 = quad_of(chunk) * 4, c = group_of(chunk) * 8;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const bool is = c < D && t4 + e >= p0 && t4 + e < p1;
-                x[4 * u + e] = is ? *reinterpret_cast<const uint4 *>(rows + (t4 + e) * stride + c * 2) : make_uint4(0, 0, 0, 0);
+                x[4 * u + e] = is ? load_once(rows + (t4 + e) * stride + c * 2) : make_uint4(0, 0, 0, 0);
                 amax = max(amax, bf16x8_amax(x[4 * u + e]));
             }
         }
@@ -122,7 +137,7 @@ __global__ __launch_bounds__(NT) void kv8_append_kernel(KvPages p, const char *_
 #pragma unroll
         for (int u = 0; u < KC; ++u) {
             const int chunk = u * NT + tid, t = chunk / (D / 8), c = chunk % (D / 8) * 8;
-            x[u] = t >= p0 && t < p1 ? *reinterpret_cast<const uint4 *>(rows + t * stride + c * 2) : make_uint4(0, 0, 0, 0);
+            x[u] = t >= p0 && t < p1 ? load_once(rows + t * stride + c * 2) : make_uint4(0, 0, 0, 0);
             amax = max(amax, bf16x8_amax(x[u]));
         }
     }
@@ -143,7 +158,7 @@ __global__ __launch_bounds__(NT) void kv8_append_kernel(KvPages p, const char *_
     if (is_v) {
 #pragma unroll
         for (int u = 0; u < VC; ++u) {
-            const int chunk = u * NT + tid, quad = chunk & 15, t4 = quad * 4, c = (chunk >> 4) * 8;
+            const int chunk = u * NT + tid, quad = quad_of(chunk), t4 = quad * 4, c = group_of(chunk) * 8;
             if (c >= D || t4 >= p1 || (t4 + 4 <= p0 && !grows)) continue;
             uint32_t is_new = 0, is_old = 0;
 #pragma unroll
@@ -152,16 +167,25 @@ __global__ __launch_bounds__(NT) void kv8_append_kernel(KvPages p, const char *_
                 if (t4 + e < p0) is_old |= 255u << 8 * e;
             }
             char *dst = rec + 64 * D + (c >> 4) * 1024 + (c & 8) * 64 + (quad & 3) * 16 + (quad >> 2) * 4;
-            const bool merge = is_new != ~0u;   // (what lies beside the new tokens in their words stays)
-            uint32_t was[8];
+            uint32_t codes[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) was[i] = merge ? *reinterpret_cast<const uint32_t *>(dst + i * 64) : 0u;
+            for (int i = 0; i < 8; ++i) codes[i] = encode4(at(x[4 * u], i), at(x[4 * u + 1], i), at(x[4 * u + 2], i), at(x[4 * u + 3], i));
+            if (is_new == ~0u) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t codes = encode4(at(x[4 * u], i), at(x[4 * u + 1], i), at(x[4 * u + 2], i), at(x[4 * u + 3], i));
-                uint32_t w = was[i];
-                if (grows) w = (recode(w, shrink) & is_old) | (w & ~is_old);
-                *reinterpret_cast<uint32_t *>(dst + i * 64) = (codes & is_new) | (w & ~is_new);
+                for (int i = 0; i < 8; ++i) *reinterpret_cast<uint32_t *>(dst + i * 64) = codes[i];
+            } else if (grows && is_old) {
+                uint32_t was[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) was[i] = *reinterpret_cast<const uint32_t *>(dst + i * 64);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    *reinterpret_cast<uint32_t *>(dst + i * 64) = (codes[i] & is_new) | (recode(was[i], shrink) & is_old) | (was[i] & ~(is_new | is_old));
+            } else {   // what lies beside the new tokens in their words stays: bytes, no trip to memory for the words
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (is_new >> 8 * e & 255)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) dst[i * 64 + e] = (char)(codes[i] >> 8 * e);
             }
         }
     } else {
@@ -207,23 +231,71 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__rest
     using High = std::integral_constant<bool, true>;
     char *out = (is_v ? v : k) + (int64_t)h * D * 2;
     const int64_t row = (int64_t)p.n_kv * D * 2;
-    if (is_v) {   // lanes are tokens: the bytes of a channel are neighbours
-        const int64_t t = t0 + (tid & 63);
-        if (t >= T) return;
-        const char *rec;
-        int tok;
-        float unit;
-        const bool in = place(t, rec, tok, unit);
-        const uint8_t *src = reinterpret_cast<const uint8_t *>(rec) + 64 * D + ((tok >> 2) & 3) * 16 + (tok >> 4) * 4 + (tok & 3);
+    if (is_v) {
+        // Four tokens that lie in one word of every channel, eight channels: eight words, turned into the tokens' rows with v_perm.  The batch's tokens
+        // need not begin where the cache's words do: the first and last quads are then cut off, and one more is needed.
+        constexpr int CG = D / 8, STEP = 256 / CG;
+        const int shift = max(slots[t0], 0) & 3, c = tid % CG * 8;
+        for (int quad = tid / CG; quad < 17; quad += STEP) {
+            const int64_t first = t0 - shift + quad * 4;
+            int slot[4];
+            bool in[4];
+            int from = -1;
+            bool one = true;   // the quad's tokens are neighbours in the cache, as a request's are
 #pragma unroll
-        for (int u = 0; u < D / 32; ++u) {
-            const int c = (u * 4 + (tid >> 6)) * 8;
-            uint32_t b[8];
+            for (int e = 0; e < 4; ++e) {
+                const int64_t t = first + e;
+                in[e] = t >= t0 && t < min(t0 + 64, T);
+                slot[e] = in[e] ? slots[t] : -1;
+                if (in[e]) {
+                    if (from < 0) from = slot[e] - e;
+                    one &= slot[e] == from + e && slot[e] >= 0 && (slot[e] >> log_page) < p.n_pages;
+                }
+            }
+            if (!(in[0] | in[1] | in[2] | in[3])) continue;
+            uint4 y[4];
+            if (one && (from & 3) == 0) {
+                const char *rec;
+                int tok;
+                float unit;
+                place(in[0] ? first : max(first, t0), rec, tok, unit);
+                const char *src = rec + 64 * D + ((tok >> 2) & 3) * 16 + (tok >> 4) * 4 + c * 64;
+                uint32_t w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) b[i] = src[(c + i) * 64];
-            const uint32_t w0 = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, w1 = b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24;
-            const uint4 y = make_uint4(pair(w0, unit, Low{}), pair(w0, unit, High{}), pair(w1, unit, Low{}), pair(w1, unit, High{}));
-            *reinterpret_cast<uint4 *>(out + t * row + c * 2) = in ? y : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < 8; ++i) w[i] = *reinterpret_cast<const uint32_t *>(src + i * 64);
+                auto rows4 = [&](const uint32_t *q, uint32_t (&o)[4]) {   // bytes [channel][token] to [token][channel]
+                    const uint32_t a = __builtin_amdgcn_perm(q[1], q[0], 0x05010400u), b = __builtin_amdgcn_perm(q[3], q[2], 0x05010400u);
+                    const uint32_t d = __builtin_amdgcn_perm(q[1], q[0], 0x07030602u), f = __builtin_amdgcn_perm(q[3], q[2], 0x07030602u);
+                    o[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+                    o[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+                    o[2] = __builtin_amdgcn_perm(f, d, 0x05040100u);
+                    o[3] = __builtin_amdgcn_perm(f, d, 0x07060302u);
+                };
+                uint32_t lo[4], hi[4];
+                rows4(w, lo);
+                rows4(w + 4, hi);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    y[e] = make_uint4(pair(lo[e], unit, Low{}), pair(lo[e], unit, High{}), pair(hi[e], unit, Low{}), pair(hi[e], unit, High{}));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = make_uint4(0, 0, 0, 0);
+                    const char *rec;
+                    int tok;
+                    float unit;
+                    if (!in[e] || !place(first + e, rec, tok, unit)) continue;
+                    const uint8_t *src = reinterpret_cast<const uint8_t *>(rec) + 64 * D + ((tok >> 2) & 3) * 16 + (tok >> 4) * 4 + (tok & 3) + c * 64;
+                    uint32_t b[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) b[i] = src[i * 64];
+                    const uint32_t w0 = b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, w1 = b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24;
+                    y[e] = make_uint4(pair(w0, unit, Low{}), pair(w0, unit, High{}), pair(w1, unit, Low{}), pair(w1, unit, High{}));
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (in[e]) store_once(out + (first + e) * row + c * 2, y[e]);
         }
     } else {
         constexpr int PER = D / 8;   // threads of a token
@@ -238,7 +310,7 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__rest
             const bool in = place(t, rec, tok, unit);
             const uint2 w = *reinterpret_cast<const uint2 *>(rec + (tok >> 4) * 16 * D + (c >> 6) * 1024 + (tok & 15) * 64 + (c & 63));
             const uint4 y = make_uint4(pair(w.x, unit, Low{}), pair(w.x, unit, High{}), pair(w.y, unit, Low{}), pair(w.y, unit, High{}));
-            *reinterpret_cast<uint4 *>(out + t * row + c * 2) = in ? y : make_uint4(0, 0, 0, 0);
+            store_once(out + t * row + c * 2, in ? y : make_uint4(0, 0, 0, 0));
         }
     }
 }
@@ -248,8 +320,14 @@ hipError_t launch_append(const KvPages &p, const void *k, const void *v, int64_t
                          int S, const int *slots, int *err_word, hipStream_t stream)
 {
     const int64_t places = T / 64 + 2 * (int64_t)S;
-    hipLaunchKernelGGL((kv8_append_kernel<D, 256>), dim3((unsigned)(places * 2 * p.n_kv)), dim3(256), 0, stream, p, static_cast<const char *>(k),
-                       static_cast<const char *>(v), k_stride, v_stride, (int)T, seq_offsets, S, slots, err_word);
+    auto go = [&](auto nt) {
+        constexpr int NT = decltype(nt)::value;
+        hipLaunchKernelGGL((kv8_append_kernel<D, NT>), dim3((unsigned)(places * 2 * p.n_kv)), dim3(NT), 0, stream, p, static_cast<const char *>(k),
+                           static_cast<const char *>(v), k_stride, v_stride, (int)T, seq_offsets, S, slots, err_word);
+    };
+    // (a token or a few to a request: a wave has room for them, and four would wait for each other)
+    if (T <= 4 * (int64_t)S) go(std::integral_constant<int, 64>{});
+    else go(std::integral_constant<int, 256>{});
     return hipGetLastError();
 }
 
