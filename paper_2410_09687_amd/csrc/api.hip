@@ -22,6 +22,7 @@ hipError_t prepare_kmeans_kernels();
 hipError_t prepare_mx_kernels();
 hipError_t prepare_plan_kernels();
 hipError_t prepare_mx4_kernels();
+hipError_t prepare_i8_kernels();
 hipError_t prepare_kernels()
 {
     hipError_t e = prepare_linear_kernels();
@@ -31,6 +32,7 @@ hipError_t prepare_kernels()
     if ((e = prepare_mx_kernels()) != hipSuccess) return e;
     if ((e = prepare_plan_kernels()) != hipSuccess) return e;
     if ((e = prepare_mx4_kernels()) != hipSuccess) return e;
+    if ((e = prepare_i8_kernels()) != hipSuccess) return e;
     return prepare_route_kernels();
 }
 }  // namespace moin
@@ -734,7 +736,7 @@ int linear_i8_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, 
     const size_t u_bytes = align_up((size_t)pv.T * (size_t)a.r * 2, 256), xq_bytes = align_up((size_t)pv.T * (size_t)pitch, 256),
                  xs_bytes = align_up((size_t)pv.T * 4, 256);
     const bool gathered = gathered_pays_mx(pv, d_in, d_out, a.r), decode = gathered && a.r > 0;
-    const bool few = gathered && pv.T <= I8_FEW_TOKENS, quantised = !(few && i8_few_quantises(pv.T, d_in));
+    const bool few = gathered && pv.T <= i8_few_most(d_out), quantised = !(few && i8_few_quantises(pv.T, d_in));
     size_t yb_bytes = 0;
     if (decode) {
         if (few) m.plain_splits = 1;
@@ -2061,7 +2063,7 @@ int moin_i8_linear(moin_ctx *ctx, const void *x, int64_t T, const void *Wq, cons
     if (rc != MOIN_OK) return rc;
     char *xq = static_cast<char *>(ctx->ws);
     float *xs = reinterpret_cast<float *>(xq + xq_bytes);
-    const bool few = T <= I8_FEW_TOKENS;
+    const bool few = T <= i8_few_most(d_out);
     if (!(few && i8_few_quantises(T, d_in)) &&
         timed(ctx, MOIN_K_MX_QUANT, st, [&] { return launch_i8_quantize(x, T, d_in, xq, xs, st); }) != hipSuccess)
         return MOIN_EHIP;

@@ -1,7 +1,7 @@
 // Matrix product in 8-bit integers: rows of x [T, d_in] and of the weight [d_out, d_in] have a scale each,
 //     s = max(amax / 127 in fp32, 2^-126),   code = x / s to the nearest, ties to even,   y = s_t s_o sum_c xq_c wq_c,
 // sums in int32, exact; one rounding to fp32, two for the scales.  A row with an infinity or a NaN has a scale of NaN and codes of 0.
-// This file: the quantiser, and the product of up to 64 tokens, bound by the weight's bytes.  Larger ones run on the
+// This file: the quantiser, and the product of up to 128 tokens, bound by the weight's bytes.  Larger ones run on the
 // streams of tiles of mx.hip.
 #include <algorithm>
 
@@ -28,29 +28,31 @@ __device__ __forceinline__ float i8_scale_of(uint32_t amax)
     if (amax >= 0x7F800000u) return bits_f32(0x7FC00000u);
     return fmaxf(__fdiv_rn(bits_f32(amax), 127.f), bits_f32(0x00800000u));
 }
-// x / s to the nearest.  The product with the reciprocal may land on the wrong side of a midpoint; what it leaves, x - q s, is exact in fp32 (x
-// has 8 bits, s 24, q 7, and x's last bit lies above s's) and shows it.
-__device__ __forceinline__ int i8_code(float x, float s, float inv)
-{
-    float q = rintf(x * inv);
-    const float left = fmaf(-q, s, x), half = 0.5f * s;
-    if (fabsf(left) > half || (fabsf(left) == half && ((int)q & 1))) q += copysignf(1.f, left);
-    return (int)fminf(fmaxf(q, -127.f), 127.f);
-}
+// x / s to the nearest, eight values.  The product with the reciprocal may land on the wrong side of a midpoint; what it leaves, x - q s, is exact
+// in fp32 (x has 8 bits, s 24, q 7, and x's last bit lies above s's) and shows it: where none of eight leaves half a step or more, all are right.
+// (Magnitudes above 127 do not come: s is the largest value's 127th part, rounded.)
 __device__ __forceinline__ uint2 i8_codes(const uint4 &v, float s, float inv)
 {
     if (!(s == s)) return make_uint2(0, 0);   // (the scale alone says so)
-    uint32_t c[2];
+    float q[8], most = 0.f;
+    auto x = [&](int i) { return bits_f32(i & 1 ? word(v, i >> 1) & 0xFFFF0000u : word(v, i >> 1) << 16); };
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        c[i] = 0;
+    for (int i = 0; i < 8; ++i) {
+        q[i] = rintf(x(i) * inv);
+        most = fmaxf(most, fabsf(fmaf(-q[i], s, x(i))));
+    }
+    const float half = 0.5f * s;
+    if (most >= half) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t w = word(v, 2 * i + e / 2);
-            c[i] |= (uint32_t)(i8_code(bits_f32(e & 1 ? w & 0xFFFF0000u : w << 16), s, inv) & 255) << 8 * e;
+        for (int i = 0; i < 8; ++i) {
+            const float left = fmaf(-q[i], s, x(i));
+            if (fabsf(left) > half || (fabsf(left) == half && ((int)q[i] & 1))) q[i] += copysignf(1.f, left);
         }
     }
-    return make_uint2(c[0], c[1]);
+    uint32_t c[2] = {0, 0};   // (of q + 128, whose high bit is then turned)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(q[i] + 128.f, i % 4, c[i / 4]);
+    return make_uint2(c[0] ^ 0x80808080u, c[1] ^ 0x80808080u);
 }
 
 // A row to WAVES waves (one of four rows a workgroup, or all four of one): its largest magnitude, then its codes, zeros up to the pitch.  Rows of up to
@@ -95,6 +97,10 @@ __global__ __launch_bounds__(256) void i8_quantize_kernel(const char *__restrict
         *reinterpret_cast<uint2 *>(out + c * 8) = c < n8 ? i8_codes(*reinterpret_cast<const uint4 *>(x + (int64_t)c * 16), s, inv) : make_uint2(0, 0);
 }
 
+// A workgroup quantises the tokens itself up to this many pieces of 512 columns.
+constexpr int FUSED_ITEMS = 24;
+int fused_items(int64_t T, int d_in) { return T > 16 ? FUSED_ITEMS + 1 : (int)T * ((i8_pitch(d_in) + 511) / 512); }
+
 struct FewArgs {
     const char *x, *xq;    // bf16 tokens (FUSED) or their codes
     const float *xs;
@@ -104,87 +110,121 @@ struct FewArgs {
     int T, d_in, pitch, d_out, y_f32;
 };
 
-// 16 outputs a workgroup, all tokens; its KW waves take the 128-byte blocks of the contraction in turn and add their sums at the end.  A lane's
+// 16 RT outputs a workgroup, all tokens; its KW waves take a range of the contraction's 128-byte blocks each and add their sums at the end.  A lane's
 // operands are 16 bytes of a row as they lie in memory (the order of the contraction is free).
 // FUSED: the workgroup quantises the tokens itself, into LDS, while its first weights are on their way.
-template <int NT, int KW, bool FUSED>
+template <int RT, int NT, int KW, bool FUSED>
 __global__ __launch_bounds__(64 * KW) void i8_few_kernel(FewArgs a)
 {
-    constexpr int AHEAD = NT > 2 ? 2 : 4;   // blocks of a wave whose loads are on their way together
+    constexpr int AHEAD = NT > 1 ? 1 : 2;                    // blocks of a wave whose loads are on their way together
+    constexpr int KEEP = (FUSED_ITEMS + KW - 1) / KW;        // pieces of 512 columns of the tokens that a wave quantises
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16, nb = a.pitch / 128, lp = a.pitch + 16;
-    const char *w = a.W + (int64_t)min(n0 + m, a.d_out - 1) * a.pitch + g * 32;
-    uint4 wa[AHEAD][2];
+    const int n0 = blockIdx.x * 16 * RT, nb = a.pitch / 128, lp = a.pitch + 16;
+    const int per = (nb + KW - 1) / KW, first = wave * per, end = min(nb, first + per);
+    const char *w[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) w[rt] = a.W + (int64_t)min(n0 + rt * 16 + m, a.d_out - 1) * a.pitch + g * 32;
+    uint4 wa[AHEAD][RT][2];
     auto load_w = [&](int b0) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-            const char *p = w + min(b0 + u * KW, nb - 1) * 128;
-            wa[u][0] = *reinterpret_cast<const uint4 *>(p);
-            wa[u][1] = *reinterpret_cast<const uint4 *>(p + 16);
-        }
+        for (int u = 0; u < AHEAD; ++u)
+            if (b0 + u < end)   // (uniform)
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    const char *p = w[rt] + (b0 + u) * 128;
+                    wa[u][rt][0] = *reinterpret_cast<const uint4 *>(p);
+                    wa[u][rt][1] = *reinterpret_cast<const uint4 *>(p + 16);
+                }
     };
-    load_w(wave);
     float *lds_s = reinterpret_cast<float *>(smem + (FUSED ? a.T * lp : 0));   // [16 NT] the tokens' scales
     if constexpr (FUSED) {
-        const int n8 = a.d_in / 8;
-        for (int t = wave; t < a.T; t += KW) {
-            const char *x = a.x + (int64_t)t * a.d_in * 2;
-            uint32_t amax = 0;
-            for (int c = lane; c < n8; c += 64) amax = max(amax, bf16x8_amax(*reinterpret_cast<const uint4 *>(x + c * 16)));
+        // pieces of 512 columns, dealt to the waves: all of them read at once, the largest magnitudes meet in LDS
+        uint32_t *amax = reinterpret_cast<uint32_t *>(lds_s);
+        const int n8 = a.d_in / 8, p8 = a.pitch / 8, segs = (p8 + 63) >> 6, items = a.T * segs;
+        uint4 x[KEEP];
 #pragma unroll
-            for (int d = 1; d < 64; d <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, d));
-            const float s = i8_scale_of(amax), inv = 1.f / s;
-            if (lane == 0) lds_s[t] = s;
-            for (int c = lane; c < a.pitch / 8; c += 64)
-                *reinterpret_cast<uint2 *>(smem + t * lp + c * 8) = c < n8 ? i8_codes(*reinterpret_cast<const uint4 *>(x + c * 16), s, inv) : make_uint2(0, 0);
+        for (int u = 0; u < KEEP; ++u) {
+            const int i = wave + u * KW, t = i / segs, c = (i - t * segs) * 64 + lane;
+            x[u] = i < items && c < n8 ? *reinterpret_cast<const uint4 *>(a.x + ((int64_t)t * n8 + c) * 16) : make_uint4(0, 0, 0, 0);
         }
+        if (threadIdx.x < 16) amax[threadIdx.x] = 0;
+        load_w(first);
+        lds_barrier();
+#pragma unroll
+        for (int u = 0; u < KEEP; ++u) {
+            const int i = wave + u * KW;
+            if (i >= items) break;
+            uint32_t top = bf16x8_amax(x[u]);
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+            if (lane == 0) atomicMax(&amax[i / segs], top);
+        }
+        lds_barrier();
+        float s_t = 0.f;
+        if (threadIdx.x < 16) s_t = i8_scale_of(amax[threadIdx.x]);
+#pragma unroll
+        for (int u = 0; u < KEEP; ++u) {
+            const int i = wave + u * KW, t = i / segs, c = (i - t * segs) * 64 + lane;
+            if (i >= items) break;
+            const float s = i8_scale_of(amax[t]);
+            if (c < p8) *reinterpret_cast<uint2 *>(smem + t * lp + c * 8) = i8_codes(x[u], s, 1.f / s);   // (zeros beyond the columns)
+        }
+        lds_barrier();
+        if (threadIdx.x < 16) lds_s[threadIdx.x] = s_t;
     } else {
+        load_w(first);
         for (int t = threadIdx.x; t < 16 * NT; t += 64 * KW) lds_s[t] = a.xs[min(t, a.T - 1)];
     }
-    lds_barrier();
-    i32x4_t acc[NT];
+    i32x4_t acc[RT][NT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) acc[nt] = i32x4_t{0, 0, 0, 0};
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) acc[rt][nt] = i32x4_t{0, 0, 0, 0};
     const char *x[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int t = min(nt * 16 + m, a.T - 1);
         x[nt] = FUSED ? smem + t * lp + g * 32 : a.xq + (int64_t)t * a.pitch + g * 32;
     }
-    for (int b0 = wave; b0 < nb; b0 += KW * AHEAD) {
-        i32x4_t av[AHEAD][2];
-        uint4 xb[AHEAD][NT][2];
+    for (int b0 = first; b0 < end; b0 += AHEAD) {
+        i32x4_t av[AHEAD][RT][2], xb[AHEAD][NT][2];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const bool in = b0 + u * KW < nb;
-            const int at = min(b0 + u * KW, nb - 1) * 128;
+            const int at = min(b0 + u, nb - 1) * 128;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int z = 0; z < 2; ++z) xb[u][nt][z] = *reinterpret_cast<const uint4 *>(x[nt] + at + z * 16);
+                for (int z = 0; z < 2; ++z) xb[u][nt][z] = *reinterpret_cast<const i32x4_t *>(x[nt] + at + z * 16);
 #pragma unroll
-            for (int z = 0; z < 2; ++z) av[u][z] = __builtin_bit_cast(i32x4_t, in ? wa[u][z] : make_uint4(0, 0, 0, 0));
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int z = 0; z < 2; ++z) av[u][rt][z] = __builtin_bit_cast(i32x4_t, wa[u][rt][z]);
         }
-        if (b0 + KW * AHEAD < nb) load_w(b0 + KW * AHEAD);
+        load_w(b0 + AHEAD);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
+            if (b0 + u < end)
 #pragma unroll
-            for (int z = 0; z < 2; ++z)
+                for (int z = 0; z < 2; ++z)
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-                    acc[nt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(av[u][z], __builtin_bit_cast(i32x4_t, xb[u][nt][z]), acc[nt], 0, 0, 0);
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+                            acc[rt][nt] = __builtin_amdgcn_mfma_i32_16x16x64_i8(av[u][rt][z], xb[u][nt][z], acc[rt][nt], 0, 0, 0);
     }
     // the waves' sums, through LDS behind the scales
     i32x4_t *sums = reinterpret_cast<i32x4_t *>(lds_s + 16 * NT);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) sums[(wave * NT + nt) * 64 + lane] = acc[nt];
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) sums[((wave * RT + rt) * NT + nt) * 64 + lane] = acc[rt][nt];
     lds_barrier();
-    for (int i = threadIdx.x; i < NT * 64; i += 64 * KW) {
+    for (int i = threadIdx.x; i < RT * NT * 64; i += 64 * KW) {
         i32x4_t v = sums[i];
 #pragma unroll
-        for (int k = 1; k < KW; ++k) v += sums[k * NT * 64 + i];
-        const int t = (i >> 6) * 16 + (i & 15), o = n0 + ((i & 63) >> 4) * 4;
+        for (int k = 1; k < KW; ++k) v += sums[k * RT * NT * 64 + i];
+        const int t = (i >> 6) % NT * 16 + (i & 15), o = n0 + (i >> 6) / NT * 16 + ((i & 63) >> 4) * 4;
         if (t >= a.T || o >= a.d_out) continue;
         const float st = lds_s[t];
         const f32x4_t so = *reinterpret_cast<const f32x4_t *>(a.ws + o);
@@ -197,28 +237,21 @@ __global__ __launch_bounds__(64 * KW) void i8_few_kernel(FewArgs a)
     }
 }
 
-constexpr int FUSED_BYTES = 32768;   // of the tokens' codes that a workgroup keeps in LDS
-
-template <int NT, int KW, bool FUSED>
+constexpr int few_lds(int RT, int NT, int KW) { return 16 * NT * 4 + KW * RT * NT * 1024; }   // scales, the waves' sums
+template <int RT, int NT, int KW, bool FUSED>
 hipError_t few(const FewArgs &a, hipStream_t stream)
 {
-    const size_t lds = (FUSED ? (size_t)a.T * (a.pitch + 16) : 0) + 16 * NT * 4 + (size_t)KW * NT * 1024;
-    hipLaunchKernelGGL((i8_few_kernel<NT, KW, FUSED>), dim3((unsigned)((a.d_out + 15) / 16)), dim3(64 * KW), lds, stream, a);
+    const size_t lds = (FUSED ? (size_t)a.T * (a.pitch + 16) : 0) + few_lds(RT, NT, KW);
+    hipLaunchKernelGGL((i8_few_kernel<RT, NT, KW, FUSED>), dim3((unsigned)((a.d_out + 16 * RT - 1) / (16 * RT))), dim3(64 * KW), lds, stream, a);
     return hipGetLastError();
 }
-template <int KW>
-hipError_t few_tokens(const FewArgs &a, bool fused, hipStream_t stream)
-{
-    if (fused) return few<1, KW, true>(a, stream);
-    return a.T <= 16 ? few<1, KW, false>(a, stream) : a.T <= 32 ? few<2, KW, false>(a, stream) : few<4, KW, false>(a, stream);
-}
-
 }  // namespace
 
 hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *codes, float *scales, hipStream_t stream)
 {
     if (rows <= 0) return hipSuccess;
-    if (rows >= 4 * compute_units())
+    // (a row of more than 2048 columns to a wave would be read twice: 8192 x 8192 70 us)
+    if (rows >= 4 * compute_units() && cols <= 2048)
         hipLaunchKernelGGL(i8_quantize_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, static_cast<const char *>(src), rows, cols,
                            i8_pitch(cols), static_cast<char *>(codes), scales);
     else
@@ -227,16 +260,37 @@ hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *cod
     return hipGetLastError();
 }
 
-bool i8_few_quantises(int64_t T, int d_in) { return T <= 16 && T * i8_pitch(d_in) <= FUSED_BYTES; }
+// Up to 128 tokens; 64 where the weight has rows enough for the tiles of 128 x 128 to fill the chip.  Us with and without (few, tiles): 128 tokens
+// 2048 -> 256 13 / 20, 2048 -> 5632 16 / 20, 5632 -> 2048 29 / 42, 8192 -> 8192 45 / 77, but 8192 -> 28672 103 / 88.
+int i8_few_most(int d_out) { return (d_out + 15) / 16 >= 4 * compute_units() ? 64 : 128; }
+
+bool i8_few_quantises(int64_t T, int d_in) { return fused_items(T, d_in) <= FUSED_ITEMS; }
 
 hipError_t launch_i8_few(const void *x, const void *xq, const float *xs, const void *Wq, const float *ws, int T, int d_in, int d_out, void *y,
                          int y_f32, hipStream_t stream)
 {
     const FewArgs a{static_cast<const char *>(x), static_cast<const char *>(xq), xs, static_cast<const char *>(Wq), ws, static_cast<char *>(y),
                     T, d_in, i8_pitch(d_in), d_out, y_f32};
-    const bool fused = i8_few_quantises(T, d_in);
-    const int tiles = (d_out + 15) / 16;
-    return tiles * 2 < 3 * compute_units() ? few_tokens<8>(a, fused, stream) : few_tokens<4>(a, fused, stream);
+    const int tiles = (d_out + 15) / 16, n_cus = compute_units();
+    const bool wide = tiles >= 4 * n_cus, broad = tiles * 4 >= 5 * n_cus;
+    if (i8_few_quantises(T, d_in)) return wide ? few<2, 1, 4, true>(a, stream) : tiles * 2 >= 3 * n_cus ? few<1, 1, 8, true>(a, stream) : few<1, 1, 16, true>(a, stream);
+    if (T <= 16) return wide ? few<2, 1, 4, false>(a, stream) : few<1, 1, 8, false>(a, stream);
+    if (T <= 32) return wide ? few<4, 2, 4, false>(a, stream) : broad ? few<2, 2, 4, false>(a, stream) : few<1, 2, 8, false>(a, stream);
+    if (T <= 64) return wide ? few<4, 4, 4, false>(a, stream) : broad ? few<2, 4, 8, false>(a, stream) : few<1, 4, 8, false>(a, stream);
+    return wide ? few<4, 8, 4, false>(a, stream) : broad ? few<2, 8, 4, false>(a, stream) : few<1, 8, 8, false>(a, stream);
+}
+
+hipError_t prepare_i8_kernels()
+{
+    auto allow = [](auto kernel, int bytes) {
+        return hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    };
+    hipError_t e = allow(&i8_few_kernel<4, 8, 4, false>, few_lds(4, 8, 4));
+    if (e == hipSuccess) e = allow(&i8_few_kernel<2, 8, 4, false>, few_lds(2, 8, 4));
+    if (e == hipSuccess) e = allow(&i8_few_kernel<1, 8, 8, false>, few_lds(1, 8, 8));
+    if (e == hipSuccess) e = allow(&i8_few_kernel<2, 4, 8, false>, few_lds(2, 4, 8));
+    if (e == hipSuccess) e = allow(&i8_few_kernel<4, 4, 4, false>, few_lds(4, 4, 4));
+    return e;
 }
 
 }  // namespace moin

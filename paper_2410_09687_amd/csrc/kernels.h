@@ -274,9 +274,9 @@ int compute_units();   // of the current device
 // Base in 8-bit integers (i8.hip, mx.hip): rows of codes padded with zeros to this many bytes, a scale of fp32 for each row.
 constexpr int i8_pitch(int cols) { return cols <= 256 ? 256 : (cols + 127) / 128 * 128; }
 constexpr int I8_MAX_COLS = 131072;   // sums of as many products of 127 x 127 fit 31 bits
-constexpr int I8_FEW_TOKENS = 64;     // up to here launch_i8_few
 hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *codes, float *scales, hipStream_t stream);
-// y [T, d_out] of up to I8_FEW_TOKENS tokens, whose codes and scales are given -- or, where launch_i8_few_quantises, x itself.
+// y [T, d_out] of a few tokens (launch_i8_few, up to i8_few_most), whose codes and scales are given -- or, where launch_i8_few_quantises, x itself.
+int i8_few_most(int d_out);
 bool i8_few_quantises(int64_t T, int d_in);
 hipError_t launch_i8_few(const void *x, const void *xq, const float *xs, const void *Wq, const float *ws, int T, int d_in, int d_out, void *y,
                          int y_f32, hipStream_t stream);
