@@ -94,14 +94,15 @@ __global__ __launch_bounds__(NT) void kv8_append_kernel(KvPages p, const char *_
         return;
     }
     if (n_all == 0 || r < 0 || (id >= S && r == 0)) return;
-    const int slot0 = uniform(slots[tok0]), log_page = p.log_blocks + 6;
+    // (a request's first block: its slots and the first of them in one trip to memory)
+    const int log_page = p.log_blocks + 6, ahead = slots[tok0 + (id < S ? min(lane, n_all - 1) : 0)], slot0 = uniform(ahead);
     if (slot0 < 0 || (slot0 >> log_page) >= p.n_pages) {   // a request that got no pages, or one that is given others' than there are
         if (slot0 != -1 && tid == 0) atomicOr(err_word, ERR_BAD_PAGE);
         return;
     }
     const int first = max(0, 64 * r - (slot0 & 63)), n = min(n_all, 64 * (r + 1) - (slot0 & 63)) - first;   // its tokens in this block
     if (n <= 0) return;
-    const int slot = slots[tok0 + first + min(lane, n - 1)], start = uniform(slot);
+    const int slot = id < S ? __shfl(ahead, min(lane, n - 1)) : slots[tok0 + first + min(lane, n - 1)], start = uniform(slot);
     const bool wrong = start < 0 || (start >> log_page) >= p.n_pages || (start & 63) + n > 64;
     if (wrong || __ballot(slot != start + min(lane, n - 1))) {   // a page that there is not, or tokens that do not follow each other
         if (tid == 0) atomicOr(err_word, ERR_BAD_PAGE);
