@@ -736,7 +736,9 @@ int linear_i8_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, 
     const size_t u_bytes = align_up((size_t)pv.T * (size_t)a.r * 2, 256), xq_bytes = align_up((size_t)pv.T * (size_t)pitch, 256),
                  xs_bytes = align_up((size_t)pv.T * 4, 256);
     const bool gathered = gathered_pays_mx(pv, d_in, d_out, a.r), decode = gathered && a.r > 0;
-    const bool few = gathered && pv.T <= i8_few_most(d_out), quantised = !(few && i8_few_quantises(pv.T, d_in));
+    // (with adapters the tiles' sums may be cut into parts, which the expand adds.  Us, few tokens / tiles: 64 tokens 2048 -> 2048 22 / 25, 128 5632 -> 2048
+    // 48 / 40, 4096 -> 4096 42 / 38)
+    const bool few = gathered && (decode ? pv.T <= 64 : i8_few_pays(pv.T, d_out)), quantised = !(few && i8_few_quantises(pv.T, d_in));
     size_t yb_bytes = 0;
     if (decode) {
         if (few) m.plain_splits = 1;
@@ -2063,7 +2065,7 @@ int moin_i8_linear(moin_ctx *ctx, const void *x, int64_t T, const void *Wq, cons
     if (rc != MOIN_OK) return rc;
     char *xq = static_cast<char *>(ctx->ws);
     float *xs = reinterpret_cast<float *>(xq + xq_bytes);
-    const bool few = T <= i8_few_most(d_out);
+    const bool few = i8_few_pays(T, d_out);
     if (!(few && i8_few_quantises(T, d_in)) &&
         timed(ctx, MOIN_K_MX_QUANT, st, [&] { return launch_i8_quantize(x, T, d_in, xq, xs, st); }) != hipSuccess)
         return MOIN_EHIP;

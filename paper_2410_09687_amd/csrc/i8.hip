@@ -121,6 +121,14 @@ __global__ __launch_bounds__(64 * KW) void i8_few_kernel(FewArgs a)
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), m = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * 16 * RT, nb = a.pitch / 128, lp = a.pitch + 16;
+    if (blockIdx.y) {   // a group of 128 tokens behind the first
+        const int t0 = blockIdx.y * 128;
+        a.xq += (int64_t)t0 * a.pitch;
+        a.xs += t0;
+        a.y += (int64_t)t0 * a.d_out * (a.y_f32 ? 4 : 2);
+        a.T -= t0;
+    }
+    a.T = min(a.T, 128);
     const int per = (nb + KW - 1) / KW, first = wave * per, end = min(nb, first + per);
     const char *w[RT];
 #pragma unroll
@@ -242,7 +250,8 @@ template <int RT, int NT, int KW, bool FUSED>
 hipError_t few(const FewArgs &a, hipStream_t stream)
 {
     const size_t lds = (FUSED ? (size_t)a.T * (a.pitch + 16) : 0) + few_lds(RT, NT, KW);
-    hipLaunchKernelGGL((i8_few_kernel<RT, NT, KW, FUSED>), dim3((unsigned)((a.d_out + 16 * RT - 1) / (16 * RT))), dim3(64 * KW), lds, stream, a);
+    hipLaunchKernelGGL((i8_few_kernel<RT, NT, KW, FUSED>), dim3((unsigned)((a.d_out + 16 * RT - 1) / (16 * RT)), (unsigned)((a.T + 127) / 128)),
+                       dim3(64 * KW), lds, stream, a);
     return hipGetLastError();
 }
 }  // namespace
@@ -260,9 +269,14 @@ hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *cod
     return hipGetLastError();
 }
 
-// Up to 128 tokens; 64 where the weight has rows enough for the tiles of 128 x 128 to fill the chip.  Us with and without (few, tiles): 128 tokens
-// 2048 -> 256 13 / 20, 2048 -> 5632 16 / 20, 5632 -> 2048 29 / 42, 8192 -> 8192 45 / 77, but 8192 -> 28672 103 / 88.
-int i8_few_most(int d_out) { return (d_out + 15) / 16 >= 4 * compute_units() ? 64 : 128; }
+// Up to 128 tokens; 64 where the weight has rows enough for the tiles of 128 x 128 to fill the chip; more in groups of 128 as long as each workgroup
+// has a compute unit of its own.  Us with and without (few, tiles): 128 tokens 2048 -> 256 13 / 20, 2048 -> 5632 16 / 20, 5632 -> 2048 29 / 42, 8192 -> 8192
+// 45 / 77, but 8192 -> 28672 103 / 88; 256 tokens 2048 -> 2048 14 / 20, 5632 -> 2048 29 / 42; 1000 2048 -> 256 15 / 21.
+bool i8_few_pays(int64_t T, int d_out)
+{
+    const int64_t tiles = (d_out + 15) / 16, n_cus = compute_units();
+    return T <= 64 || (T <= 128 && tiles < 4 * n_cus) || (T + 127) / 128 * tiles <= n_cus;
+}
 
 bool i8_few_quantises(int64_t T, int d_in) { return fused_items(T, d_in) <= FUSED_ITEMS; }
 

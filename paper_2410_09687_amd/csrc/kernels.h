@@ -275,8 +275,8 @@ int compute_units();   // of the current device
 constexpr int i8_pitch(int cols) { return cols <= 256 ? 256 : (cols + 127) / 128 * 128; }
 constexpr int I8_MAX_COLS = 131072;   // sums of as many products of 127 x 127 fit 31 bits
 hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *codes, float *scales, hipStream_t stream);
-// y [T, d_out] of a few tokens (launch_i8_few, up to i8_few_most), whose codes and scales are given -- or, where launch_i8_few_quantises, x itself.
-int i8_few_most(int d_out);
+// y [T, d_out] of few tokens (where i8_few_pays), whose codes and scales are given -- or, where launch_i8_few_quantises, x itself.
+bool i8_few_pays(int64_t T, int d_out);
 bool i8_few_quantises(int64_t T, int d_in);
 hipError_t launch_i8_few(const void *x, const void *xq, const float *xs, const void *Wq, const float *ws, int T, int d_in, int d_out, void *y,
                          int y_f32, hipStream_t stream);
