@@ -56,7 +56,7 @@ struct KvTile {            // one workgroup's work, per kv head
 };
 
 struct KvPlanView {
-    int *head;             // [4]: records of either list; free pages before the step
+    int *head;             // [4]: records of either list; free pages before the step; tiles of many rows, also those that the list has no room for
     int4 *req;             // [S] {keys before, first of its pages among those the step deals or -1, pages dealt, first record in `tile`}
     int2 *req_tiles;       // [S] {parts of each of its tiles, first place of their partial results}
     KvTile *few, *tile;

@@ -112,6 +112,19 @@ def test_many_requests():
     Step(9, rng.integers(0, 300, 700), rng.integers(0, 2, 700), 4, 2, 64).check()
 
 
+@pytest.mark.parametrize("heads,H,D", [(8, 2, 64), (3, 3, 128), (200, 1, 64), (130, 2, 64)])
+@pytest.mark.parametrize("S", [2, 7, 64, 65])
+def test_tiles_of_several_requests_are_all_taken(S, heads, H, D):
+    """Lists of tiles that go by the keys that they see (up to 64 requests), ties and requests without tokens among them: no row is left out."""
+    rng = np.random.default_rng(S + heads)
+    new = rng.choice([0, 9, 9, 40, 64, 65, 70], S)
+    new[0] = 70
+    kv = rng.choice([0, 0, 31, 64, 300], S)
+    s = Step(S, kv if S < 64 else kv % 65, new if S < 64 else new % 41 + (np.arange(S) == 1) * 9, heads, H, D)
+    out = torch.full((s.T, heads, D), float("nan"), dtype=BF16, device="cuda")
+    s.check(out=out)
+
+
 def test_loud_scores_and_other_scales():
     s = Step(11, [200, 50, 1000], [1, 60, 3], 8, 2, 64, loud=30.0)
     s.check(F32)
