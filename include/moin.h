@@ -665,7 +665,7 @@ int moin_kv_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pag
  *   q [T, n_heads, head_dim], k [T, n_kv, head_dim]  x_dt; q_out, k_out the same shapes, bf16; rows of
  *             tokens `stride` elements apart (multiples of 8, of 4 for fp32 inputs), so that they may be columns of one
  *             projection's output.  n_heads or n_kv may be 0 (q or k alone).  The outputs may be the inputs
- *             themselves, with their strides, else they must not overlap them
+ *             themselves (bf16, the same strides), else they must not overlap them
  *   positions [T] int32 (any), freqs [rot_dim / 2] double: radians a position.  NULL without rotation
  *   q_gain, k_gain [head_dim] bf16 or NULL (ones; without MOIN_QK_NORM they must be)
  * head_dim 64, 128 or 256; rot_dim a multiple of 16; pointers 16-byte aligned.  Angles are reduced in 64 bits;

@@ -2016,6 +2016,9 @@ int moin_qk_norm_rope(moin_ctx *ctx, const void *q, const void *k, moin_dtype x_
                out_stride >= row && stride <= far && out_stride <= far;
     };
     if (!rows_ok(q, q_out, q_stride, q_out_stride, n_heads) || !rows_ok(k, k_out, k_stride, k_out_stride, n_kv)) return MOIN_EINVAL;
+    // (in place: bf16 over bf16, row over row)
+    if ((n_heads > 0 && q_out == q && (x_dt != MOIN_BF16 || q_out_stride != q_stride)) || (n_kv > 0 && k_out == k && (x_dt != MOIN_BF16 || k_out_stride != k_stride)))
+        return MOIN_EINVAL;
     if (rot_dim > 0 && (!positions || !freqs || misaligned(freqs, 8))) return MOIN_EINVAL;
     if (misaligned(q_gain, 16) || misaligned(k_gain, 16)) return MOIN_EINVAL;
     DeviceGuard guard(ctx->device);

@@ -28,6 +28,13 @@ __device__ __forceinline__ bf16x8_t e4m3_operand(uint32_t a, uint32_t b, float s
     return operand(e4m3_low(a, scale), e4m3_high(a, scale), e4m3_low(b, scale), e4m3_high(b, scale));
 }
 
+// Records of tiles of few rows are read once: past the caches.  (256 requests of up to 4096 keys 53.9 us, 50.6 like this; two of 100000 and more 112, 104.)
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_once(const char *p)
+{
+    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(p)));
+}
+
 template <int D_>
 struct E4M3 {
     static constexpr int D = D_, NJ = D / 16, KD = D / 32, KL = D / 64;
@@ -61,9 +68,9 @@ struct E4M3 {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int l = 0; l < KL; ++l) r.k[i][l] = *reinterpret_cast<const uint4 *>(s.rec + (at.k + (i * KL + l) * 1024));
+            for (int l = 0; l < KL; ++l) r.k[i][l] = load_once(s.rec + (at.k + (i * KL + l) * 1024));
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) r.v[j] = *reinterpret_cast<const uint4 *>(s.rec + (at.v + j * 1024));
+        for (int j = 0; j < NJ; ++j) r.v[j] = load_once(s.rec + (at.v + j * 1024));
     }
 
     __device__ __forceinline__ static int k_channel(int j, int g) { return (j >> 1) * 64 + g * 16 + (j & 1) * 8; }

@@ -167,6 +167,10 @@ def test_refusals():
         with pytest.raises(moin.MoinError) as e:
             run(**kw)
         assert e.value.code == -1
+    lib, st = moin.load(), moin._stream_ptr()
+    for dt, ostride in ((0, 640), (1, 768)):      # in place: fp32 over itself, other strides
+        assert lib.moin_qk_norm_rope(ctx()._h, qkv.data_ptr(), None, dt, 640, 0, 2, 8, 0, 64, None, None, 0, 0, None, None, 1.0, qkv.data_ptr(), None,
+                                     ostride, 0, st) == -1
     for kw in (dict(positions=pos), dict(freqs=f), dict(positions=pos[:3], freqs=f), dict(q=q[:3]), dict(q=q[0]), dict(q=qkv[:, 0:8:2]),
                dict(q_gain=gains[0][:32]), dict(out=(q,)), dict(out=(q[:, :4], k)), dict(q=q.cpu())):
         with pytest.raises(ValueError):
