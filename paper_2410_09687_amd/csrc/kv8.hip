@@ -235,9 +235,11 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__rest
     if (is_v) {
         // Four tokens that lie in one word of every channel, eight channels: eight words, turned into the tokens' rows with v_perm.  The batch's tokens
         // need not begin where the cache's words do: the first and last quads are then cut off, and one more is needed.
-        constexpr int CG = D / 8, STEP = 256 / CG;
-        const int shift = max(slots[t0], 0) & 3, c = tid % CG * 8;
-        for (int quad = tid / CG; quad < 17; quad += STEP) {
+        // A wave takes 8 quads x 8 groups of channels: 32 bytes of a channel's run, 128 of a token's row.
+        const int shift = max(slots[t0], 0) & 3, lane = tid & 63;
+        for (int b = tid >> 6; b < 3 * (D / 64); b += 4) {
+            const int quad = b / (D / 64) * 8 + (lane & 7), c = (b % (D / 64) * 8 + (lane >> 3)) * 8;
+            if (quad > 16) continue;
             const int64_t first = t0 - shift + quad * 4;
             int slot[4];
             bool in[4];
