@@ -55,16 +55,16 @@ __device__ __forceinline__ uint2 i8_codes(const uint4 &v, float s, float inv)
     return make_uint2(c[0] ^ 0x80808080u, c[1] ^ 0x80808080u);
 }
 
-// A row to WAVES waves (one of four rows a workgroup, or all four of one): its largest magnitude, then its codes, zeros up to the pitch.  Rows of up to
+// A row to WAVES waves (1: four rows a workgroup; 4 or 16: one): its largest magnitude, then its codes, zeros up to the pitch.  Rows of up to
 // KEEP chunks of 8 a lane stay in registers between the two.
 template <int WAVES>
-__global__ __launch_bounds__(256) void i8_quantize_kernel(const char *__restrict__ src, int64_t rows, int cols, int pitch, char *__restrict__ codes,
+__global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void i8_quantize_kernel(const char *__restrict__ src, int64_t rows, int cols, int pitch, char *__restrict__ codes,
                                                           float *__restrict__ scales)
 {
-    constexpr int N = WAVES * 64, KEEP = 4;
-    __shared__ uint32_t lds_amax[4];
+    constexpr int N = WAVES * 64, KEEP = WAVES == 16 ? 1 : 4;
+    __shared__ uint32_t lds_amax[WAVES];
     const int wave = uniform(threadIdx.x >> 6), tid = threadIdx.x % N;
-    const int64_t row = (int64_t)blockIdx.x * (4 / WAVES) + (WAVES == 4 ? 0 : wave);
+    const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * 4 + wave : (int64_t)blockIdx.x;
     if (row >= rows) return;
     const char *x = src + row * cols * 2;
     const int n8 = cols / 8;
@@ -80,10 +80,11 @@ __global__ __launch_bounds__(256) void i8_quantize_kernel(const char *__restrict
     for (int c = KEEP * N + tid; c < n8; c += N) amax = max(amax, bf16x8_amax(*reinterpret_cast<const uint4 *>(x + (int64_t)c * 16)));
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, d));
-    if constexpr (WAVES == 4) {
+    if constexpr (WAVES > 1) {
         if ((tid & 63) == 0) lds_amax[wave] = amax;
         lds_barrier();
-        amax = max(max(lds_amax[0], lds_amax[1]), max(lds_amax[2], lds_amax[3]));
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) amax = max(amax, lds_amax[w]);
     }
     const float s = i8_scale_of(amax), inv = 1.f / s;
     if (tid == 0) scales[row] = s;
@@ -259,13 +260,15 @@ hipError_t few(const FewArgs &a, hipStream_t stream)
 hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *codes, float *scales, hipStream_t stream)
 {
     if (rows <= 0) return hipSuccess;
-    // (a row of more than 2048 columns to a wave would be read twice: 8192 x 8192 70 us)
-    if (rows >= 4 * compute_units() && cols <= 2048)
-        hipLaunchKernelGGL(i8_quantize_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, static_cast<const char *>(src), rows, cols,
-                           i8_pitch(cols), static_cast<char *>(codes), scales);
-    else
-        hipLaunchKernelGGL(i8_quantize_kernel<4>, dim3((unsigned)rows), dim3(256), 0, stream, static_cast<const char *>(src), rows, cols,
-                           i8_pitch(cols), static_cast<char *>(codes), scales);
+    auto go = [&](auto kernel, int64_t wgs, int threads) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(threads), 0, stream, static_cast<const char *>(src), rows, cols, i8_pitch(cols),
+                           static_cast<char *>(codes), scales);
+    };
+    // Many rows: a wave each, as long as it keeps them (2048 columns; 8192 x 8192 70 us like that, 41 with four waves to a row).  Few: as many lanes as there
+    // are chunks (24 x 8192 5.2 us with four waves to a row, 4.6 with 16).
+    if (rows >= 4 * compute_units() && cols <= 2048) go(&i8_quantize_kernel<1>, (rows + 3) / 4, 256);
+    else if (rows < compute_units() && cols > 2048) go(&i8_quantize_kernel<16>, rows, 1024);
+    else go(&i8_quantize_kernel<4>, rows, 256);
     return hipGetLastError();
 }
 
