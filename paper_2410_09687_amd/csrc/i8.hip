@@ -1,6 +1,7 @@
 // Matrix product in 8-bit integers: rows of x [T, d_in] and of the weight [d_out, d_in] have a scale each,
 //     s = max(amax / 127 in fp32, 2^-126),   code = x / s to the nearest, ties to even,   y = s_t s_o sum_c xq_c wq_c,
 // sums in int32, exact; one rounding to fp32, two for the scales.  A row with an infinity or a NaN has a scale of NaN and codes of 0.
+// (s rounded to fp32 belongs to the definition, so that codes are the same wherever they are made.)
 // This file: the quantiser, and the product of up to 128 tokens, bound by the weight's bytes.  Larger ones run on the
 // streams of tiles of mx.hip.
 #include <algorithm>
@@ -98,7 +99,8 @@ __global__ __launch_bounds__(WAVES == 16 ? 1024 : 256) void i8_quantize_kernel(c
         *reinterpret_cast<uint2 *>(out + c * 8) = c < n8 ? i8_codes(*reinterpret_cast<const uint4 *>(x + (int64_t)c * 16), s, inv) : make_uint2(0, 0);
 }
 
-// A workgroup quantises the tokens itself up to this many pieces of 512 columns.
+// A workgroup quantises the tokens itself up to this many pieces of 512 columns.  (2048 -> 2048, six tokens, 24 pieces: 5.9 us, 7.9 in a launch of its own;
+// 2048 -> 5632, eight tokens, 32 pieces: 10.3 and 8.6.)
 constexpr int FUSED_ITEMS = 24;
 int fused_items(int64_t T, int d_in) { return T > 16 ? FUSED_ITEMS + 1 : (int)T * ((i8_pitch(d_in) + 511) / 512); }
 
@@ -113,7 +115,11 @@ struct FewArgs {
 
 // 16 RT outputs a workgroup, all tokens; its KW waves take a range of the contraction's 128-byte blocks each and add their sums at the end.  A lane's
 // operands are 16 bytes of a row as they lie in memory (the order of the contraction is free).
-// FUSED: the workgroup quantises the tokens itself, into LDS, while its first weights are on their way.
+// FUSED: the workgroup quantises the tokens itself, into LDS, while its first weights are on their way: a launch less (one token 2048 -> 5632 10.7 us when
+// one wave did it, 5.6 with pieces dealt to sixteen).
+// One token 8192 -> 28672 45 us, 5.2 TB/s of weights; 24 tokens 48, 4.8 TB/s, where the tokens come out of L2 for every 64 outputs.  In turn instead of in
+// ranges the waves' blocks take 55 and 65 (of 32 outputs); 24 tokens and 16 / 32 / 64 outputs a workgroup 77 / 64 / 54, 64 tokens 134 / 97 / 73.  Past the
+// caches: 61 for the 24.
 template <int RT, int NT, int KW, bool FUSED>
 __global__ __launch_bounds__(64 * KW) void i8_few_kernel(FewArgs a)
 {
@@ -288,6 +294,9 @@ hipError_t launch_i8_few(const void *x, const void *xq, const float *xs, const v
 {
     const FewArgs a{static_cast<const char *>(x), static_cast<const char *>(xq), xs, static_cast<const char *>(Wq), ws, static_cast<char *>(y),
                     T, d_in, i8_pitch(d_in), d_out, y_f32};
+    // Outputs a workgroup and waves by the weight's rows: 64 or 32 outputs where that leaves a workgroup for every unit, as the tokens come from L2 once for
+    // each; else as many waves as hide the trips.  Us: 32 tokens 2048 -> 5632 with 16 / 32 outputs 10.9 / 9.1, 64 tokens 14.7 / 11.1, but 2048 -> 2048 7.9 /
+    // 9.0 and 9.6 / 11.0; one token 2048 -> 2048 with 8 / 16 waves 5.5 / 5.2, six 7.2 / 5.9.
     const int tiles = (d_out + 15) / 16, n_cus = compute_units();
     const bool wide = tiles >= 4 * n_cus, broad = tiles * 4 >= 5 * n_cus;
     if (i8_few_quantises(T, d_in)) return wide ? few<2, 1, 4, true>(a, stream) : tiles * 2 >= 3 * n_cus ? few<1, 1, 8, true>(a, stream) : few<1, 1, 16, true>(a, stream);

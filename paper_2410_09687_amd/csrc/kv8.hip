@@ -3,7 +3,9 @@
 // blocks that earlier ones have begun: E is then the larger one of the block's and what the new tokens ask for, and where
 // it grows, what the block holds is rounded again -- a shift of the exponent, exact but for values that become subnormal.
 //
-// So the block, not the token, is what a workgroup takes: it alone reads and writes its codes of one head's keys or values.
+// So the block, not the token, is what a workgroup takes: it alone reads and writes its codes of one head's keys or values.  Bound by memory: 65536 tokens of
+// eight heads of 128 95 us, 4.2 TB/s, and back 101, 4.1 TB/s (a copy of 1 GiB 5.0); 256 single tokens of four heads of 64 6.2 us, a chain of
+// four trips to memory.
 #include <type_traits>
 
 #include "gemm_core.h"
@@ -205,7 +207,7 @@ __global__ __launch_bounds__(NT) void kv8_append_kernel(KvPages p, const char *_
     }
 }
 
-// 64 tokens of the batch, one head's keys (blockIdx.x even) or values.
+// 64 tokens of the batch, one head's keys (blockIdx.x even) or values.  (Values a byte at a time, lanes as tokens: 219 us instead of 101 for 65536 tokens.)
 template <int D>
 __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__restrict__ k, char *__restrict__ v, int64_t T,
                                                          const int *__restrict__ slots, int *err_word)

@@ -283,7 +283,9 @@ __device__ __forceinline__ void i8_scale(f32x16_t (&acc)[FP][FQ], const Params &
 // are no scales, and every block takes the bf16 MFMAs); it is not instantiated:
 // measured against the eight-wave bf16 kernel on the 2048 -> 2048 prefill shape it
 // took 262 us against 252 us on the same device.
-// On integers the accumulators hold int32 sums through the base's blocks and become fp32 in front of the adapter's.
+// On integers the accumulators hold int32 sums through the base's blocks and become fp32 in front of the adapter's, five vector instructions a sum, one wave
+// on the SIMD, nothing to hide them: 16384 tokens 2048 -> 5632, rank 64, 223 us (FP8: 188), 8192 x 8192 x 8192 454, 2.4 PFLOP/s (FP8 408; the library's
+// integer product 481).
 template <int BASE, bool Y_F32>
 __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
 {

@@ -5,6 +5,7 @@
 // over D / 16 of them.  Statistics and rotation are fp32, the result is rounded once.  Angles are taken in turns, p f_i / 2 pi in 64 bits
 // of which the whole turns are dropped: fp32 angles of far positions are off by p 2^-24, here it is p 2^-53.
 // Sines and cosines are the same for all heads of a token: a wave computes each of them once and passes them on through LDS.
+// Bound by memory: 16384 tokens of 32 + 8 heads of 128 channels 68 us, 4.9 TB/s there and back (a copy of 1 GiB 5.0); one token 2.6 us.
 #include <algorithm>
 
 #include "gemm_core.h"
@@ -143,7 +144,7 @@ hipError_t launch(const RotateArgs &a, hipStream_t stream)
 {
     constexpr int HPW = 64 * 16 / D;
     const int groups = (a.n_heads + a.n_kv + HPW - 1) / HPW;
-    // A wave takes all heads of a token where there are tokens enough to fill the chip, else a group.
+    // A wave takes all heads of a token where there are tokens enough to fill the chip, else a group: its sines are then the group's own.
     const int parts = a.T * groups <= 16 * compute_units() ? groups : 1, per = (groups + parts - 1) / parts;
     const dim3 grid((unsigned)((a.T * parts + WAVES - 1) / WAVES));
     if (a.neighbours)
