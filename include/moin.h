@@ -694,7 +694,8 @@ int64_t moin_kv8_page_bytes(int32_t page_tokens, int32_t n_kv, int32_t head_dim)
 /* moin_kv8_append: as moin_kv_append; seq_offsets [S+1] and slots [T] are a plan's (moin_kv_plan_build): the tokens of
  * request s, from seq_offsets[s] on, follow one another in its pages.  A request whose first slot is -1 is skipped.  Offsets that run
  * backwards, a first slot that the cache does not have, a later block whose slots do not follow each other or whose page does not
- * exist raise the sticky data fault; such a request or block is left as it was.  No two requests may append to one block.
+ * exist raise the sticky data fault; such a request or block is left as it was (with offsets that run backwards blocks
+ * of others, too).  No two requests may append to one block.
  * moin_kv8_gather: as moin_kv_gather, any slots. */
 int moin_kv8_append(moin_ctx *ctx, const moin_kv_pages *pages, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
                     int64_t T, const int32_t *seq_offsets, int32_t S, const int32_t *slots, void *stream);

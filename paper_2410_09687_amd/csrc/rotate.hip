@@ -2,7 +2,7 @@
 //     x' = g x / sqrt(mean x^2 + eps)   over the channels of a token's head,
 //     (a, b) -> (a cos p f_i - b sin p f_i, b cos p f_i + a sin p f_i)   for pair i < R / 2 of its first R channels.
 // One pass: a lane holds 16 channels of a head, both halves of its pairs among them, so the rotation moves nothing between lanes and the norm is a sum
-// over D / 16 of them.  Statistics and rotation are fp32, the result is rounded once.  Angles are taken in turns, p f_i / 2 pi in 64 bits
+// over D / 16 of them.  Statistics and rotation are fp32 (64 bits where squares leave its range), the result is rounded once.  Angles are taken in turns, p f_i / 2 pi in 64 bits
 // of which the whole turns are dropped: fp32 angles of far positions are off by p 2^-24, here it is p 2^-53.
 // Sines and cosines are the same for all heads of a token: a wave computes each of them once and passes them on through LDS.
 // Bound by memory: 16384 tokens of 32 + 8 heads of 128 channels 68 us, 4.9 TB/s there and back (a copy of 1 GiB 5.0); one token 2.6 us.
@@ -94,7 +94,15 @@ __global__ __launch_bounds__(64 * WAVES) void qk_norm_rope_kernel(RotateArgs a, 
             for (int i = 0; i < 8; ++i) sum = fmaf(x0[i], x0[i], fmaf(x1[i], x1[i], sum));
 #pragma unroll
             for (int d = 1; d < LPH; d <<= 1) sum += __shfl_xor(sum, d);
-            const float r = rsqrtf(sum * (1.f / D) + a.eps);
+            float r = rsqrtf(sum * (1.f / D) + a.eps);
+            if (__ballot(!(sum < 1e36f) || (sum < 1e-30f && a.eps < 1e-25f))) {   // squares that fp32 does not hold
+                double wide = 0.0;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) wide = fma((double)x0[i], (double)x0[i], fma((double)x1[i], (double)x1[i], wide));
+#pragma unroll
+                for (int d = 1; d < LPH; d <<= 1) wide += __shfl_xor(wide, d);
+                r = (float)(1.0 / sqrt(wide * (1.0 / D) + (double)a.eps));
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 x0[i] *= r;

@@ -99,6 +99,15 @@ def test_far_and_negative_positions():
     check(qkv, pos, gains, 4, 2, moin.rope_frequencies(128, 1e6), neighbours=True)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("size,eps", [(1e30, 1e-6), (2e38, 1e-6), (1e-18, 1e-30), (1e-25, 1e-38), (1e19, 1.0)])
+def test_magnitudes_whose_squares_fp32_does_not_hold(size, eps, dtype):
+    qkv, pos, gains = inputs(11, 9, 6, 2, 64)
+    x = (qkv.float() / qkv.float().abs().amax() * size)
+    x[0] = qkv[0]
+    check(x.to(dtype), pos, gains, 6, 2, moin.rope_frequencies(64), eps=eps)
+
+
 def test_position_zero_passes_everything():
     qkv, pos, gains = inputs(6, 5, 4, 2, 64)
     pos.zero_()
