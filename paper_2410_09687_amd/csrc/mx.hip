@@ -169,6 +169,7 @@ struct Tile {
     int kb0;                   // first contraction block (plain mode: the part's; else 0)
     int64_t y_off;             // byte offset of the output plane (plain mode)
     int valid;
+    int odd;                   // of the workgroup's tiles: which of the two scale areas is its own (integers)
 };
 
 // E: the tile's edge; a plan tile is TILE_M / E of them along the tokens (the last may be empty: q_rows <= 0).
@@ -179,6 +180,7 @@ __device__ __forceinline__ Tile load_tile(const Params &p, int id, int n_work)
     constexpr int SUB = TILE_M / E;
     Tile t;
     t.valid = id < n_work;
+    t.odd = 0;
     const int cid = t.valid ? id : 0;
     const int64_t ldq = (int64_t)p.d_in * EB, ldu = (int64_t)p.r * 2;
     if (p.plain) {
@@ -233,20 +235,19 @@ __device__ __forceinline__ f32x16_t i8_products(const Frag &a, const Frag &b, f3
     v = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_shufflevector(a, a, 4, 5, 6, 7), __builtin_shufflevector(b, b, 4, 5, 6, 7), v, 0, 0, 0);
     return __builtin_bit_cast(f32x16_t, v);
 }
-// The base product's sums to fp32 with their scales, in front of the adapter's blocks or the epilogue; the wave's outputs begin at n, its tokens at t.
+// The base product's sums to fp32 with their scales, in front of the adapter's blocks or the epilogue; out, tok: scales in LDS, of the wave's outputs
+// and tokens.
 template <bool AGPR, int FP, int FQ>
-__device__ __forceinline__ void i8_scale(f32x16_t (&acc)[FP][FQ], const Params &p, int n, int t, int lane)
+__device__ __forceinline__ void i8_scale(f32x16_t (&acc)[FP][FQ], const char *out, const char *tok, int lane)
 {
-    const float *ws = reinterpret_cast<const float *>(p.Ws), *xs = reinterpret_cast<const float *>(p.xs);
     float st[FQ];
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) st[j] = xs[min((int64_t)t + j * 32 + (lane & 31), p.T - 1)];
+    for (int j = 0; j < FQ; ++j) st[j] = *reinterpret_cast<const float *>(tok + (j * 32 + (lane & 31)) * 4);
 #pragma unroll
     for (int i = 0; i < FP; ++i) {
         f32x4_t so[4];
 #pragma unroll
-        for (int g = 0; g < 4; ++g)   // (d_out is a multiple of 8: four outputs are all there or none is)
-            so[g] = *reinterpret_cast<const f32x4_t *>(ws + min(n + i * 32 + 8 * g + 4 * (lane >> 5), p.d_out - 4));
+        for (int g = 0; g < 4; ++g) so[g] = *reinterpret_cast<const f32x4_t *>(out + (i * 32 + 8 * g + 4 * (lane >> 5)) * 4);
 #pragma unroll
         for (int j = 0; j < FQ; ++j) {
 #pragma unroll
@@ -323,6 +324,7 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
     struct Fetch {
         const char *pp, *pq, *ps, *qs;
         uint32_t ld, p_last, q_last;
+        int odd;
     };
     auto fetch_of = [&](const Tile &t, int b) __attribute__((always_inline)) {
         Fetch f;
@@ -343,6 +345,11 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
             f.ps = p.Ws + ((int64_t)(t.kb0 + sb) * p.d_out + t.n0) * 4;
             f.qs = p.xs + ((int64_t)(t.kb0 + sb) * p.T + t.row0) * 4;
         }
+        if constexpr (I8) {   // (the tile's, with every block again: no branch here either)
+            f.ps = p.Ws + (int64_t)t.n0 * 4;
+            f.qs = p.xs + (int64_t)t.row0 * 4;
+            f.odd = t.odd;
+        }
         return f;
     };
     auto issue_one = [&](const Fetch &f, int st, int n) __attribute__((always_inline)) {
@@ -354,8 +361,8 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
             const uint32_t off = __umul24(row, f.ld) + ((j & 1) ? c16b : c16a);
             __builtin_amdgcn_global_load_lds(MOIN_GPTR((q ? f.pq : f.pp) + off),
                                              MOIN_LPTR(stage + (q ? OP_BYTES : 0) + (wave * LOADS + j) * 1024), 16, 0, 0);
-        } else if constexpr (MX) {
-            char *sc_ = smem + SMEM_STAGES + st * SC_BYTES;
+        } else if constexpr (MX || I8) {
+            char *sc_ = smem + SMEM_STAGES + (I8 ? f.odd : st) * SC_BYTES;
             const bool q = n == 2 * LOADS + 1;
             const uint32_t row = min((uint32_t)(wave * 64) + (uint32_t)lane, q ? f.q_last : f.p_last);
             __builtin_amdgcn_global_load_lds(MOIN_GPTR((q ? f.qs : f.ps) + row * 4u),
@@ -365,7 +372,7 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
     auto issue = [&](const Tile &t, int b, int st) __attribute__((always_inline)) {
         const Fetch f = fetch_of(t, b);
 #pragma unroll
-        for (int n = 0; n < 2 * LOADS + (MX ? 2 : 0); ++n) issue_one(f, st, n);
+        for (int n = 0; n < 2 * LOADS + (MX || I8 ? 2 : 0); ++n) issue_one(f, st, n);
     };
 
     // fragment addresses: byte (16 h) ^ (16 f) of the lane's row in the first patch of
@@ -439,6 +446,7 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
     Tile cur = load_tile<BASE>(p, id, band_end);
     id += nslot;
     Tile nxt = load_tile<BASE>(p, id, band_end);
+    nxt.odd = 1;
 
     // fetch cursor: tile and block index of the next block to request
     Tile pft = cur;
@@ -494,7 +502,7 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
         if (n < FP + FQ) read_frag_n(smem + ((s + 1) & 1) * STAGE_BYTES, 0, n);
         else if constexpr (MX) read_scale_n(smem + SMEM_STAGES + ((s + 1) & 1) * SC_BYTES, n - (FP + FQ));
         issue_one(fsecond, s & 1, n);
-        if constexpr (MX) {
+        if constexpr (MX || I8) {
             if (n == 3) issue_one(fsecond, s & 1, 2 * LOADS);
             if (n == 7) issue_one(fsecond, s & 1, 2 * LOADS + 1);
         }
@@ -522,7 +530,7 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
     // prologue of the stream: two blocks in flight, the first one landed
     issue(cur, 0, 0);
     issue(cur, 1, 1);   // every tile has at least two blocks
-    wait_vm_then_barrier<2 * LOADS + (MX ? 2 : 0)>();
+    wait_vm_then_barrier<2 * LOADS + (MX || I8 ? 2 : 0)>();
 
     int s = 0;
     for (;;) {
@@ -542,7 +550,8 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
         if constexpr (I8) {
             int lane_s = lane;
             asm volatile("; lane id, rematerialised\n\ts_nop 15\n\ts_nop 15" : "+v"(lane_s) : : "memory");
-            i8_scale<true, FP, FQ>(acc, p, cur.n0 + wp * (FP * 32), cur.row0 + wq * (FQ * 32), lane_s);
+            const char *area = smem + SMEM_STAGES + cur.odd * SC_BYTES;
+            i8_scale<true, FP, FQ>(acc, area + wp * (FP * 32) * 4, area + (BT + wq * (FQ * 32)) * 4, lane_s);
             asm volatile("s_nop 15" ::: "memory");   // the assembly's writes before the adapter's MFMAs read them
         }
         for (; b < total; ++b, ++s) body(s, std::false_type{}, std::false_type{});
@@ -561,6 +570,7 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
         cur = nxt;
         id += nslot;
         nxt = load_tile<BASE>(p, id, band_end);
+        nxt.odd = cur.odd ^ 1;
     }
     // the last blocks' repeated requests must have landed before the LDS is released
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -641,9 +651,18 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
         const int jb = b - nb;
         const bool hi = jb < nkb1;
         const int kb = base ? b : (hi ? jb : jb - nkb1);
-        f.pq = (base ? q0 : (hi ? uh : ul)) + kb * ROWB;
-        f.pp = (base ? p0 : be) + kb * ROWB;
-        f.ps = MX ? sc0 + (base ? b : 0) * sc_pitch : nullptr;   // (an adapter block repeats the first one's: no branch)
+        if constexpr (MX) {
+            f.pq = (base ? q0 : (hi ? uh : ul)) + kb * ROWB;
+            f.pp = (base ? p0 : be) + kb * ROWB;
+            f.ps = sc0 + (base ? b : 0) * sc_pitch;   // (an adapter block repeats the first one's: no branch)
+        } else {
+            // (values to choose from: their addresses would be chosen, and the operands read from scratch memory, a wait for every request in flight)
+            const char *x = q0, *xh = uh, *xl = ul, *w = p0, *wb = be;
+            asm("" : "+s"(x), "+s"(xh), "+s"(xl), "+s"(w), "+s"(wb));
+            f.pq = (base ? x : (hi ? xh : xl)) + kb * ROWB;
+            f.pp = (base ? w : wb) + kb * ROWB;
+            f.ps = nullptr;
+        }
         f.ld = base ? ldq : ldu;
         return f;
     };
@@ -753,6 +772,9 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
         if constexpr (MX) regroup();
     };
 
+    if constexpr (!MX) {   // the tile's scales, once
+        __builtin_amdgcn_global_load_lds(MOIN_GPTR((sq ? xs + (int64_t)row0 * 4 : Ws + (int64_t)n0 * 4) + srow), MOIN_LPTR(smem + 2 * OP_BYTES + wave * 256), 4, 0, 0);
+    }
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
         const Fetch f = fetch_of(min(s, total - 1));
@@ -769,7 +791,7 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
     }
     int b = 0;
     for (; b < nb; ++b) body(b, std::true_type{});
-    if constexpr (!MX) mxs::i8_scale<false, FP, FQ>(acc, p, n0 + wp * (FP * 32), row0 + wq * (FQ * 32), lane);
+    if constexpr (!MX) mxs::i8_scale<false, FP, FQ>(acc, smem + 2 * OP_BYTES + wp * (FP * 32) * 4, smem + 2 * OP_BYTES + (BT + wq * (FQ * 32)) * 4, lane);
     for (; b < total; ++b) body(b, std::false_type{});
     // the stages become the waves' scratch: no request (waited for in the last blocks) and no stale read is under way
     asm volatile("s_nop 15\n\ts_nop 15\n\ts_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
