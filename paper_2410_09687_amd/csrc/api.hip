@@ -713,6 +713,47 @@ int linear_mx_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, 
     return MOIN_OK;
 }
 
+// Product in 8-bit integers without adapters: the tokens' codes into the workspace, few tokens straight from the weight, else tiles -- where these do not
+// fill the chip in parts of the contraction, whose int32 sums a third launch adds, exactly.
+int i8_plain(moin_ctx *ctx, const void *x, int64_t T, const void *Wq, const float *ws, int32_t d_in, int32_t d_out, void *y, int y_f32,
+             hipStream_t stream)
+{
+    const int pitch = i8_pitch(d_in);
+    const bool few = i8_few_pays(T, d_in, d_out);
+    MxLinearArgs m{};
+    m.plain_splits = 1;
+    m.plain_kb_per_split = pitch / 128;
+    if (!few) mx_plain_shape(T, pitch, d_out, &m.plain_splits, &m.plain_kb_per_split);
+    const bool parts = m.plain_splits > 1;
+    const size_t xq_bytes = align_up((size_t)T * (size_t)pitch, 256), xs_bytes = align_up((size_t)T * 4, 256), row = (size_t)d_out * 4;
+    const int rc = ensure_ws(ctx, xq_bytes + xs_bytes + (parts ? (size_t)m.plain_splits * (size_t)T * row : 0), stream, false,
+                             xq_bytes + xs_bytes + (size_t)i8_parts_rows(T, d_in, d_out) * row);
+    if (rc != MOIN_OK) return rc;
+    char *xq = static_cast<char *>(ctx->ws), *sums = xq + xq_bytes + xs_bytes;
+    float *xs = reinterpret_cast<float *>(xq + xq_bytes);
+    if (!(few && i8_few_quantises(T, d_in)) &&
+        timed(ctx, MOIN_K_MX_QUANT, stream, [&] { return launch_i8_quantize(x, T, d_in, xq, xs, stream); }) != hipSuccess)
+        return MOIN_EHIP;
+    if (timed(ctx, MOIN_K_I8_LINEAR, stream, [&] {
+            if (few) return launch_i8_few(x, xq, xs, Wq, ws, (int)T, d_in, d_out, y, y_f32, stream);
+            m.lin.y = parts ? sums : y;
+            m.lin.y_f32 = parts || y_f32;
+            m.lin.d_in = d_in;
+            m.lin.d_out = d_out;
+            m.xq = xq;
+            m.xs = xs;
+            m.Wq = Wq;
+            m.Ws = ws;
+            m.raw = parts;
+            PlanView pv{};
+            pv.T = T;
+            const hipError_t e = launch_linear_i8_stream(pv, m, compute_units(), stream);
+            return e != hipSuccess || !parts ? e : launch_i8_join(sums, m.plain_splits, xs, ws, T, d_out, y, y_f32, stream);
+        }) != hipSuccess)
+        return MOIN_EHIP;
+    return MOIN_OK;
+}
+
 // Base in 8-bit integers: the tokens' codes into the workspace, then as on the MXFP8 base.
 int linear_i8_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, const void *Wq, const float *ws, const void *A_stack,
                            const void *B_stack, int32_t d_in, int32_t d_out, int32_t r, float scale, void *y, moin_dtype y_dt,
@@ -720,12 +761,12 @@ int linear_i8_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, 
 {
     const PlanView &pv = plan->pv;
     if (capturing(stream)) plan->pinned = 1;
-    const bool adapters = pv.E > 0 && r > 0;
+    if (pv.E == 0 || r == 0) return i8_plain(ctx, x, pv.T, Wq, ws, d_in, d_out, y, y_dt == MOIN_F32, stream);
     MxLinearArgs m;
     LinearArgs &a = m.lin;
     a.x = x; a.W = nullptr; a.A_stack = A_stack; a.B_stack = B_stack;
     a.y = y; a.y_f32 = (y_dt == MOIN_F32);
-    a.d_in = d_in; a.d_out = d_out; a.r = adapters ? r : 0; a.scale = scale; a.act = ctx->act;
+    a.d_in = d_in; a.d_out = d_out; a.r = r; a.scale = scale; a.act = ctx->act;
     a.u_hi = a.u_lo = nullptr;
     a.ldu = a.r;                          // (a multiple of 64 here)
     m.Wq = Wq;
@@ -735,21 +776,18 @@ int linear_i8_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, 
     const int pitch = i8_pitch(d_in);
     const size_t u_bytes = align_up((size_t)pv.T * (size_t)a.r * 2, 256), xq_bytes = align_up((size_t)pv.T * (size_t)pitch, 256),
                  xs_bytes = align_up((size_t)pv.T * 4, 256);
-    const bool gathered = gathered_pays_mx(pv, d_in, d_out, a.r), decode = gathered && a.r > 0;
-    // (with adapters the tiles' sums may be cut into parts, which the expand adds.  Us, few tokens / tiles: 64 tokens 2048 -> 2048 22 / 25, 128 5632 -> 2048
-    // 48 / 40, 4096 -> 4096 42 / 38)
-    const bool few = gathered && (decode ? pv.T <= 64 : i8_few_pays(pv.T, d_out)), quantised = !(few && i8_few_quantises(pv.T, d_in));
+    const bool decode = gathered_pays_mx(pv, d_in, d_out, a.r);
+    // (the tiles' sums may be cut into parts, which the expand adds anyway, so that few tokens end earlier than without adapters.  Us, few / tiles: 128 tokens
+    // 2048 -> 256 24 / 21, 2048 -> 2048 24.2 / 22.5, 1024 -> 4096 21 / 25; 80 2048 -> 2048 22.1 / 21.7)
+    const bool few = decode && pv.T <= 64 && i8_few_pays(pv.T, d_in, d_out), quantised = !(few && i8_few_quantises(pv.T, d_in));
     size_t yb_bytes = 0;
     if (decode) {
         if (few) m.plain_splits = 1;
         else mx_plain_shape(pv.T, pitch, d_out, &m.plain_splits, &m.plain_kb_per_split);
         yb_bytes = align_up((size_t)m.plain_splits * (size_t)pv.T * (size_t)d_out * 4, 256);
-    } else if (gathered) {
-        m.plain_splits = 1;            // no adapters anywhere: the plain product writes y itself
-        m.plain_kb_per_split = pitch / 128;
     }
     const size_t head_bytes = 2 * u_bytes + xq_bytes + xs_bytes;
-    const size_t yb_most = pv.decode && a.r > 0 ? align_up((size_t)mx_plain_rows(pv.T, pitch, d_out) * (size_t)d_out * 4, 256) : 0;
+    const size_t yb_most = pv.decode ? align_up((size_t)mx_plain_rows(pv.T, pitch, d_out) * (size_t)d_out * 4, 256) : 0;
     const int rc = ensure_ws(ctx, head_bytes + yb_bytes, stream, false, head_bytes + yb_most);
     if (rc != MOIN_OK) return rc;
     char *w = static_cast<char *>(ctx->ws);
@@ -779,7 +817,7 @@ int linear_i8_planned_impl(moin_ctx *ctx, const moin_plan *plan, const void *x, 
         if (timed(ctx, MOIN_K_DECODE_EXPAND, stream, [&] { return launch_decode_expand(pv, d, stream); }) != hipSuccess) return MOIN_EHIP;
         return MOIN_OK;
     }
-    if (a.r > 0 && timed(ctx, MOIN_K_SHRINK, stream, [&] { return launch_prefill_shrink(pv, a, stream); }) != hipSuccess) return MOIN_EHIP;
+    if (timed(ctx, MOIN_K_SHRINK, stream, [&] { return launch_prefill_shrink(pv, a, stream); }) != hipSuccess) return MOIN_EHIP;
     if (timed(ctx, MOIN_K_I8_LINEAR, stream, [&] { return base(y, y_dt == MOIN_F32); }) != hipSuccess) return MOIN_EHIP;
     return MOIN_OK;
 }
@@ -2062,35 +2100,7 @@ int moin_i8_linear(moin_ctx *ctx, const void *x, int64_t T, const void *Wq, cons
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return MOIN_EHIP;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int pitch = i8_pitch(d_in);
-    const size_t xq_bytes = align_up((size_t)T * (size_t)pitch, 256);
-    const int rc = ensure_ws(ctx, xq_bytes + align_up((size_t)T * 4, 256), st);
-    if (rc != MOIN_OK) return rc;
-    char *xq = static_cast<char *>(ctx->ws);
-    float *xs = reinterpret_cast<float *>(xq + xq_bytes);
-    const bool few = i8_few_pays(T, d_out);
-    if (!(few && i8_few_quantises(T, d_in)) &&
-        timed(ctx, MOIN_K_MX_QUANT, st, [&] { return launch_i8_quantize(x, T, d_in, xq, xs, st); }) != hipSuccess)
-        return MOIN_EHIP;
-    return timed(ctx, MOIN_K_I8_LINEAR, st, [&] {
-               if (few) return launch_i8_few(x, xq, xs, Wq, ws, (int)T, d_in, d_out, y, y_dt == MOIN_F32, st);
-               MxLinearArgs m{};
-               m.lin.y = y;
-               m.lin.y_f32 = y_dt == MOIN_F32;
-               m.lin.d_in = d_in;
-               m.lin.d_out = d_out;
-               m.xq = xq;
-               m.xs = xs;
-               m.Wq = Wq;
-               m.Ws = ws;
-               m.plain_splits = 1;
-               m.plain_kb_per_split = pitch / 128;
-               PlanView pv{};
-               pv.T = T;
-               return launch_linear_i8_stream(pv, m, compute_units(), st);
-           }) == hipSuccess
-               ? MOIN_OK
-               : MOIN_EHIP;
+    return i8_plain(ctx, x, T, Wq, ws, d_in, d_out, y, y_dt == MOIN_F32, st);
 }
 
 int moin_lora_linear_i8_planned(moin_ctx *ctx, const moin_plan *plan, const void *x, const void *Wq, const float *ws, const void *A_stack,

@@ -252,6 +252,24 @@ __global__ __launch_bounds__(64 * KW) void i8_few_kernel(FewArgs a)
     }
 }
 
+// A thread takes four outputs of a token.
+__global__ __launch_bounds__(256) void i8_join_kernel(const i32x4_t *__restrict__ parts, int n, const float *__restrict__ xs, const float *__restrict__ ws,
+                                                      int64_t quads, int per_row, char *__restrict__ y, int y_f32)
+{
+    const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (q >= quads) return;
+    i32x4_t v = parts[q];
+    for (int u = 1; u < n; ++u) v += parts[u * quads + q];
+    const int64_t t = q / per_row;
+    const float st = xs[t];
+    const f32x4_t so = reinterpret_cast<const f32x4_t *>(ws)[q - t * per_row];
+    float r[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = (float)v[e] * (st * so[e]);
+    if (y_f32) *reinterpret_cast<float4 *>(y + q * 16) = make_float4(r[0], r[1], r[2], r[3]);
+    else *reinterpret_cast<uint2 *>(y + q * 8) = make_uint2(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]));
+}
+
 constexpr int few_lds(int RT, int NT, int KW) { return 16 * NT * 4 + KW * RT * NT * 1024; }   // scales, the waves' sums
 template <int RT, int NT, int KW, bool FUSED>
 hipError_t few(const FewArgs &a, hipStream_t stream)
@@ -278,13 +296,15 @@ hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *cod
     return hipGetLastError();
 }
 
-// Up to 128 tokens; 64 where the weight has rows enough for the tiles of 128 x 128 to fill the chip; more in groups of 128 as long as each workgroup
-// has a compute unit of its own.  Us with and without (few, tiles): 128 tokens 2048 -> 256 13 / 20, 2048 -> 5632 16 / 20, 5632 -> 2048 29 / 42, 8192 -> 8192
-// 45 / 77, but 8192 -> 28672 103 / 88; 256 tokens 2048 -> 2048 14 / 20, 5632 -> 2048 29 / 42; 1000 2048 -> 256 15 / 21.
-bool i8_few_pays(int64_t T, int d_out)
+// Each group of 128 tokens reads the weight for itself, a workgroup all of its tokens' codes: what a token costs grows with d_in, what the tiles of
+// 128 x 128 cost does so over the parts of their contraction.  Us, few / tiles: 64 tokens 2048 -> 2048 9.8 / 12.7, 4096 -> 4096 14.5 / 15.9, 8192 -> 8192 28 / 25;
+// 128 2048 -> 5632 15.8 / 17.6, 2048 -> 256 13.6 / 12.2, 5632 -> 2048 28 / 17; 24 131072 -> 64 166 / 168.  More than one group only while each workgroup has
+// a compute unit of its own: 1000 tokens 1024 -> 256 11.4 / 13.7, 256 2048 -> 2048 14.2 / 16.2, but 1000 1024 -> 2048 27 / 22.
+bool i8_few_pays(int64_t T, int d_in, int d_out)
 {
-    const int64_t tiles = (d_out + 15) / 16, n_cus = compute_units();
-    return T <= 64 || (T <= 128 && tiles < 4 * n_cus) || (T + 127) / 128 * tiles <= n_cus;
+    const int64_t tiles = (d_out + 15) / 16;
+    if (T <= 24) return true;
+    return std::min<int64_t>(T, 128) * d_in <= 1 << 18 && (T <= 128 || (T + 127) / 128 * tiles <= compute_units());
 }
 
 bool i8_few_quantises(int64_t T, int d_in) { return fused_items(T, d_in) <= FUSED_ITEMS; }
@@ -304,6 +324,14 @@ hipError_t launch_i8_few(const void *x, const void *xq, const float *xs, const v
     if (T <= 32) return wide ? few<4, 2, 4, false>(a, stream) : broad ? few<2, 2, 4, false>(a, stream) : few<1, 2, 8, false>(a, stream);
     if (T <= 64) return wide ? few<4, 4, 4, false>(a, stream) : broad ? few<2, 4, 8, false>(a, stream) : few<1, 4, 8, false>(a, stream);
     return wide ? few<4, 8, 4, false>(a, stream) : broad ? few<2, 8, 4, false>(a, stream) : few<1, 8, 8, false>(a, stream);
+}
+
+hipError_t launch_i8_join(const void *parts, int n, const float *xs, const float *ws, int64_t T, int d_out, void *y, int y_f32, hipStream_t stream)
+{
+    const int64_t quads = T * (d_out / 4);
+    hipLaunchKernelGGL(i8_join_kernel, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream, static_cast<const i32x4_t *>(parts), n, xs, ws, quads,
+                       d_out / 4, static_cast<char *>(y), y_f32);
+    return hipGetLastError();
 }
 
 hipError_t prepare_i8_kernels()

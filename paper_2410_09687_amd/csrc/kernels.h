@@ -260,6 +260,7 @@ struct MxLinearArgs {
     // contraction range in this many parts (mx_plain_shape), part s written to
     // lin.y + s * T * d_out elements
     int plain_splits, plain_kb_per_split;
+    int raw = 0;           // integers: the parts are int32 sums without their scales
 };
 void mx_plain_shape(int64_t T, int d_in, int d_out, int *k_splits, int *kb_per_split);
 int64_t mx_plain_rows(int64_t T, int d_in, int d_out);   // as decode_base_rows
@@ -276,11 +277,14 @@ constexpr int i8_pitch(int cols) { return cols <= 256 ? 256 : (cols + 127) / 128
 constexpr int I8_MAX_COLS = 131072;   // sums of as many products of 127 x 127 fit 31 bits
 hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *codes, float *scales, hipStream_t stream);
 // y [T, d_out] of few tokens (where i8_few_pays), whose codes and scales are given -- or, where launch_i8_few_quantises, x itself.
-bool i8_few_pays(int64_t T, int d_out);
+bool i8_few_pays(int64_t T, int d_in, int d_out);
 bool i8_few_quantises(int64_t T, int d_in);
 hipError_t launch_i8_few(const void *x, const void *xq, const float *xs, const void *Wq, const float *ws, int T, int d_in, int d_out, void *y,
                          int y_f32, hipStream_t stream);
 hipError_t launch_linear_i8_stream(const PlanView &pv, const MxLinearArgs &a, int n_cus, hipStream_t stream);   // (xs, Ws: fp32)
+// y [T, d_out] from n parts' int32 sums, one after the other.
+hipError_t launch_i8_join(const void *parts, int n, const float *xs, const float *ws, int64_t T, int d_out, void *y, int y_f32, hipStream_t stream);
+int64_t i8_parts_rows(int64_t T, int d_in, int d_out);   // the most rows of parts (n T, n > 1) that a product of up to T tokens takes
 
 // Norms and rotation of queries and keys (rotate.hip); strides in elements between the rows of tokens.
 struct RotateArgs {

@@ -155,6 +155,7 @@ struct Params {
     // kb_per_split blocks (more than one on 128 x 128 tiles only), part s written to
     // y + s * plane_bytes
     int plain, tiles_m, k_splits, kb_per_split;
+    int raw;                   // integers, plain: the parts' int32 sums as they are
     int64_t plane_bytes;
 };
 
@@ -285,7 +286,7 @@ __device__ __forceinline__ void i8_scale(f32x16_t (&acc)[FP][FQ], const char *ou
 // measured against the eight-wave bf16 kernel on the 2048 -> 2048 prefill shape it
 // took 262 us against 252 us on the same device.
 // On integers the accumulators hold int32 sums through the base's blocks and become fp32 in front of the adapter's, five vector instructions a sum, one wave
-// on the SIMD, nothing to hide them: 16384 tokens 2048 -> 5632, rank 64, 223 us (FP8: 188), 8192 x 8192 x 8192 454, 2.4 PFLOP/s (FP8 408; the library's
+// on the SIMD, nothing to hide them: 16384 tokens 2048 -> 5632, rank 64, 215 us (FP8: 188), 8192 x 8192 x 8192 443, 2.5 PFLOP/s (FP8 408; the library's
 // integer product 481).
 template <int BASE, bool Y_F32>
 __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
@@ -791,7 +792,7 @@ __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p
     }
     int b = 0;
     for (; b < nb; ++b) body(b, std::true_type{});
-    if constexpr (!MX) mxs::i8_scale<false, FP, FQ>(acc, smem + 2 * OP_BYTES + wp * (FP * 32) * 4, smem + 2 * OP_BYTES + (BT + wq * (FQ * 32)) * 4, lane);
+    if (!MX && !p.raw) mxs::i8_scale<false, FP, FQ>(acc, smem + 2 * OP_BYTES + wp * (FP * 32) * 4, smem + 2 * OP_BYTES + (BT + wq * (FQ * 32)) * 4, lane);
     for (; b < total; ++b) body(b, std::false_type{});
     // the stages become the waves' scratch: no request (waited for in the last blocks) and no stale read is under way
     asm volatile("s_nop 15\n\ts_nop 15\n\ts_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -864,6 +865,20 @@ int64_t mx_plain_rows(int64_t T, int d_in, int d_out)
     return most;
 }
 
+int64_t i8_parts_rows(int64_t T, int d_in, int d_out)
+{
+    const int64_t cols = (d_out + mxm::BT - 1) / mxm::BT;
+    int64_t most = 0;
+    for (int want = 2; want <= 4; ++want) {   // (as mx_plain_rows)
+        const int64_t t = std::min<int64_t>(T, compute_units() / want / cols * mxm::BT);
+        if (t <= 0) continue;
+        int parts = 0, per = 0;
+        mx_plain_shape(t, i8_pitch(d_in), d_out, &parts, &per);
+        if (parts > 1) most = std::max(most, t * parts);
+    }
+    return most;
+}
+
 template <int BASE>
 static hipError_t launch_stream(const PlanView &pv, const MxLinearArgs &a, int n_cus, hipStream_t stream_)
 {
@@ -881,6 +896,7 @@ static hipError_t launch_stream(const PlanView &pv, const MxLinearArgs &a, int n
     p.n_tiles_n = (a.lin.d_out + mxs::BT - 1) / mxs::BT;
     p.y_f32 = a.lin.y_f32;
     p.plain = a.plain_splits > 0;
+    p.raw = a.raw;
     p.tiles_m = (int)((pv.T + mxs::BT - 1) / mxs::BT);
     p.k_splits = a.plain_splits > 0 ? a.plain_splits : 1;
     p.kb_per_split = a.plain_kb_per_split;

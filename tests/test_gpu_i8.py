@@ -106,6 +106,38 @@ def test_rows_and_channels_with_nans_stay_alone():
         assert torch.equal(torch.isnan(y), nan)
 
 
+@pytest.mark.parametrize("T,d_in,d_out", [(25, 16384, 40), (100, 4096, 72), (128, 5632, 264), (129, 2120, 2056)])
+def test_tiles_over_parts_of_the_contraction(T, d_in, d_out):
+    """Few tiles: each in parts, whose sums are added; eager and captured, without and with the plan of no adapters, and beside NaNs."""
+    own = moin.Context(0)
+    try:
+        p = Product(T, T, d_in, d_out)
+        for y in (BF16, F32):
+            p.check(moin.moin_i8_linear(own, p.x, p.w8, y_dtype=y))
+        plan = moin.Plan(own).build(torch.tensor([0, T], dtype=I32, device="cuda"), torch.zeros(1, dtype=I32, device="cuda"), T, 3)
+        want, y = moin.moin_i8_linear(own, p.x, p.w8), torch.empty((T, d_out), dtype=BF16, device="cuda")
+        assert torch.equal(moin.moin_lora_linear_i8_planned(own, plan, p.x, p.w8, None, None, 1.0), want)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            moin.moin_i8_linear(own, p.x, p.w8, out=y)
+        other = p.x.flip(0).contiguous()
+        for _ in range(3):
+            y.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(y, want)
+            assert torch.equal(moin.moin_i8_linear(own, other, p.w8), want.flip(0))
+        del graph
+        plan.close()
+        p.x[3, 5] = float("nan")
+        got = moin.moin_i8_linear(own, p.x, p.w8)
+        assert torch.isnan(got[3]).all() and torch.equal(got[4:], want[4:]) and torch.equal(got[:3], want[:3])
+    finally:
+        torch.cuda.synchronize()
+        own.close()
+
+
 def adapters(p, off, ids, A, B, scale, act=None):
     """Result and bound.  u is carried as two bf16 (2^-16 of it), its sum of d_in products and that of r terms beside the base are fp32."""
     x, base = f64(p.x), p.base()
