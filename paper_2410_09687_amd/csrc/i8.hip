@@ -284,6 +284,14 @@ hipError_t few(const FewArgs &a, hipStream_t stream)
 hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *codes, float *scales, hipStream_t stream)
 {
     if (rows <= 0) return hipSuccess;
+    constexpr int64_t AT_ONCE = 1 << 23;   // rows of a launch, whose threads number less than 2^32
+    for (; rows > AT_ONCE; rows -= AT_ONCE) {
+        const hipError_t e = launch_i8_quantize(src, AT_ONCE, cols, codes, scales, stream);
+        if (e != hipSuccess) return e;
+        src = static_cast<const char *>(src) + AT_ONCE * cols * 2;
+        codes = static_cast<char *>(codes) + AT_ONCE * i8_pitch(cols);
+        scales += AT_ONCE;
+    }
     auto go = [&](auto kernel, int64_t wgs, int threads) {
         hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(threads), 0, stream, static_cast<const char *>(src), rows, cols, i8_pitch(cols),
                            static_cast<char *>(codes), scales);

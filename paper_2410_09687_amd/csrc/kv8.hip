@@ -6,6 +6,7 @@
 // So the block, not the token, is what a workgroup takes: it alone reads and writes its codes of one head's keys or values.  Bound by memory: 65536 tokens of
 // eight heads of 128 95 us, 4.2 TB/s, and back 101, 4.1 TB/s (a copy of 1 GiB 5.0); 256 single tokens of four heads of 64 6.2 us, a chain of
 // four trips to memory.
+#include <algorithm>
 #include <type_traits>
 
 #include "gemm_core.h"
@@ -78,17 +79,18 @@ __device__ __forceinline__ int request_at(const int *seq_offsets, int S, int id)
     return lo;
 }
 
-// NT threads take a block's keys (blockIdx.x even) or values of one head.  Registers hold the new tokens between the search for their largest magnitude and
+// NT threads take a block's keys (of an even place) or values of one head.  Registers hold the new tokens between the search for their largest magnitude and
 // the conversion.
 template <int D, int NT>
-__global__ __launch_bounds__(NT) void kv8_append_kernel(KvPages p, const char *__restrict__ k, const char *__restrict__ v, int64_t k_stride,
+__global__ __launch_bounds__(NT) void kv8_append_kernel(unsigned place0, KvPages p, const char *__restrict__ k, const char *__restrict__ v, int64_t k_stride,
                                                         int64_t v_stride, int T, const int *__restrict__ seq_offsets, int S,
                                                         const int *__restrict__ slots, int *err_word)
 {
     __shared__ uint32_t lds_amax[NT / 64];
     const int tid = threadIdx.x, lane = tid & 63;
-    const bool is_v = blockIdx.x & 1;
-    const int h = (int)((blockIdx.x >> 1) % (unsigned)p.n_kv), id = (int)((blockIdx.x >> 1) / (unsigned)p.n_kv);
+    const unsigned place = place0 + blockIdx.x;
+    const bool is_v = place & 1;
+    const int h = (int)((place >> 1) % (unsigned)p.n_kv), id = (int)((place >> 1) / (unsigned)p.n_kv);
     const int s = id < S ? id : uniform(request_at(seq_offsets, S, id - S));
     const int tok0 = uniform(seq_offsets[s]), n_all = uniform(seq_offsets[s + 1]) - tok0, r = id < S ? 0 : id - S - ((tok0 >> 6) + s) + 1;
     if (tok0 < 0 || n_all < 0 || n_all > T - tok0) {
@@ -320,6 +322,8 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__rest
     }
 }
 
+constexpr int64_t AT_ONCE = 1 << 23;   // workgroups of a launch, whose threads number less than 2^32
+
 template <int D>
 hipError_t launch_append(const KvPages &p, const void *k, const void *v, int64_t k_stride, int64_t v_stride, int64_t T, const int *seq_offsets,
                          int S, const int *slots, int *err_word, hipStream_t stream)
@@ -327,8 +331,10 @@ hipError_t launch_append(const KvPages &p, const void *k, const void *v, int64_t
     const int64_t places = T / 64 + 2 * (int64_t)S;
     auto go = [&](auto nt) {
         constexpr int NT = decltype(nt)::value;
-        hipLaunchKernelGGL((kv8_append_kernel<D, NT>), dim3((unsigned)(places * 2 * p.n_kv)), dim3(NT), 0, stream, p, static_cast<const char *>(k),
-                           static_cast<const char *>(v), k_stride, v_stride, (int)T, seq_offsets, S, slots, err_word);
+        const int64_t all = places * 2 * p.n_kv;
+        for (int64_t at = 0; at < all; at += AT_ONCE)
+            hipLaunchKernelGGL((kv8_append_kernel<D, NT>), dim3((unsigned)std::min(all - at, AT_ONCE)), dim3(NT), 0, stream, (unsigned)at, p,
+                               static_cast<const char *>(k), static_cast<const char *>(v), k_stride, v_stride, (int)T, seq_offsets, S, slots, err_word);
     };
     // (a token or a few to a request: a wave has room for them, and four would wait for each other)
     if (T <= 4 * (int64_t)S) go(std::integral_constant<int, 64>{});
@@ -339,8 +345,10 @@ hipError_t launch_append(const KvPages &p, const void *k, const void *v, int64_t
 template <int D>
 hipError_t launch_gather(const KvPages &p, void *k, void *v, int64_t T, const int *slots, int *err_word, hipStream_t stream)
 {
-    hipLaunchKernelGGL(kv8_gather_kernel<D>, dim3((unsigned)((T + 63) / 64 * 2 * p.n_kv)), dim3(256), 0, stream, p, static_cast<char *>(k),
-                       static_cast<char *>(v), T, slots, err_word);
+    const int64_t row = (int64_t)p.n_kv * D * 2, most = std::max<int64_t>(1, AT_ONCE / (2 * p.n_kv)) * 64;
+    for (int64_t t = 0; t < T; t += most)
+        hipLaunchKernelGGL(kv8_gather_kernel<D>, dim3((unsigned)((std::min(T - t, most) + 63) / 64 * 2 * p.n_kv)), dim3(256), 0, stream, p,
+                           static_cast<char *>(k) + t * row, static_cast<char *>(v) + t * row, std::min(T - t, most), slots + t, err_word);
     return hipGetLastError();
 }
 

@@ -95,13 +95,14 @@ __global__ __launch_bounds__(64 * WAVES) void qk_norm_rope_kernel(RotateArgs a, 
 #pragma unroll
             for (int d = 1; d < LPH; d <<= 1) sum += __shfl_xor(sum, d);
             float r = rsqrtf(sum * (1.f / D) + a.eps);
-            if (__ballot(!(sum < 1e36f) || (sum < 1e-30f && a.eps < 1e-25f))) {   // squares that fp32 does not hold
+            const bool beyond = !(sum < 1e36f) || (sum < 1e-30f && a.eps < 1e-25f);
+            if (__ballot(beyond)) {   // squares that fp32 does not hold
                 double wide = 0.0;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) wide = fma((double)x0[i], (double)x0[i], fma((double)x1[i], (double)x1[i], wide));
 #pragma unroll
                 for (int d = 1; d < LPH; d <<= 1) wide += __shfl_xor(wide, d);
-                r = (float)(1.0 / sqrt(wide * (1.0 / D) + (double)a.eps));
+                if (beyond) r = (float)(1.0 / sqrt(wide * (1.0 / D) + (double)a.eps));   // (the wave's other heads: as they would be without this one)
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -164,8 +165,21 @@ hipError_t launch(const RotateArgs &a, hipStream_t stream)
 
 }  // namespace
 
-hipError_t launch_qk_norm_rope(const RotateArgs &a, hipStream_t stream)
+hipError_t launch_qk_norm_rope(const RotateArgs &all, hipStream_t stream)
 {
+    RotateArgs a = all;
+    constexpr int64_t AT_ONCE = 1 << 24;   // tokens of a launch, whose threads number less than 2^32
+    for (; a.T > AT_ONCE; a.T -= AT_ONCE) {
+        RotateArgs part = a;
+        part.T = AT_ONCE;
+        const hipError_t e = launch_qk_norm_rope(part, stream);
+        if (e != hipSuccess) return e;
+        auto on = [](const void *p, int64_t elements) { return static_cast<const char *>(p) + AT_ONCE * elements; };
+        const int eb = a.x_f32 ? 4 : 2;
+        if (a.q) a.q = on(a.q, a.q_stride * eb), a.q_out = const_cast<char *>(on(a.q_out, a.q_out_stride * 2));
+        if (a.k) a.k = on(a.k, a.k_stride * eb), a.k_out = const_cast<char *>(on(a.k_out, a.k_out_stride * 2));
+        if (a.positions) a.positions += AT_ONCE;
+    }
     switch (a.D) {
     case 64: return a.x_f32 ? launch<64, true>(a, stream) : launch<64, false>(a, stream);
     case 128: return a.x_f32 ? launch<128, true>(a, stream) : launch<128, false>(a, stream);

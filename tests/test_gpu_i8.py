@@ -94,6 +94,17 @@ def test_the_largest_sums_do_not_wrap():
     ctx().check()
 
 
+def test_more_rows_than_a_launch_takes():
+    rows, far = 2 ** 23 + 3, 2 ** 23 - 2
+    x = torch.zeros((rows, 8), dtype=BF16, device="cuda")
+    x[:5], x[far:] = normal(9, 5, 8), normal(10, 5, 8)
+    got = moin.moin_i8_quantize(ctx(), x)
+    for at in (0, far):
+        want = moin.moin_i8_quantize(ctx(), x[at:at + 5].clone())
+        assert torch.equal(got.codes[at:at + 5], want.codes) and torch.equal(got.scales[at:at + 5], want.scales)
+    assert not got.codes[5:far].any() and (got.scales[5:far] == 2.0 ** -126).all()
+
+
 def test_rows_and_channels_with_nans_stay_alone():
     for T in (4, 40, 100):
         p = Product(T, T, 512, 72)

@@ -108,6 +108,29 @@ def test_magnitudes_whose_squares_fp32_does_not_hold(size, eps, dtype):
     check(x.to(dtype), pos, gains, 6, 2, moin.rope_frequencies(64), eps=eps)
 
 
+def test_heads_do_not_depend_on_others_magnitudes():
+    qkv, pos, gains = inputs(12, 600, 30, 2, 64)
+    kw = dict(positions=pos, freqs=moin.rope_frequencies(64), q_gain=gains[0], k_gain=gains[1])
+    want, _ = moin.moin_qk_norm_rope(ctx(), qkv[:, :30], qkv[:, 30:32], **kw)
+    qkv[:, 0] *= 1e30
+    got, _ = moin.moin_qk_norm_rope(ctx(), qkv[:, :30], qkv[:, 30:32], **kw)
+    assert torch.equal(got[:, 1:], want[:, 1:])
+
+
+def test_more_tokens_than_a_launch_takes():
+    T, far = 2 ** 24 + 3, 2 ** 24 - 2
+    q = torch.zeros((T, 1, 64), dtype=BF16, device="cuda")
+    pos = torch.arange(T, dtype=I32, device="cuda")
+    qkv, _, gains = inputs(13, 5, 1, 0, 64)
+    q[:5], q[far:] = qkv[:, :1], qkv[:, :1]
+    kw = dict(freqs=moin.rope_frequencies(64), q_gain=gains[0])
+    got, _ = moin.moin_qk_norm_rope(ctx(), q, None, positions=pos, **kw)
+    for at in (0, far):
+        want, _ = moin.moin_qk_norm_rope(ctx(), qkv[:, :1], None, positions=pos[at:at + 5].clone(), **kw)
+        assert torch.equal(got[at:at + 5], want)
+    assert not got[5:far].any()
+
+
 def test_position_zero_passes_everything():
     qkv, pos, gains = inputs(6, 5, 4, 2, 64)
     pos.zero_()
