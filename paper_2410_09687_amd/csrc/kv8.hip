@@ -4,7 +4,7 @@
 // it grows, what the block holds is rounded again -- a shift of the exponent, exact but for values that become subnormal.
 //
 // So the block, not the token, is what a workgroup takes: it alone reads and writes its codes of one head's keys or values.  Bound by memory: 65536 tokens of
-// eight heads of 128 95 us, 4.2 TB/s, and back 101, 4.1 TB/s (a copy of 1 GiB 5.0); 256 single tokens of four heads of 64 6.2 us, a chain of
+// eight heads of 128 97 us, 4.2 TB/s, and back 81 - 96, 4.2 - 5.0 TB/s (a copy of 1 GiB 5.0); 256 single tokens of four heads of 64 6.2 us, a chain of
 // four trips to memory.
 #include <algorithm>
 #include <type_traits>
@@ -209,7 +209,8 @@ __global__ __launch_bounds__(NT) void kv8_append_kernel(unsigned place0, KvPages
     }
 }
 
-// 64 tokens of the batch, one head's keys (blockIdx.x even) or values.  (Values a byte at a time, lanes as tokens: 219 us instead of 101 for 65536 tokens.)
+// 64 tokens of the batch, one head's keys (blockIdx.x even) or values.  (Values a byte at a time, lanes as tokens: 219 us instead of 101 for 65536 tokens; each quad reading its slots itself: a trip
+// to memory more, 101 and 9.2 instead of 96 and 7.6 for 256 requests' last 31 tokens.)
 template <int D>
 __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__restrict__ k, char *__restrict__ v, int64_t T,
                                                          const int *__restrict__ slots, int *err_word)
@@ -218,8 +219,7 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__rest
     const bool is_v = blockIdx.x & 1;
     const int h = (int)((blockIdx.x >> 1) % (unsigned)p.n_kv);
     const int64_t t0 = (int64_t)((blockIdx.x >> 1) / (unsigned)p.n_kv) * 64;
-    auto place = [&](int64_t t, const char *&rec, int &tok, float &unit) {   // false: zeros
-        const int slot = slots[t];
+    auto place = [&](int slot, const char *&rec, int &tok, float &unit) {   // false: zeros
         const bool in = slot >= 0 && (slot >> log_page) < p.n_pages;
         if (!in && slot != -1) atomicOr(err_word, ERR_BAD_PAGE);
         const int at = in ? slot & ((1 << log_page) - 1) : 0;
@@ -240,21 +240,22 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__rest
         // Four tokens that lie in one word of every channel, eight channels: eight words, turned into the tokens' rows with v_perm.  The batch's tokens
         // need not begin where the cache's words do: the first and last quads are then cut off, and one more is needed.
         // A wave takes 8 quads x 8 groups of channels: 32 bytes of a channel's run, 128 of a token's row.
-        const int shift = max(slots[t0], 0) & 3, lane = tid & 63;
+        const int lane = tid & 63, own = t0 + lane < T ? slots[t0 + lane] : -1;   // (the batch's 64 slots in one trip to memory)
+        const int shift = max(uniform(own), 0) & 3;
         for (int b = tid >> 6; b < 3 * (D / 64); b += 4) {
             const int quad = b / (D / 64) * 8 + (lane & 7), c = (b % (D / 64) * 8 + (lane >> 3)) * 8;
-            if (quad > 16) continue;
             const int64_t first = t0 - shift + quad * 4;
             int slot[4];
             bool in[4];
-            int from = -1;
+            int from = -1, any = -1;
             bool one = true;   // the quad's tokens are neighbours in the cache, as a request's are
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int64_t t = first + e;
                 in[e] = t >= t0 && t < min(t0 + 64, T);
-                slot[e] = in[e] ? slots[t] : -1;
+                slot[e] = __shfl(own, (quad * 4 - shift + e) & 63);
                 if (in[e]) {
+                    any = slot[e];
                     if (from < 0) from = slot[e] - e;
                     one &= slot[e] == from + e && slot[e] >= 0 && (slot[e] >> log_page) < p.n_pages;
                 }
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__rest
                 const char *rec;
                 int tok;
                 float unit;
-                place(in[0] ? first : max(first, t0), rec, tok, unit);
+                place(any, rec, tok, unit);   // (whichever: they share their words)
                 const char *src = rec + 64 * D + ((tok >> 2) & 3) * 16 + (tok >> 4) * 4 + c * 64;
                 uint32_t w[8];
 #pragma unroll
@@ -291,7 +292,7 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__rest
                     const char *rec;
                     int tok;
                     float unit;
-                    if (!in[e] || !place(first + e, rec, tok, unit)) continue;
+                    if (!in[e] || !place(slot[e], rec, tok, unit)) continue;
                     const uint8_t *src = reinterpret_cast<const uint8_t *>(rec) + 64 * D + ((tok >> 2) & 3) * 16 + (tok >> 4) * 4 + (tok & 3) + c * 64;
                     uint32_t b[8];
 #pragma unroll
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__rest
             const char *rec;
             int tok;
             float unit;
-            const bool in = place(t, rec, tok, unit);
+            const bool in = place(slots[t], rec, tok, unit);
             const uint2 w = *reinterpret_cast<const uint2 *>(rec + (tok >> 4) * 16 * D + (c >> 6) * 1024 + (tok & 15) * 64 + (c & 63));
             const uint4 y = make_uint4(pair(w.x, unit, Low{}), pair(w.x, unit, High{}), pair(w.y, unit, Low{}), pair(w.y, unit, High{}));
             store_once(out + t * row + c * 2, in ? y : make_uint4(0, 0, 0, 0));
