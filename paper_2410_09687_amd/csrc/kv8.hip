@@ -210,7 +210,7 @@ __global__ __launch_bounds__(NT) void kv8_append_kernel(unsigned place0, KvPages
 }
 
 // 64 tokens of the batch, one head's keys (blockIdx.x even) or values.  (Values a byte at a time, lanes as tokens: 219 us instead of 101 for 65536 tokens; each quad reading its slots itself: a trip
-// to memory more, 101 and 9.2 instead of 96 and 7.6 for 256 requests' last 31 tokens.)
+// to memory more, 101 and 9.2 instead of 96 and 7.6 for the begun blocks of 256 requests.)
 template <int D>
 __global__ __launch_bounds__(256) void kv8_gather_kernel(KvPages p, char *__restrict__ k, char *__restrict__ v, int64_t T,
                                                          const int *__restrict__ slots, int *err_word)
