@@ -305,13 +305,15 @@ hipError_t launch_i8_quantize(const void *src, int64_t rows, int cols, void *cod
 }
 
 // Each group of 128 tokens reads the weight for itself, a workgroup all of its tokens' codes: what a token costs grows with d_in, what the tiles of
-// 128 x 128 cost does so over the parts of their contraction.  Us, few / tiles: 64 tokens 2048 -> 2048 9.8 / 12.7, 4096 -> 4096 14.5 / 15.9, 8192 -> 8192 28 / 25;
-// 128 2048 -> 5632 15.8 / 17.6, 2048 -> 256 13.6 / 12.2, 5632 -> 2048 28 / 17; 24 131072 -> 64 166 / 168.  More than one group only while each workgroup has
-// a compute unit of its own: 1000 tokens 1024 -> 256 11.4 / 13.7, 256 2048 -> 2048 14.2 / 16.2, but 1000 1024 -> 2048 27 / 22.
+// 128 x 128 cost does so over the parts of their contraction.  Us, few / tiles, weights out of memory: 64 tokens 2048 -> 2048 10.9 / 13.1, 4096 -> 4096
+// 15.8 / 16.9, 5632 -> 2048 18.9 / 17.0; 128 2048 -> 5632 16.9 / 18.6, 2048 -> 256 14.0 / 12.9, 4096 -> 4096 23 / 20; 32 8192 -> 28672 55 / 59, 8192 -> 1024 17.0 / 17.9; 24
+// 32768 -> 2048 48 / 43, 16 of it 39 / 43.  Large weights of many outputs: 32 tokens 4096 -> 14336 22.6 / 21.1, 64 29 / 23; 96 2048 -> 32000 34 / 23.  More than one group
+// only while each workgroup has a compute unit of its own: 1000 tokens 1024 -> 256 11.4 / 13.7, 256 2048 -> 2048 14.3 / 16.0, but 1000 1024 -> 2048 27 / 22.
 bool i8_few_pays(int64_t T, int d_in, int d_out)
 {
     const int64_t tiles = (d_out + 15) / 16;
     if (T <= 24) return true;
+    if (T > 32 && d_out >= 32 * compute_units() && (int64_t)d_in * d_out >= 1 << 25) return false;
     return std::min<int64_t>(T, 128) * d_in <= 1 << 18 && (T <= 128 || (T + 127) / 128 * tiles <= compute_units());
 }
 

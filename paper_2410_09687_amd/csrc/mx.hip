@@ -602,8 +602,10 @@ __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
 
 // The same products, k-step for k-step in the same order, on 128 x 128 tiles, one per workgroup of four waves (2 x 2 accumulators
 // each), for calls whose 256 x 256 tiles do not fill the chip: the small batches and narrow projections of decode
-// and prefill.  LDS bounds it (see linear_mid.hip); two workgroups share a compute unit, two stages each (four stages and
-// the unit to itself: the same time where there is a tile per unit).
+// and prefill.  LDS bounds it (see linear_mid.hip); two workgroups share a compute unit, two stages each; where
+// there is a tile per unit or less, three stages cover the trip to memory that the other workgroup's work covers else.  Us of the kernel on integers, 2 / 3
+// stages: 1000 tokens 4096 -> 4096 26.9 / 22.5, 1300 5632 -> 2048 33.6 / 24.0, 200 4096 -> 14336 26.7 / 20.1, but 1300 4096 -> 4096 (352 tiles) 31 / 36 (four
+// stages: as three).
 // Us of a layer, seven projections, 256 x 256 tiles / these: decode of 1 token 167 / 133, 69 225 / 188, 338 327 / 285, 1000 463 /
 // 424.  Of the kernel: 2048 -> 2048 1890 tokens 28 / 20, 4096 30 / 25; 5632 -> 2048 1890 tokens 57 / 42, 4096 61 / 52.
 namespace mxm {
@@ -618,10 +620,11 @@ constexpr int BT = 128, FP = 2, FQ = 2;
 constexpr int OP_BYTES = BT * ROWB;
 constexpr int LOADS = 4;                  // requests of a wave per operand per block, 8 rows each, and on FP8 one of scale words
 constexpr int SC_BYTES = 2 * BT * 4;      // scale words of a block: 128 output rows, then 128 tokens
-constexpr int NS = 2, STAGE_BYTES = 2 * OP_BYTES + SC_BYTES;   // 33 KB a stage
+constexpr int STAGE_BYTES = 2 * OP_BYTES + SC_BYTES;   // 33 KB a stage
 }  // namespace mxm
 
-template <int BASE, bool Y_F32>
+// NS: stages.
+template <int BASE, bool Y_F32, int NS>
 __global__ __launch_bounds__(mxm::NT, 2) void linear_mx_mid_kernel(mxs::Params p)
 {
     using namespace mxm;
@@ -845,8 +848,11 @@ static hipError_t allow_lds()
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_stream4_kernel<BASE, Y_F32>),
                                              hipFuncAttributeMaxDynamicSharedMemorySize, mxs::SMEM_BYTES);
     if (e != hipSuccess) return e;
-    return hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_mx_mid_kernel<BASE, Y_F32>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, mxm::NS * mxm::STAGE_BYTES);
+    const hipError_t e2 = hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_mx_mid_kernel<BASE, Y_F32, 2>),
+                                              hipFuncAttributeMaxDynamicSharedMemorySize, 2 * mxm::STAGE_BYTES);
+    if (e2 != hipSuccess) return e2;
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_mx_mid_kernel<BASE, Y_F32, 3>),
+                               hipFuncAttributeMaxDynamicSharedMemorySize, 3 * mxm::STAGE_BYTES);
 }
 
 hipError_t prepare_mx_kernels()
@@ -860,12 +866,11 @@ hipError_t prepare_mx_kernels()
 
 bool mx_stream_kernel_fits(int d_in, int r) { return d_in % 128 == 0 && d_in >= 256 && r % 64 == 0; }
 
-// 128 x 128 tiles as long as the chip holds all of them at a time, as in linear_mid.hip.  Us of the kernel, 256 x 256 tiles / these:
-// 2048 -> 2048 512 tiles 29.6 / 24.5, 544 29.8 / 33.6, 768 31.2 / 35.7; 5632 -> 2048 512 61 / 52, 544 61 / 76; 2048 -> 5632 528
-// 31.3 / 35.1.  (Beyond the larger tiles' first round about equal: 1152 56 / 52, 5632 outputs 1232 57 / 60.)  Per round of those, as
-// in linear_mid.hip, where row tiles are half empty or a round nearly so: 2048 -> 2048 64 sequences of 128 tokens 62 / 47, 20 of 300
-// 56 / 42; 2048 -> 5632 12 of 112 55 / 36, 64 of 128 172 / 134; 5632 -> 2048 64 of 128 133 / 95, 20 of 300 118 / 87.
-static bool mx_mid_pays(int64_t tiles, int64_t rounds, int n_cus) { return tiles <= 2 * n_cus * rounds; }
+// 128 x 128 tiles, two of which a compute unit holds, up to 2.6 of them a compute unit and round of the larger ones: rows half empty, or a last round nearly
+// so.  Us of the kernel, 256 x 256 tiles / these, rank 64, integers and FP8: 2048 -> 5632 20 sequences of 300 tokens (2.58) 130 / 113, 115 / 108; 4096 -> 4096 20 of
+// 300 (2.5) 162 / 138, 148 / 130; 5632 -> 2048 40 of 300 (2.5) 210 / 181, 194 / 170; integers without adapters 2048 -> 5632 3000 tokens (2.06) 59 / 53; but 4096 -> 4096 12 of
+// 500 (3) 113 / 114, 104 / 106; 2048 -> 5632 12 of 500 (2.75) 102 / 98, 90 / 93; 5632 -> 2048 12 of 500 (3) 74 / 83, 70 / 80; 16 of 1000 (4) 170 / 211, 151 / 186.
+static bool mx_mid_pays(int64_t tiles, int64_t rounds, int n_cus) { return 5 * tiles <= 13 * n_cus * rounds; }
 
 // Parts of the contraction range for the plain (decode) base product: a workgroup of the 128 x 128 tiles per compute unit
 // (two per unit lost up to 3 %), at least two blocks per part, at most four parts (the decode expand kernel sums up to
@@ -942,16 +947,20 @@ static hipError_t launch_stream(const PlanView &pv, const MxLinearArgs &a, int n
     p.plane_bytes = (int64_t)pv.T * a.lin.d_out * (a.lin.y_f32 ? 4 : 2);
     const int64_t cols = (a.lin.d_out + mxm::BT - 1) / mxm::BT;
     const int64_t rows = p.plain ? (pv.T + mxm::BT - 1) / mxm::BT : host_tiles(pv, mxm::BT);
-    if (mx_mid_pays(rows * cols, p.plain ? 1 : tile_rounds(pv, p.n_tiles_n, n_cus), n_cus)) {
+    const int64_t rounds = p.plain ? ((int64_t)p.tiles_m * p.n_tiles_n + n_cus - 1) / n_cus : tile_rounds(pv, p.n_tiles_n, n_cus);
+    if (mx_mid_pays(rows * cols, rounds, n_cus)) {
         p.n_tiles_n = (int)cols;
         p.tiles_m = (int)rows;
         const int64_t work = (p.plain ? rows * p.k_splits : (int64_t)pv.max_tiles * (TILE_M / mxm::BT)) * cols;
         if (work > 0x7ffffff0LL) return hipErrorInvalidValue;
         const dim3 grid((unsigned)((work + 7) / 8 * 8));
-        if (p.y_f32)
-            hipLaunchKernelGGL((linear_mx_mid_kernel<BASE, true>), grid, dim3(mxm::NT), mxm::NS * mxm::STAGE_BYTES, stream_, p);
-        else
-            hipLaunchKernelGGL((linear_mx_mid_kernel<BASE, false>), grid, dim3(mxm::NT), mxm::NS * mxm::STAGE_BYTES, stream_, p);
+        auto go = [&](auto kernel, int stages) {
+            hipLaunchKernelGGL(kernel, grid, dim3(mxm::NT), stages * mxm::STAGE_BYTES, stream_, p);
+        };
+        // One more stage where a tile has its compute unit to itself: the kernel's comment.
+        const bool alone = rows * cols * p.k_splits <= n_cus;
+        if (p.y_f32) alone ? go(linear_mx_mid_kernel<BASE, true, 3>, 3) : go(linear_mx_mid_kernel<BASE, true, 2>, 2);
+        else alone ? go(linear_mx_mid_kernel<BASE, false, 3>, 3) : go(linear_mx_mid_kernel<BASE, false, 2>, 2);
         return hipGetLastError();
     }
     // one workgroup per compute unit (the LDS footprint allows no more), fewer
