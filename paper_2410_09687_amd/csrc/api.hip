@@ -723,7 +723,7 @@ int i8_plain(moin_ctx *ctx, const void *x, int64_t T, const void *Wq, const floa
     MxLinearArgs m{};
     m.plain_splits = 1;
     m.plain_kb_per_split = pitch / 128;
-    if (!few) mx_plain_shape(T, pitch, d_out, &m.plain_splits, &m.plain_kb_per_split);
+    if (!few) i8_parts(T, d_in, d_out, &m.plain_splits, &m.plain_kb_per_split);
     const bool parts = m.plain_splits > 1;
     const size_t xq_bytes = align_up((size_t)T * (size_t)pitch, 256), xs_bytes = align_up((size_t)T * 4, 256), row = (size_t)d_out * 4;
     const int rc = ensure_ws(ctx, xq_bytes + xs_bytes + (parts ? (size_t)m.plain_splits * (size_t)T * row : 0), stream, false,

@@ -284,6 +284,7 @@ hipError_t launch_i8_few(const void *x, const void *xq, const float *xs, const v
 hipError_t launch_linear_i8_stream(const PlanView &pv, const MxLinearArgs &a, int n_cus, hipStream_t stream);   // (xs, Ws: fp32)
 // y [T, d_out] from n parts' int32 sums, one after the other.
 hipError_t launch_i8_join(const void *parts, int n, const float *xs, const float *ws, int64_t T, int d_out, void *y, int y_f32, hipStream_t stream);
+void i8_parts(int64_t T, int d_in, int d_out, int *parts, int *per_part);   // of the contraction, in 128-byte blocks
 int64_t i8_parts_rows(int64_t T, int d_in, int d_out);   // the most rows of parts (n T, n > 1) that a product of up to T tokens takes
 
 // Norms and rotation of queries and keys (rotate.hip); strides in elements between the rows of tokens.

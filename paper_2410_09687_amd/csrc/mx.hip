@@ -909,6 +909,18 @@ int64_t mx_plain_rows(int64_t T, int d_in, int d_out)
     return most;
 }
 
+// Parts of the product without adapters, which a launch of their own has to add: where they spare each tile 16 blocks or more.  Us with and without: 700 tokens 5632 ->
+// 2048 (22 blocks) 28 / 34, 300 4096 -> 4096 (16) 23 / 25, 100 4096 -> 14336 (16) 26.4 / 28.4, but 400 4096 -> 4096 (16) 27.7 / 25.8, 400 2048 -> 2048 (12) 20.0 / 16.3, 1000
+// (8) 23.7 / 18.2, 200 2048 -> 5632 (8) 19.2 / 16.4.
+void i8_parts(int64_t T, int d_in, int d_out, int *parts, int *per_part)
+{
+    const int blocks = i8_pitch(d_in) / 128;
+    mx_plain_shape(T, i8_pitch(d_in), d_out, parts, per_part);
+    if (blocks - *per_part >= 16) return;
+    *parts = 1;
+    *per_part = blocks;
+}
+
 int64_t i8_parts_rows(int64_t T, int d_in, int d_out)
 {
     const int64_t cols = (d_out + mxm::BT - 1) / mxm::BT;
@@ -917,7 +929,7 @@ int64_t i8_parts_rows(int64_t T, int d_in, int d_out)
         const int64_t t = std::min<int64_t>(T, compute_units() / want / cols * mxm::BT);
         if (t <= 0) continue;
         int parts = 0, per = 0;
-        mx_plain_shape(t, i8_pitch(d_in), d_out, &parts, &per);
+        i8_parts(t, d_in, d_out, &parts, &per);
         if (parts > 1) most = std::max(most, t * parts);
     }
     return most;
