@@ -68,6 +68,31 @@ struct KvPlanView {
     bool has_few, has_tile;
 };
 
+// The list of tiles of many rows of up to this many requests goes by the keys that a tile sees, the most first (kv_slots_kernel).
+constexpr int KV_ORDERED_REQUESTS = 64;
+__host__ __device__ inline int kv_tiles_of(int n, int group) { return (int)(((int64_t)n * group + KV_TILE_ROWS - 1) / KV_TILE_ROWS); }
+// A request as that order has it: keys before its new tokens, those, its tiles and their parts; zeros: not in the list.  One that is not served has
+// no keys, whatever length it came with: keys and new tokens together stay below 2^31, and no position or difference of two wraps.
+struct alignas(16) KvListed {
+    int kv, n, tiles, parts;
+};
+__host__ __device__ inline KvListed kv_listed(const int4 &req, int n, int parts, int group)
+{
+    return req.w >= 0 ? KvListed{req.y >= 0 ? req.x : 0, n, kv_tiles_of(n, group), parts} : KvListed{0, 0, 0, 0};
+}
+// Position of the last row of its tile t: the first one ends with the last token, the others with row 128 k - 1.
+__host__ __device__ inline int kv_tile_sees(const KvListed &r, int t, int group)
+{
+    return r.kv + (t ? ((r.tiles - t) * KV_TILE_ROWS - 1) / group : r.n - 1);
+}
+// Records of request o in front of a tile of another that sees so much; `wins`: of equals o's come first.
+__host__ __device__ inline int kv_records_before(const KvListed &o, int sees, bool wins, int group)
+{
+    const int y = sees - o.kv + (wins ? 0 : 1);   // o's tokens from this one on see more, or as much and come first
+    // (tokens times group stay below 2^31 - 128)
+    return o.parts * (y <= 0 ? o.tiles : y >= o.n ? 0 : 1 + o.tiles - (y * group + KV_TILE_ROWS) / KV_TILE_ROWS);
+}
+
 struct KvPlanArgs {
     const int *kv_lens, *new_lens;
     int *block_table;

@@ -302,9 +302,6 @@ __global__ __launch_bounds__(PT) void kv_plan_kernel(KvPlanView v, KvPlanArgs a,
     }
 }
 
-constexpr int KV_ORDERED_REQUESTS = 64;
-__device__ __forceinline__ int tiles_of(int n, int group) { return (int)(((int64_t)n * group + KV_TILE_ROWS - 1) / KV_TILE_ROWS); }
-
 // Slots, table entries and tiles of requests with many new tokens: workgroup (request, chunk of 2048 tokens).
 __global__ __launch_bounds__(256) void kv_slots_kernel(KvPlanView v, KvPlanArgs a, int log_page)
 {
@@ -323,7 +320,7 @@ __global__ __launch_bounds__(256) void kv_slots_kernel(KvPlanView v, KvPlanArgs 
     if (q.w < 0 || !v.has_tile) return;
     const int L = served ? kv + n : 0;
     const int2 t2 = v.req_tiles[s];
-    const int parts = t2.x, n_tiles = tiles_of(n, v.group), recs = n_tiles * parts;
+    const int parts = t2.x, n_tiles = kv_tiles_of(n, v.group), recs = n_tiles * parts;
     if (q.w + recs > v.max_tile || (parts > 1 && t2.y + recs * KV_TILE_PLACES > v.max_pslots)) return;
     // Few requests: the list goes by the keys that a tile sees, over all of them, so that the last workgroups of the attention are short ones (a
     // request after the other, the last one's longest tiles begin when most of the chip has nothing left).  A tile's place is the number of those before
@@ -331,13 +328,10 @@ __global__ __launch_bounds__(256) void kv_slots_kernel(KvPlanView v, KvPlanArgs 
     // 8 heads on 2 of 256, 150 / 103 and 155 / 104; 64 of up to 300 tokens behind up to 2000 160 / 143 and 163 / 146.  Of the plan: eight requests
     // 11.0 / 12.6, 64 12.0 / 13.7.
     const bool ordered = v.S > 1 && v.S <= KV_ORDERED_REQUESTS && v.head[3] <= v.max_tile;
-    __shared__ int4 other[KV_ORDERED_REQUESTS];   // {keys before, new tokens, tiles, parts}; zeros: not in the list
+    __shared__ KvListed listed[KV_ORDERED_REQUESTS];
     if (ordered) {
-        for (int i = tid; i < v.S; i += 256) {
-            const int4 o = v.req[i];
-            const int on = a.seq_offsets[i + 1] - a.seq_offsets[i];
-            other[i] = o.w >= 0 ? make_int4(o.x, on, tiles_of(on, v.group), v.req_tiles[i].x) : make_int4(0, 0, 0, 0);
-        }
+        for (int i = tid; i < v.S; i += 256)
+            listed[i] = kv_listed(v.req[i], a.seq_offsets[i + 1] - a.seq_offsets[i], v.req_tiles[i].x, v.group);
         __syncthreads();
     }
     auto write = [&](int r, int at) {
@@ -349,17 +343,12 @@ __global__ __launch_bounds__(256) void kv_slots_kernel(KvPlanView v, KvPlanArgs 
         return;
     }
     // eight lanes to a tile
+    const KvListed own = listed[s];
     for (int r0 = c * 32; r0 < recs; r0 += nc * 32) {
-        const int r = r0 + tid / 8, t = r / parts;
-        const int sees = kv + (t ? ((n_tiles - t) * KV_TILE_ROWS - 1) / v.group : n - 1);   // position of the tile's last row
+        const int r = r0 + tid / 8, sees = kv_tile_sees(own, r / parts, v.group);
         int at = 0;
-        for (int i = tid & 7; i < v.S; i += 8) {
-            const int4 o = other[i];
-            const int y = sees - o.x + (i < s ? 0 : 1);   // its tokens from this one on see more, or as much and come first
-            // (tokens times group stay below 2^31.  The first tile ends with the last token, the others with row 128 k - 1.)
-            const int before = y <= 0 ? o.z : y >= o.y ? 0 : 1 + o.z - (y * v.group + KV_TILE_ROWS) / KV_TILE_ROWS;
-            at += i == s ? 0 : before * o.w;
-        }
+        for (int i = tid & 7; i < v.S; i += 8)
+            if (i != s) at += kv_records_before(listed[i], sees, i < s, v.group);
 #pragma unroll
         for (int d = 1; d < 8; d <<= 1) at += __shfl_xor(at, d);
         if (r < recs && (tid & 7) == 0) write(r, r + at);
