@@ -1,12 +1,13 @@
 // Matrix product in 8-bit integers: rows of x [T, d_in] and of the weight [d_out, d_in] have a scale each,
 //     s = max(amax / 127 in fp32, 2^-126),   code = x / s to the nearest, ties to even,   y = s_t s_o sum_c xq_c wq_c,
-// sums in int32, exact; one rounding to fp32, two for the scales.  A row with an infinity or a NaN has a scale of NaN and codes of 0.
+// sums in int32, exact; one rounding to fp32, two for the scales (i8_scale.h).  A row with an infinity or a NaN has a scale of NaN and codes of 0.
 // (s rounded to fp32 belongs to the definition, so that codes are the same wherever they are made.)
 // This file: the quantiser, and the product of up to 128 tokens, bound by the weight's bytes.  Larger ones run on the
 // streams of tiles of mx.hip.
 #include <algorithm>
 
 #include "gemm_core.h"
+#include "i8_scale.h"
 #include "kernels.h"
 
 namespace moin {
@@ -241,11 +242,11 @@ __global__ __launch_bounds__(64 * KW) void i8_few_kernel(FewArgs a)
         for (int k = 1; k < KW; ++k) v += sums[k * RT * NT * 64 + i];
         const int t = (i >> 6) % NT * 16 + (i & 15), o = n0 + (i >> 6) / NT * 16 + ((i & 63) >> 4) * 4;
         if (t >= a.T || o >= a.d_out) continue;
-        const float st = lds_s[t];
+        const I8Token st(lds_s[t]);
         const f32x4_t so = *reinterpret_cast<const f32x4_t *>(a.ws + o);
         float r[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = (float)v[e] * (st * so[e]);
+        for (int e = 0; e < 4; ++e) r[e] = st(v[e], so[e]);
         const int64_t at = (int64_t)t * a.d_out + o;
         if (a.y_f32) *reinterpret_cast<float4 *>(a.y + at * 4) = make_float4(r[0], r[1], r[2], r[3]);
         else *reinterpret_cast<uint2 *>(a.y + at * 2) = make_uint2(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]));
@@ -261,11 +262,11 @@ __global__ __launch_bounds__(256) void i8_join_kernel(const i32x4_t *__restrict_
     i32x4_t v = parts[q];
     for (int u = 1; u < n; ++u) v += parts[u * quads + q];
     const int64_t t = q / per_row;
-    const float st = xs[t];
+    const I8Token st(xs[t]);
     const f32x4_t so = reinterpret_cast<const f32x4_t *>(ws)[q - t * per_row];
     float r[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = (float)v[e] * (st * so[e]);
+    for (int e = 0; e < 4; ++e) r[e] = st(v[e], so[e]);
     if (y_f32) *reinterpret_cast<float4 *>(y + q * 16) = make_float4(r[0], r[1], r[2], r[3]);
     else *reinterpret_cast<uint2 *>(y + q * 8) = make_uint2(pack_bf16x2(r[0], r[1]), pack_bf16x2(r[2], r[3]));
 }

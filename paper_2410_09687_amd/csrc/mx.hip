@@ -26,6 +26,7 @@
 #include <type_traits>
 
 #include "gemm_core.h"
+#include "i8_scale.h"
 #include "kernels.h"
 #include "stream_epilogue.h"
 #include "stream_tile.h"
@@ -259,9 +260,13 @@ __device__ __forceinline__ f32x16_t i8_products(const Frag &a, const Frag &b, f3
 template <bool AGPR, int FP, int FQ>
 __device__ __forceinline__ void i8_scale(f32x16_t (&acc)[FP][FQ], const char *out, const char *tok, int lane)
 {
-    float st[FQ];
+    float st[FQ], far[FQ];
 #pragma unroll
-    for (int j = 0; j < FQ; ++j) st[j] = *reinterpret_cast<const float *>(tok + (j * 32 + (lane & 31)) * 4);
+    for (int j = 0; j < FQ; ++j) {
+        const I8Token t(*reinterpret_cast<const float *>(tok + (j * 32 + (lane & 31)) * 4));
+        st[j] = t.s;
+        far[j] = t.far;
+    }
 #pragma unroll
     for (int i = 0; i < FP; ++i) {
         f32x4_t so[4];
@@ -269,20 +274,24 @@ __device__ __forceinline__ void i8_scale(f32x16_t (&acc)[FP][FQ], const char *ou
         for (int g = 0; g < 4; ++g) so[g] = *reinterpret_cast<const f32x4_t *>(out + (i * 32 + 8 * g + 4 * (lane >> 5)) * 4);
 #pragma unroll
         for (int j = 0; j < FQ; ++j) {
+            // (AGPR: in place, register by register: as a whole the accumulator would be copied, and others spilled for it.  Sixteen at a time: one after the
+            // other each step waits for the one before it.)
+            float v[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
+            for (int e = 0; e < 16; ++e)
+                if constexpr (AGPR) asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v[e]) : "a"(acc[i][j][e]));
+                else v[e] = acc[i][j][e];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[e] = i8_result((int)f32_bits(v[e]), st[j], far[j], so[e >> 2][e & 3]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
                 if constexpr (AGPR) {
-                    // (in place, register by register: as a whole the accumulator would be copied, and others spilled for it)
-                    int v;
-                    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(acc[i][j][e]));
-                    const float f = (float)v * (st[j] * so[e >> 2][e & 3]);
                     float x;
-                    asm volatile("v_accvgpr_write_b32 %0, %1" : "=a"(x) : "v"(f));
+                    asm volatile("v_accvgpr_write_b32 %0, %1" : "=a"(x) : "v"(v[e]));
                     acc[i][j][e] = x;
                 } else {
-                    acc[i][j][e] = (float)(int)f32_bits(acc[i][j][e]) * (st[j] * so[e >> 2][e & 3]);
+                    acc[i][j][e] = v[e];
                 }
-            }
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -303,8 +312,9 @@ __device__ __forceinline__ void i8_scale(f32x16_t (&acc)[FP][FQ], const char *ou
 // are no scales, and every block takes the bf16 MFMAs); it is not instantiated:
 // measured against the eight-wave bf16 kernel on the 2048 -> 2048 prefill shape it
 // took 262 us against 252 us on the same device.
-// On integers the accumulators hold int32 sums through the base's blocks and become fp32 in front of the adapter's, five vector instructions a sum, one wave
-// on the SIMD, nothing to hide them: 16384 tokens 2048 -> 5632, rank 64, 215 us (FP8: 188), 8192 x 8192 x 8192 443, 2.5 PFLOP/s (FP8 408; the library's
+// On integers the accumulators hold int32 sums through the base's blocks and become fp32 in front of the adapter's, six vector instructions a sum, one wave
+// on the SIMD, nothing to hide them (five, the two scales multiplied first, lose what leaves fp32's range: 15720 tokens 2048 -> 5632 in 32
+// sequences 254.5 us with them, 256.5 with six sixteen sums at a time, 258 four at a time): 16384 tokens 2048 -> 5632, rank 64, 215 us (FP8: 188), 8192 x 8192 x 8192 443, 2.5 PFLOP/s (FP8 408; the library's
 // integer product 481).
 template <int BASE, bool Y_F32>
 __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
