@@ -43,12 +43,11 @@ __device__ __forceinline__ uint2 i8_codes(const uint4 &v, float s, float inv)
         q[i] = rintf(x(i) * inv);
         most = fmaxf(most, fabsf(fmaf(-q[i], s, x(i))));
     }
-    const float half = 0.5f * s;
-    if (most >= half) {
+    if (2.f * most >= s) {   // (twice what is left, not half of s: the smallest scales have no half in fp32)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float left = fmaf(-q[i], s, x(i));
-            if (fabsf(left) > half || (fabsf(left) == half && ((int)q[i] & 1))) q[i] += copysignf(1.f, left);
+            const float left = fmaf(-q[i], s, x(i)), twice = 2.f * fabsf(left);
+            if (twice > s || (twice == s && ((int)q[i] & 1))) q[i] += copysignf(1.f, left);
         }
     }
     uint32_t c[2] = {0, 0};   // (of q + 128, whose high bit is then turned)
