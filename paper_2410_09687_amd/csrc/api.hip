@@ -724,16 +724,19 @@ int i8_plain(moin_ctx *ctx, const void *x, int64_t T, const void *Wq, const floa
     m.plain_splits = 1;
     m.plain_kb_per_split = pitch / 128;
     if (!few) i8_parts(T, d_in, d_out, &m.plain_splits, &m.plain_kb_per_split);
-    const bool parts = m.plain_splits > 1;
+    const bool parts = m.plain_splits > 1, quantised = !(few && i8_few_quantises(T, d_in));
     const size_t xq_bytes = align_up((size_t)T * (size_t)pitch, 256), xs_bytes = align_up((size_t)T * 4, 256), row = (size_t)d_out * 4;
-    const int rc = ensure_ws(ctx, xq_bytes + xs_bytes + (parts ? (size_t)m.plain_splits * (size_t)T * row : 0), stream, false,
-                             xq_bytes + xs_bytes + (size_t)i8_parts_rows(T, d_in, d_out) * row);
-    if (rc != MOIN_OK) return rc;
-    char *xq = static_cast<char *>(ctx->ws), *sums = xq + xq_bytes + xs_bytes;
-    float *xs = reinterpret_cast<float *>(xq + xq_bytes);
-    if (!(few && i8_few_quantises(T, d_in)) &&
-        timed(ctx, MOIN_K_MX_QUANT, stream, [&] { return launch_i8_quantize(x, T, d_in, xq, xs, stream); }) != hipSuccess)
-        return MOIN_EHIP;
+    char *xq = nullptr, *sums = nullptr;
+    float *xs = nullptr;
+    if (quantised) {   // (else there is nothing to keep, here or for fewer tokens)
+        const int rc = ensure_ws(ctx, xq_bytes + xs_bytes + (parts ? (size_t)m.plain_splits * (size_t)T * row : 0), stream, false,
+                                 xq_bytes + xs_bytes + (size_t)i8_parts_rows(T, d_in, d_out) * row);
+        if (rc != MOIN_OK) return rc;
+        xq = static_cast<char *>(ctx->ws);
+        xs = reinterpret_cast<float *>(xq + xq_bytes);
+        sums = xq + xq_bytes + xs_bytes;
+    }
+    if (quantised && timed(ctx, MOIN_K_MX_QUANT, stream, [&] { return launch_i8_quantize(x, T, d_in, xq, xs, stream); }) != hipSuccess) return MOIN_EHIP;
     if (timed(ctx, MOIN_K_I8_LINEAR, stream, [&] {
             if (few) return launch_i8_few(x, xq, xs, Wq, ws, (int)T, d_in, d_out, y, y_f32, stream);
             m.lin.y = parts ? sums : y;
