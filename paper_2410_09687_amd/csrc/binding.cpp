@@ -332,6 +332,12 @@ PyObject *plan_build(PyObject *const *a)
     return PyLong_FromLongLong(S);
 }
 
+// Whether a call has adapters: both stacks of them or neither.
+bool has_stacks(PyObject *A, PyObject *B)
+{
+    if ((A == Py_None) != (B == Py_None)) fail(PyExc_ValueError, "A_stack and B_stack go together");
+    return A != Py_None;
+}
 struct Dims {
     int32_t d_in, d_out, E, r;
 };
@@ -339,7 +345,7 @@ Dims stack_dims(const at::Tensor &W, PyObject *A, PyObject *B)
 {
     if (W.dim() != 2) fail(PyExc_ValueError, "W [d_out,d_in] expected");
     const int64_t d_out = W.size(0), d_in = W.size(1);
-    if (A == Py_None || B == Py_None) return Dims{size32(d_in), size32(d_out), 0, 0};
+    if (!has_stacks(A, B)) return Dims{size32(d_in), size32(d_out), 0, 0};
     const at::Tensor &a = tensor(A, "A_stack"), &b = tensor(B, "B_stack");
     if (a.dim() != 3 || b.dim() != 3 || a.size(2) != d_in || b.size(0) != a.size(0) || b.size(1) != d_out || b.size(2) != a.size(1))
         fail(PyExc_ValueError, "A_stack [E,r,d_in] / B_stack [E,d_out,r] shape mismatch");
@@ -755,7 +761,7 @@ Stacks stacks(PyObject *a, PyObject *b, int32_t d_in, int32_t d_out, PyObject *p
 {
     Stacks s{nullptr, nullptr, 0};
     int32_t E = 0;
-    if (a != Py_None && b != Py_None) {
+    if (has_stacks(a, b)) {
         const at::Tensor &A = tensor(a, "A_stack"), &B = tensor(b, "B_stack");
         if (A.dim() != 3 || B.dim() != 3 || A.size(2) != d_in || B.size(0) != A.size(0) || B.size(1) != d_out || B.size(2) != A.size(1))
             fail(PyExc_ValueError, "A_stack [E,r,d_in] / B_stack [E,d_out,r] shape mismatch");

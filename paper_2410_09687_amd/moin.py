@@ -307,7 +307,9 @@ def _y_out(x, d_out, y_dtype, out):
 
 def _stack_dims(W, A_stack, B_stack):
     d_out, d_in = W.shape
-    if A_stack is None or B_stack is None:
+    if (A_stack is None) != (B_stack is None):
+        raise ValueError("A_stack and B_stack go together")
+    if A_stack is None:
         return d_in, d_out, 0, 0
     E, r = A_stack.shape[0], A_stack.shape[1]
     if tuple(A_stack.shape) != (E, r, d_in) or tuple(B_stack.shape) != (E, d_out, r):
