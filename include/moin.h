@@ -715,9 +715,12 @@ int moin_kv8_attention(moin_ctx *ctx, const moin_kv_plan *plan, const moin_kv_pa
  *   moin_i8_quantize     src [rows, cols] bf16 -> codes [rows, pitch] int8, scales [rows] fp32
  *   moin_i8_linear       y [T, d_out] = s_t s_o sum_c xq wq, any T: x [T, d_in] bf16 is quantised by the call, a scale
  *                        for each token; Wq [d_out, pitch], ws [d_out] from moin_i8_quantize, a scale for each channel.
- *                        Sums are exact (int32) and rounded to fp32 once.
+ *                        Sums are exact (int32) and rounded to fp32 once, so are the products with s_t and then with s_o, in all of
+ *                        fp32's range.  A few tokens of a few thousand columns take no workspace.
  *   moin_lora_linear_i8_planned
- *                        moin_lora_linear_planned on such a base: the adapters' products are those of the bf16 x.
+ *                        moin_lora_linear_planned on such a base: the adapters' products are those of the bf16 x.  Without adapters
+ *                        as moin_i8_linear; with them the base's sum is rounded to fp32 in up to four parts of the contraction
+ *                        on the decode path, which are added in fp32, and the adapters' terms are added to it in fp32.
  * cols / d_in a multiple of 8 up to 131072, d_out of 8, r of 64; pointers 16-byte aligned (src, codes, ws too).  Stacks,
  * y, workspace (the tokens' codes, 2 T r bf16, planes of partial sums) and errors as in moin_lora_linear_mx_planned. */
 int64_t moin_i8_pitch(int64_t cols);

@@ -10,12 +10,12 @@
 // scale for 64 tokens and all channels leaves an integer's small channels few steps; and the card converts two of them an instruction.)
 //
 // Tiles of few rows are bound by memory, 128 D bytes a record and kv head: 256 requests of up to 4096 keys, 32 heads on 4 of 64 channels, 50 us, 5.4 TB/s (a
-// copy of 1 GiB moves 5.0); two of 100000 and more, 64 heads on 8 of 128, 104 us, 4.6 TB/s, the difference being beginning and end: four times
-// as many keys take 3.3 times as long.  A thousand keys: 7.4 us, half a dozen trips to memory.  Registers for four waves of a SIMD instead of three
+// long contiguous read reaches 6.8, a copy 5.0 there and back); two of 100000 and more, 64 heads on 8 of 128, 104 us, 4.6 TB/s: beginning, last records and joins take
+// a time that does not go with the keys (64 requests of 32 heads on 4 of 64: 8 us for one token, 12 for four, and 6.2 TB/s beside them); four times as many keys take 3.3 times as long.  A thousand keys: 7.4 us, half a dozen trips to memory.  Registers for four waves of a SIMD instead of three
 // (64 channels) spill: 96 us for the first.
-// Tiles of many rows are bound by the vector unit, as on the 4-bit cache: eight prompts of 2048, 32 heads on 4 of 64 channels, 183 us, 0.75 PFLOP/s; 198
+// Tiles of many rows are bound by the vector unit, as on the 4-bit cache: eight prompts of 2048, 32 heads on 4 of 64 channels, 177 - 185 us, 0.74 - 0.78 PFLOP/s; 198
 // vector instructions beside 32 of the matrix cores a wave and record by the counters, some 160 of them on the steady path (the softmax of 32 scores 104, packs 18, decoding
-// 18), the unit busy 72 % of the cycles in which a compute unit has work, the matrix cores 35 %.  Four waves of a SIMD instead of three change
+// 18), the unit busy 73 % of the cycles in which a compute unit has work, the matrix cores 35 %.  Four waves of a SIMD instead of three change
 // nothing (204, 212 us), nor does a higher priority for the decoding or the products (191 - 196).
 #include "attend_core.h"
 #include "kv8.h"

@@ -116,6 +116,9 @@ struct Columns {
         }
     }
 
+    // The weights enter the second product as bf16: their sum is taken in fp32 before, each rounding is at most 2^-9 of a weight, on its own, and the result
+    // is rounded by as much (prompts of 2048: error of 0.00182 of the results' norm, 0.00172 with three parts, of which 0.0017 are the result's own
+    // rounding).  fp32 results take three parts, 24 bits: eight such prompts 314 us over the 8-bit cache, 180 with one.
     static constexpr int NP = Y32 ? 3 : 1;
     using Scores = f32x4_t[NT][4];          // [.][tile of 16 keys]: this lane's row, its group's four keys
     using Weights = uint32_t[NP][NT][4][2]; // as a sum of NP bf16, keys 0 1 and 2 3 of a tile's four

@@ -117,7 +117,8 @@ struct FewArgs {
 // operands are 16 bytes of a row as they lie in memory (the order of the contraction is free).
 // FUSED: the workgroup quantises the tokens itself, into LDS, while its first weights are on their way: a launch less (one token 2048 -> 5632 10.7 us when
 // one wave did it, 5.6 with pieces dealt to sixteen).
-// One token 8192 -> 28672 45 us, 5.2 TB/s of weights; 24 tokens 48, 4.8 TB/s, where the tokens come out of L2 for every 64 outputs.  In turn instead of in
+// One token 8192 -> 28672 44 us, 5.4 TB/s of weights (a long read: 6.8), 41 where the last-level cache has part of the 235 MB from the call before; 24 tokens 48, 4.8 TB/s,
+// where the tokens come out of L2 for every 64 outputs.  In turn instead of in
 // ranges the waves' blocks take 55 and 65 (of 32 outputs); 24 tokens and 16 / 32 / 64 outputs a workgroup 77 / 64 / 54, 64 tokens 134 / 97 / 73.  Past the
 // caches: 61 for the 24.
 template <int RT, int NT, int KW, bool FUSED>

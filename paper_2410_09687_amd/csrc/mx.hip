@@ -314,8 +314,8 @@ __device__ __forceinline__ void i8_scale(f32x16_t (&acc)[FP][FQ], const char *ou
 // took 262 us against 252 us on the same device.
 // On integers the accumulators hold int32 sums through the base's blocks and become fp32 in front of the adapter's, six vector instructions a sum, one wave
 // on the SIMD, nothing to hide them (five, the two scales multiplied first, lose what leaves fp32's range: 15720 tokens 2048 -> 5632 in 32
-// sequences 254.5 us with them, 256.5 with six sixteen sums at a time, 258 four at a time): 16384 tokens 2048 -> 5632, rank 64, 215 us (FP8: 188), 8192 x 8192 x 8192 443, 2.5 PFLOP/s (FP8 408; the library's
-// integer product 481).
+// sequences 254.5 us a call with them, 256.5 with six sixteen sums at a time, 258 four at a time).  16384 tokens 2048 -> 5632, rank 64, 208 us (FP8: 188),
+// 8192 x 8192 x 8192 435, 2.5 PFLOP/s (FP8 408; the library's integer product 481).
 template <int BASE, bool Y_F32>
 __global__ __launch_bounds__(mxs::NT) void linear_stream4_kernel(mxs::Params p)
 {
